@@ -319,7 +319,7 @@ def run(c):
     if c["kind"] == "route":
         r = dgs.route_experts(c["logits"], c["k"], score=c["score"], bias=c["balance"], groups=c["groups"], groups_kept=c["kept"],
                               group_best=c["best"], renormalise=c["renorm"], scale=c["scale"])
-        return {"expert": r.expert, "weight": r.weight, "offsets": r.offsets, "order": r.order, "place": r.place}
+        return {"expert": r.expert, "weight": r.weight, "offsets": r.offsets, "order": r.order, "place": r.place.view(-1)}
     if c["kind"] == "route_grad":
         return {"dlogits": dgs.route_experts_grad(c["logits"], c["expert"], c["dweight"], score=c["score"], renormalise=c["renorm"],
                                                   scale=c["scale"])}
