@@ -326,6 +326,133 @@ int dgs_topk_encode_static(const float* x, uint32_t n, uint32_t k, uint32_t* out
  * it allocates nothing (one 4-byte copy from the fixed array). */
 int dgs_topk_encode_static_status(void* stream, int* device_status);
 
+/* ---- what a worker computes before its push ------------------------------------------------------------------
+ *
+ * (No counterparts in the paper, whose workers compute their gradients with a framework.)  The calls below take a
+ * worker from its activations to the flat gradient vector that dgs_worker_push reads: activations held in 8 bits
+ * between forward and backward pass, weight and bias gradients formed from them and written to the layers'
+ * slices of that vector, and, for models with experts, the router whose selection says which rows belong to which
+ * expert.  They need no context.  Common rules:
+ *   - Nothing is allocated; outputs and workspaces are the caller's.  Work is enqueued on `stream` (a cudaStream_t of
+ *     the current device; NULL = default stream) and the call returns.  All of them may be captured into a graph.
+ *     Two calls whose work may overlap need workspaces of their own.
+ *   - Results are the same bits for the same inputs, on every run.
+ *   - Outputs must not overlap inputs unless a call says so; where the ranges do, it returns DGS_EINVAL.
+ *   - Sizes of zero rows (tokens) are legal: outputs that do not depend on rows are still written.
+ *   - A row index or a list that points outside its matrix is skipped on the device and reported by
+ *     dgs_operator_status. */
+
+enum { DGS_TYPE_F32 = 0, DGS_TYPE_BF16 = 1, DGS_TYPE_FP16 = 2 };
+
+/* A matrix of the caller: element [r][c] is data[r * stride + c].  stride >= cols, or 0 for a matrix that is only read
+ * and whose rows are all the same one.  data is aligned to the element.  rows < 2^32. */
+typedef struct {
+  void* data;      /* DEVICE */
+  uint64_t rows;
+  uint64_t stride; /* elements */
+  uint32_t cols;
+  uint32_t type;   /* DGS_TYPE_* */
+} dgs_matrix;
+
+enum { DGS_FORMAT_INT8 = 0, /* codes are int8, -127 .. 127            */
+       DGS_FORMAT_E4M3 = 1 /* codes are e4m3 numbers, up to 448 */ };
+enum { DGS_ACT_NONE = 0, DGS_ACT_RELU = 1, DGS_ACT_GELU = 2, DGS_ACT_GELU_TANH = 3, DGS_ACT_SILU = 4 };
+
+/* A rows x cols matrix held in 8 bits: one byte a value and one exponent byte for each 32 values of a row.  The
+ * buffer holds codes [rows][W], W = cols up to a multiple of 32, then scale bytes [rows][4 for each 128 columns begun]; a
+ * value is code * 2^(byte - 127), 2^e the smallest power of two for which the block's largest magnitude is at most
+ * 127 * 2^e (int8) or 448 * 2^e (e4m3), with e from -126 to 121 (int8) or -117 to 119 (e4m3).  Codes are rounded to
+ * nearest, ties to even: an int8 value is off by at most 2^e / 2, which is 1/127 of the block's largest magnitude, an
+ * e4m3 value by 2^-4 of itself (or 2^e / 1024 near zero).  A block that holds an infinity or a NaN gets byte 255 and reads as NaN.
+ * Bytes behind the last column are zero. */
+typedef struct {
+  void* data;      /* DEVICE, 16-byte aligned, dgs_checkpoint_bytes long */
+  uint64_t rows;   /* < 2^32 */
+  uint32_t cols;   /* 1 .. 2^30 */
+  uint32_t format; /* DGS_FORMAT_* */
+} dgs_checkpoint;
+
+int dgs_checkpoint_bytes(uint64_t rows, uint32_t cols, uint64_t* out_bytes);
+
+/* Holds x (rows x cols) in ckpt and, unless y is NULL, writes y = act(x), of x's type, in the same pass.  y may be x
+ * itself (in place).  act: DGS_ACT_*, DGS_ACT_NONE copies. */
+int dgs_checkpoint_save(const dgs_checkpoint* ckpt, const dgs_matrix* x, int act, const dgs_matrix* y, void* stream);
+
+/* Writes the values that ckpt holds to x (in f32 and bfloat16 exactly, in fp16 rounded). */
+int dgs_checkpoint_load(const dgs_checkpoint* ckpt, const dgs_matrix* x, void* stream);
+
+/* dx = dy * act'(h), h the values that ckpt holds; dx and dy are of one type, and may be the same matrix (in place).
+ * relu'(0) = 0. */
+int dgs_checkpoint_activation_grad(const dgs_checkpoint* ckpt, int act, const dgs_matrix* dy, const dgs_matrix* dx, void* stream);
+
+enum { DGS_WEIGHT_IN_OUT = 1u << 0, /* dw is [inputs][outputs]; without it [outputs][inputs] */
+       DGS_WEIGHT_ADD = 1u << 1     /* dw and db are added to; without it they are set      */ };
+
+/* Which rows belong to which expert.  Row j of dy with offsets[e] <= j < offsets[e + 1] belongs to expert e and to
+ * row rows[j] / rows_per of the checkpoint (to row j if rows is NULL).  Offsets ascend. */
+typedef struct {
+  const uint32_t* offsets; /* DEVICE u32[experts + 1] */
+  const uint32_t* rows;    /* DEVICE u32[rows of dy] or NULL */
+  uint32_t experts;
+  uint32_t rows_per;       /* >= 1 */
+} dgs_row_lists;
+
+/* The gradient of a layer y = x W (+ b) from dy and the checkpoint of x:
+ *     dw[o][i] = sum over rows r of dy[r][o] * h[r][i],     db[o] = sum over r of dy[r][o]
+ * dw: DEVICE f32, inputs * outputs elements (4-byte aligned: a layer's slice of the flat gradient); db: DEVICE f32[outputs]
+ * or NULL.  inputs = ckpt->cols, outputs = dy->cols.  With lists, one such gradient per expert over the expert's rows,
+ * dw [experts][...] and db [experts][outputs]; an expert without rows gets zeros.  Without lists (NULL) dy has the
+ * checkpoint's rows.  Products are exact and are summed in f32 (f16 and f32 gradients are taken apart into bfloat16
+ * numbers whose sum they are).  workspace: DEVICE, 16-byte aligned, at least what dgs_checkpoint_weight_grad_bytes says for
+ * these arguments (which may be 0). */
+int dgs_checkpoint_weight_grad_bytes(const dgs_checkpoint* ckpt, const dgs_matrix* dy, const dgs_row_lists* lists, uint32_t flags,
+                                     uint64_t* out_bytes);
+int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_matrix* dy, const dgs_row_lists* lists, float* dw, float* db,
+                               uint32_t flags, void* workspace, uint64_t workspace_bytes, void* stream);
+
+enum { DGS_SCORE_SOFTMAX = 0, DGS_SCORE_SIGMOID = 1 };
+#define DGS_ROUTE_MAX_EXPERTS 1024u
+#define DGS_ROUTE_MAX_K 32u
+#define DGS_NO_EXPERT 0xffffffffu /* an empty slot */
+
+/* How a router chooses.  Scores s are the softmax of a token's logits or their sigmoid; keys are s + bias.  Experts
+ * lie in `groups` equal groups; a group's key is the sum of its group_best (1 or 2) largest keys, and the
+ * groups_kept groups of largest key stay.  Of their experts the k of largest key are chosen; ties go to the lowest
+ * index, for groups and experts.  Without bias and with group_best = 1 the logits themselves are the keys; otherwise keys
+ * are compared as 64-bit arithmetic gives them.  A token's slots list its experts in ascending order, as
+ * packets list indices.  Weights are scale * s, or scale * s / (sum of the chosen s) with renormalise.
+ * A logit of -inf takes the expert away from the token (score 0): never chosen, and a token with fewer than k experts left
+ * has DGS_NO_EXPERT and weight 0 in its last slots.  A token with a NaN or +inf among its logits has no experts and NaN weights. */
+typedef struct {
+  uint32_t k;            /* 1 .. min(DGS_ROUTE_MAX_K, experts in the kept groups) */
+  uint32_t score;        /* DGS_SCORE_* */
+  uint32_t groups;       /* divides the number of experts; 1: no groups */
+  uint32_t groups_kept;  /* 1 .. groups */
+  uint32_t group_best;   /* 1 or 2 */
+  uint32_t renormalise;  /* 0 or 1 */
+  float scale;           /* finite */
+} dgs_router;
+
+/* logits: tokens x experts, 1 .. DGS_ROUTE_MAX_EXPERTS experts, tokens * k < 2^31.  bias: DEVICE f32[experts], finite, or NULL.  Outputs:
+ *   expert   DEVICE u32[tokens][k], weight DEVICE f32[tokens][k]
+ *   offsets  DEVICE u32[experts + 1]: the list of expert e is order[offsets[e] .. offsets[e + 1])
+ *   order    DEVICE u32[tokens * k]: slots t * k + j, ascending in each list; DGS_NO_EXPERT behind the last list
+ *   place    DEVICE u32[tokens][k]: where in order a slot stands; DGS_NO_EXPERT for an empty one
+ * offsets, order and place may be NULL, all three.  workspace: DEVICE, 16-byte aligned, dgs_route_experts_bytes long. */
+int dgs_route_experts_bytes(const dgs_router* router, uint64_t tokens, uint32_t experts, uint64_t* out_bytes);
+int dgs_route_experts(const dgs_router* router, const dgs_matrix* logits, const float* bias, uint32_t* expert, float* weight,
+                      uint32_t* offsets, uint32_t* order, uint32_t* place, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* The gradient of the weights taken back to the logits: dlogits (tokens x experts, of the logits' type) from the logits,
+ * the experts chosen (DEVICE u32[tokens][k], as dgs_route_experts writes them; an index past the last expert is treated as an empty slot
+ * and reported) and dweight (DEVICE f32[tokens][k]).  The choice itself has no gradient.  dlogits may be logits (in place). */
+int dgs_route_experts_grad(const dgs_router* router, const dgs_matrix* logits, const uint32_t* expert, const float* dweight,
+                           const dgs_matrix* dlogits, void* stream);
+
+/* Waits for `stream` and stores in *device_status the lowest status that kernels of the calls above have left on the current device
+ * since the last time it was read: 0, DGS_EINVAL (an index or list pointed outside its matrix) or DGS_ETIMEOUT (a bounded wait gave up). */
+int dgs_operator_status(void* stream, int* device_status);
+
 /* Static text for a dgs_error value. */
 const char* dgs_error_string(int err);
 

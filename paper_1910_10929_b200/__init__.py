@@ -33,7 +33,17 @@ EXPORTS = (
     "dgs_prev", "dgs_launch_count", "dgs_last_cuda_error", "dgs_free", "dgs_error_string",
     "dgs_timing_enable", "dgs_timing_read", "dgs_timing_trace", "dgs_topk_encode_static",
     "dgs_topk_encode_static_status", "dgs_hardware_queues",
+    "dgs_checkpoint_bytes", "dgs_checkpoint_save", "dgs_checkpoint_load", "dgs_checkpoint_activation_grad",
+    "dgs_checkpoint_weight_grad_bytes", "dgs_checkpoint_weight_grad", "dgs_route_experts_bytes", "dgs_route_experts",
+    "dgs_route_experts_grad", "dgs_operator_status",
 )
+DGS_TYPE_F32, DGS_TYPE_BF16, DGS_TYPE_FP16 = 0, 1, 2
+DGS_FORMAT_INT8, DGS_FORMAT_E4M3 = 0, 1
+DGS_ACT_NONE, DGS_ACT_RELU, DGS_ACT_GELU, DGS_ACT_GELU_TANH, DGS_ACT_SILU = 0, 1, 2, 3, 4
+DGS_WEIGHT_IN_OUT, DGS_WEIGHT_ADD = 1, 2
+DGS_SCORE_SOFTMAX, DGS_SCORE_SIGMOID = 0, 1
+DGS_ROUTE_MAX_EXPERTS, DGS_ROUTE_MAX_K = 1024, 32
+DGS_NO_EXPERT = 0xFFFFFFFF
 DGS_ELIMIT = -6
 DGS_STATIC_MAX_N = 1 << 20
 DGS_NUM_KERNELS = 8
@@ -58,6 +68,23 @@ class dgs_config(C.Structure):
                 ("num_segments", C.c_uint32), ("segments", C.POINTER(dgs_segment)), ("theta0", C.c_void_p),
                 ("arena", C.c_void_p), ("arena_bytes", C.c_uint64), ("stream", C.c_void_p), ("flags", C.c_uint32),
                 ("pull_all_capacity", C.c_uint32)]
+
+
+class dgs_matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_uint64), ("stride", C.c_uint64), ("cols", C.c_uint32), ("type", C.c_uint32)]
+
+
+class dgs_checkpoint(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint32), ("format", C.c_uint32)]
+
+
+class dgs_row_lists(C.Structure):
+    _fields_ = [("offsets", C.c_void_p), ("rows", C.c_void_p), ("experts", C.c_uint32), ("rows_per", C.c_uint32)]
+
+
+class dgs_router(C.Structure):
+    _fields_ = [("k", C.c_uint32), ("score", C.c_uint32), ("groups", C.c_uint32), ("groups_kept", C.c_uint32),
+                ("group_best", C.c_uint32), ("renormalise", C.c_uint32), ("scale", C.c_float)]
 
 
 class DgsError(RuntimeError):
@@ -103,6 +130,18 @@ def lib() -> C.CDLL:
         L.dgs_timing_trace.argtypes = [vp, u32, C.POINTER(C.c_float), C.POINTER(C.c_float), C.POINTER(C.c_int32),
                                        C.POINTER(C.c_int32), C.POINTER(u32)]
         L.dgs_free.argtypes = [vp]
+        mat, ckpt, lists, router = (C.POINTER(t) for t in (dgs_matrix, dgs_checkpoint, dgs_row_lists, dgs_router))
+        u64 = C.c_uint64
+        L.dgs_checkpoint_bytes.argtypes = [u64, u32, C.POINTER(u64)]
+        L.dgs_checkpoint_save.argtypes = [ckpt, mat, i32, mat, vp]
+        L.dgs_checkpoint_load.argtypes = [ckpt, mat, vp]
+        L.dgs_checkpoint_activation_grad.argtypes = [ckpt, i32, mat, mat, vp]
+        L.dgs_checkpoint_weight_grad_bytes.argtypes = [ckpt, mat, lists, u32, C.POINTER(u64)]
+        L.dgs_checkpoint_weight_grad.argtypes = [ckpt, mat, lists, vp, vp, u32, vp, u64, vp]
+        L.dgs_route_experts_bytes.argtypes = [router, u64, u32, C.POINTER(u64)]
+        L.dgs_route_experts.argtypes = [router, mat, vp, vp, vp, vp, vp, vp, vp, u64, vp]
+        L.dgs_route_experts_grad.argtypes = [router, mat, vp, vp, mat, vp]
+        L.dgs_operator_status.argtypes = [vp, C.POINTER(i32)]
         L.dgs_error_string.argtypes = [i32]
         L.dgs_error_string.restype = C.c_char_p
         for name in EXPORTS:
@@ -257,6 +296,63 @@ def dgs_topk_encode_static_status(stream: int = 0) -> int:
     return int(out.value)
 
 
+def dgs_checkpoint_bytes(rows: int, cols: int) -> int:
+    out = C.c_uint64(0)
+    _check(lib().dgs_checkpoint_bytes(rows, cols, C.byref(out)), "dgs_checkpoint_bytes")
+    return int(out.value)
+
+
+def dgs_checkpoint_save(ckpt: dgs_checkpoint, x: dgs_matrix, act: int = DGS_ACT_NONE, y: Optional[dgs_matrix] = None,
+                        stream: int = 0) -> None:
+    _check(lib().dgs_checkpoint_save(ckpt, x, act, y, stream or None), "dgs_checkpoint_save")
+
+
+def dgs_checkpoint_load(ckpt: dgs_checkpoint, x: dgs_matrix, stream: int = 0) -> None:
+    _check(lib().dgs_checkpoint_load(ckpt, x, stream or None), "dgs_checkpoint_load")
+
+
+def dgs_checkpoint_activation_grad(ckpt: dgs_checkpoint, act: int, dy: dgs_matrix, dx: dgs_matrix, stream: int = 0) -> None:
+    _check(lib().dgs_checkpoint_activation_grad(ckpt, act, dy, dx, stream or None), "dgs_checkpoint_activation_grad")
+
+
+def dgs_checkpoint_weight_grad_bytes(ckpt: dgs_checkpoint, dy: dgs_matrix, lists: Optional[dgs_row_lists] = None, flags: int = 0) -> int:
+    out = C.c_uint64(0)
+    _check(lib().dgs_checkpoint_weight_grad_bytes(ckpt, dy, lists, flags, C.byref(out)), "dgs_checkpoint_weight_grad_bytes")
+    return int(out.value)
+
+
+def dgs_checkpoint_weight_grad(ckpt: dgs_checkpoint, dy: dgs_matrix, lists: Optional[dgs_row_lists], dw_ptr: int, db_ptr: int = 0,
+                               flags: int = 0, workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().dgs_checkpoint_weight_grad(ckpt, dy, lists, dw_ptr or None, db_ptr or None, flags, workspace_ptr or None, workspace_bytes,
+                                            stream or None), "dgs_checkpoint_weight_grad")
+
+
+def dgs_route_experts_bytes(router: dgs_router, tokens: int, experts: int) -> int:
+    out = C.c_uint64(0)
+    _check(lib().dgs_route_experts_bytes(router, tokens, experts, C.byref(out)), "dgs_route_experts_bytes")
+    return int(out.value)
+
+
+def dgs_route_experts(router: dgs_router, logits: dgs_matrix, bias_ptr: int, expert_ptr: int, weight_ptr: int, offsets_ptr: int = 0,
+                      order_ptr: int = 0, place_ptr: int = 0, workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().dgs_route_experts(router, logits, bias_ptr or None, expert_ptr or None, weight_ptr or None, offsets_ptr or None,
+                                   order_ptr or None, place_ptr or None, workspace_ptr or None, workspace_bytes, stream or None),
+           "dgs_route_experts")
+
+
+def dgs_route_experts_grad(router: dgs_router, logits: dgs_matrix, expert_ptr: int, dweight_ptr: int, dlogits: dgs_matrix,
+                           stream: int = 0) -> None:
+    _check(lib().dgs_route_experts_grad(router, logits, expert_ptr or None, dweight_ptr or None, dlogits, stream or None),
+           "dgs_route_experts_grad")
+
+
+def dgs_operator_status(stream: int = 0) -> int:
+    """Waits for `stream`; the lowest status that the operators' kernels have left on the current device since the last call."""
+    out = C.c_int(0)
+    _check(lib().dgs_operator_status(stream or None, C.byref(out)), "dgs_operator_status")
+    return int(out.value)
+
+
 def dgs_hardware_queues() -> Tuple[int, int]:
     """(hardware queues the library's streams want, queues the process asked the driver for)."""
     a, b = C.c_int(0), C.c_int(0)
@@ -269,5 +365,7 @@ def dgs_free(ctx: int) -> None:
 
 
 from .context import Context  # noqa: E402  (torch-backed convenience holder of arena + handle)
+from .operators import Checkpoint, Route, operator_status, route_experts, route_experts_grad  # noqa: E402  (likewise, for a worker's own operators)
 
-__all__ = [n for n in dir() if n.startswith(("dgs_", "DGS_"))] + ["Context", "DgsError", "lib", "make_config"]
+__all__ = [n for n in dir() if n.startswith(("dgs_", "DGS_"))] + ["Checkpoint", "Context", "DgsError", "Route", "lib", "make_config",
+                                                                   "operator_status", "route_experts", "route_experts_grad"]

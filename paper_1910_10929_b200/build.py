@@ -9,8 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdgs.so")
-SOURCES = [os.path.join(CSRC, "dgs.cu"), os.path.join(CSRC, "dgs_one.cu")]
-DEPENDS = SOURCES + [os.path.join(CSRC, f) for f in ("dgs_apply.cuh", "dgs_arrivals.h", "dgs_kernels.cuh", "dgs_one.cuh", "dgs_topk.cuh")] + [os.path.join(ROOT, "include", "dgs.h")]
+SOURCES = [os.path.join(CSRC, f) for f in ("dgs.cu", "dgs_one.cu", "dgs_checkpoint.cu", "dgs_route.cu", "dgs_weight.cu")]
+DEPENDS = SOURCES + [os.path.join(CSRC, f) for f in ("dgs_apply.cuh", "dgs_arrivals.h", "dgs_kernels.cuh", "dgs_one.cuh", "dgs_operators.cuh", "dgs_topk.cuh")] + [os.path.join(ROOT, "include", "dgs.h")]
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -49,7 +49,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     nvcc = os.environ.get("NVCC", "nvcc")
     tmp = LIB + f".{os.getpid()}.tmp"
     cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + [
-        "-I", os.path.join(ROOT, "include"), "-o", tmp] + SOURCES
+        "--threads", "0", "-I", os.path.join(ROOT, "include"), "-o", tmp] + SOURCES
     digest = source_hash()
     subprocess.check_call(cmd)
     os.replace(tmp, LIB)
