@@ -80,7 +80,7 @@ def test_checkpoint_refusals():
 
 def test_weight_grad_refusals():
     L, c, dy = dgs.lib(), held(), matrix()
-    call = lambda c=c, dy=dy, lists=None, dw=P * 5, db=None, flags=0, work=P * 7, size=NEED: L.dgs_checkpoint_weight_grad(   # noqa: E731
+    call = lambda c=c, dy=dy, lists=None, dw=P * 5, db=None, flags=0, work=P << 12, size=NEED: L.dgs_checkpoint_weight_grad(   # noqa: E731
         c, dy, lists, dw, db, flags, work, size, None)
     assert call(dw=None) == dgs.DGS_EINVAL and call(dw=P * 5 + 2) == dgs.DGS_EINVAL and call(db=P * 6 + 1) == dgs.DGS_EINVAL
     assert call(flags=4) == dgs.DGS_EINVAL
@@ -89,14 +89,14 @@ def test_weight_grad_refusals():
     assert call(dw=P << 4) == dgs.DGS_EINVAL                   # over the checkpoint
     assert call(db=P * 5 + 64) == dgs.DGS_EINVAL               # over dw
     for lists in (dgs.dgs_row_lists(None, None, 2, 1), dgs.dgs_row_lists(P * 9, None, 0, 1), dgs.dgs_row_lists(P * 9, None, 2, 0),
-                  dgs.dgs_row_lists(P * 9, P * 9 + 2, 2, 1), dgs.dgs_row_lists(P * 9, None, 65536, 1)):
+                  dgs.dgs_row_lists(P * 9, P * 9 + 2, 2, 1), dgs.dgs_row_lists(P * 9, None, 1025, 1)):
         assert call(lists=lists) == dgs.DGS_EINVAL
     big, long = held(rows=100_000), matrix(rows=100_000)       # split: needs a workspace
     need = dgs.dgs_checkpoint_weight_grad_bytes(big, long)
     assert need > 0
-    assert call(big, long, dw=P << 8, work=P << 9, size=need - 1) == dgs.DGS_ENOMEM
+    assert call(big, long, dw=P << 8, work=P << 12, size=need - 1) == dgs.DGS_ENOMEM
     assert call(big, long, dw=P << 8, work=None, size=need) == dgs.DGS_EINVAL
-    assert call(big, long, dw=P << 8, work=(P << 9) + 4, size=need) == dgs.DGS_EINVAL
+    assert call(big, long, dw=P << 8, work=(P << 12) + 4, size=need) == dgs.DGS_EINVAL
     assert call(big, long, dw=P << 8, work=P << 8, size=need) == dgs.DGS_EINVAL
     out = C.c_uint64(0)
     huge = dgs.dgs_matrix(P, 10, 1 << 29, 1 << 29, 0)
