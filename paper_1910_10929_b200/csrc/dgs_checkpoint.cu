@@ -9,37 +9,41 @@ namespace {
 __device__ int g_operator_status;
 
 // ---- activations and their slopes -------------------------------------------------------------
+// FAST is for results of 16 bits: the exponential and division of the hardware are off by 2^-20 at most where it counts, a rounding of the
+// result by 2^-9 or 2^-12.  (32768 x 2048 in bfloat16, gelu_tanh: 125 us exact, see the kernels for what it takes now.)
+template <bool FAST> __device__ __forceinline__ float exponential(float x) { return FAST ? __expf(x) : expf(x); }
+template <bool FAST> __device__ __forceinline__ float quotient(float a, float b) { return FAST ? __fdividef(a, b) : a / b; }
 // s = 1 / (1 + e^-u) and t = 1 - s, both from e^-|u|, which does not overflow: neither loses digits to the other.
-struct Sigmoid {
+template <bool FAST> struct Sigmoid {
   float s, t;
   __device__ __forceinline__ explicit Sigmoid(float u) {
-    const float q = expf(-fabsf(u)), r = 1.0f / (1.0f + q);
-    s = u > 0.0f ? r : q * r;
-    t = u > 0.0f ? q * r : r;
+    const float q = exponential<FAST>(-fabsf(u)), r = quotient<FAST>(1.0f, 1.0f + q), p = q * r;
+    s = u > 0.0f ? r : p;
+    t = u > 0.0f ? p : r;
   }
 };
-template <int ACT>
+template <int ACT, bool FAST>
 __device__ __forceinline__ float act_value(float x) {
   if constexpr (ACT == DGS_ACT_RELU) return x > 0.0f ? x : (x != x ? x : 0.0f);
-  if constexpr (ACT == DGS_ACT_SILU) return x * Sigmoid(x).s;
+  if constexpr (ACT == DGS_ACT_SILU) return x * Sigmoid<FAST>(x).s;
   if constexpr (ACT == DGS_ACT_GELU) return 0.5f * x * erfcf(-x * 0.70710678f);
-  if constexpr (ACT == DGS_ACT_GELU_TANH) return x * Sigmoid(1.5957691f * x * fmaf(0.044715f * x, x, 1.0f)).s;
+  if constexpr (ACT == DGS_ACT_GELU_TANH) return x * Sigmoid<FAST>(1.5957691f * x * fmaf(0.044715f * x, x, 1.0f)).s;
   return x;
 }
 // d act / d x.  With s = 1 / (1 + e^-u): silu u = x, slope s (1 + x (1 - s)); gelu_tanh is x s(u), u = 2 sqrt(2/pi) (x + 0.044715 x^3),
 // slope s + x u' s (1 - s).
-template <int ACT>
+template <int ACT, bool FAST>
 __device__ __forceinline__ float act_slope(float x) {
   if constexpr (ACT == DGS_ACT_RELU) return x > 0.0f ? 1.0f : (x != x ? x : 0.0f);
-  if constexpr (ACT == DGS_ACT_GELU) return fmaf(0.3989422804f * x, expf(-0.5f * x * x), 0.5f * erfcf(-x * 0.70710678f));
+  if constexpr (ACT == DGS_ACT_GELU) return fmaf(0.3989422804f * x, exponential<FAST>(-0.5f * x * x), 0.5f * erfcf(-x * 0.70710678f));
   if constexpr (ACT == DGS_ACT_SILU) {
-    const Sigmoid g(x);
+    const Sigmoid<FAST> g(x);
     return g.s * fmaf(x, g.t, 1.0f);
   }
   if constexpr (ACT == DGS_ACT_GELU_TANH) {
     x = x > 30.0f ? 30.0f : x < -30.0f ? -30.0f : x;   // from there on 0 or 1; cubes beyond would overflow
     const float x2 = x * x, u = 1.5957691f * x * fmaf(0.044715f, x2, 1.0f), du = 1.5957691f * fmaf(0.134145f, x2, 1.0f);
-    const Sigmoid g(u);
+    const Sigmoid<FAST> g(u);
     return g.s * fmaf(x * du, g.t, 1.0f);
   }
   return 1.0f;
@@ -47,54 +51,38 @@ __device__ __forceinline__ float act_slope(float x) {
 
 // ---- eight columns at a time ------------------------------------------------------------------
 // A unit is eight columns of a row; four lanes next to one another hold a block.  VEC: rows begin on 16 bytes, so that a unit is one
-// or two wide accesses; otherwise it is read and written element by element (odd lengths and strides).
+// or two wide accesses; otherwise it is read and written element by element (odd lengths and strides).  Units are read some at a time, so that
+// a thread has several reads under way, and stay in their type until they are used.
+template <class T> struct Eight {
+  T v[8];
+};
 template <bool VEC, class T>
-__device__ __forceinline__ void read8(const T* p, uint32_t left, float* v) {
-  if constexpr (VEC && sizeof(T) == 2) {
-    if (left >= 8) {
-      const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p));
-      const uint32_t a[4] = {w.x, w.y, w.z, w.w};
+__device__ __forceinline__ void read8(const T* p, uint32_t left, Eight<T>& e) {
+  if (VEC && left >= 8) {
+    uint4 w[sizeof(T) / 2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        T t[2];
-        memcpy(t, &a[i], 4);
-        v[2 * i] = Elem<T>::get(t[0]), v[2 * i + 1] = Elem<T>::get(t[1]);
-      }
-      return;
-    }
-  } else if constexpr (VEC) {
-    if (left >= 8) {
-      const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-      return;
-    }
+    for (uint32_t i = 0; i < sizeof(T) / 2; ++i) w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+    memcpy(e.v, w, sizeof(w));
+    return;
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = uint32_t(i) < left ? Elem<T>::get(p[i]) : 0.0f;
+  for (int i = 0; i < 8; ++i) e.v[i] = uint32_t(i) < left ? p[i] : Elem<T>::put(0.0f);
 }
 template <bool VEC, class T>
 __device__ __forceinline__ void write8(T* p, uint32_t left, const float* v) {
-  if constexpr (VEC && sizeof(T) == 2) {
-    if (left >= 8) {
-      uint32_t a[4];
+  Eight<T> e;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const T t[2] = {Elem<T>::put(v[2 * i]), Elem<T>::put(v[2 * i + 1])};
-        memcpy(&a[i], t, 4);
-      }
-      __stcs(reinterpret_cast<uint4*>(p), make_uint4(a[0], a[1], a[2], a[3]));
-      return;
-    }
-  } else if constexpr (VEC) {
-    if (left >= 8) {
-      __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
-      __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
-      return;
-    }
+  for (int i = 0; i < 8; ++i) e.v[i] = Elem<T>::put(v[i]);
+  if (VEC && left >= 8) {
+    uint4 w[sizeof(T) / 2];
+    memcpy(w, e.v, sizeof(w));
+#pragma unroll
+    for (uint32_t i = 0; i < sizeof(T) / 2; ++i) __stcs(reinterpret_cast<uint4*>(p) + i, w[i]);
+    return;
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (uint32_t(i) < left) p[i] = Elem<T>::put(v[i]);
+    if (uint32_t(i) < left) p[i] = e.v[i];
 }
 
 struct Units {
@@ -104,82 +92,121 @@ struct Units {
   uint32_t step_units;
 };
 
-// Walks the units of all rows, a stride of the grid apart: f(row, unit).
-template <class F>
-__device__ __forceinline__ void each_unit(const Units& g, F&& f) {
+// Walks the units of all rows, a stride of the grid apart, N at a time: load(i, row, unit) for each, then done(i, row, unit).
+template <int N, class L, class D>
+__device__ __forceinline__ void each_unit(const Units& g, L&& load, D&& done) {
   const uint64_t first = uint64_t(blockIdx.x) * blockDim.x + threadIdx.x;
   uint64_t row = first / g.per_row;
   uint32_t unit = uint32_t(first - row * g.per_row);
   while (row < g.rows) {
-    f(row, unit);
-    row += g.step_rows;
-    unit += g.step_units;
-    if (unit >= g.per_row) unit -= g.per_row, ++row;
+    uint64_t r[N];
+    uint32_t u[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      r[i] = row;
+      u[i] = unit;
+      if (row < g.rows) load(i, row, unit);
+      row += g.step_rows;
+      unit += g.step_units;
+      if (unit >= g.per_row) unit -= g.per_row, ++row;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (r[i] < g.rows) done(i, r[i], u[i]);
   }
 }
+template <class T> constexpr int kAtOnce = sizeof(T) == 2 ? 4 : 2;
 
 template <class T, bool FLOAT8, bool VEC, int ACT>
 __global__ void __launch_bounds__(256) k_checkpoint_save(Held h, uint8_t* codes, uint8_t* scales, const T* x, uint64_t xs, T* y, uint64_t ys, Units g) {
-  each_unit(g, [&](uint64_t row, uint32_t unit) {
-    const uint32_t col = unit * 8, left = col < h.cols ? h.cols - col : 0;
-    float v[8];
-    read8<VEC>(x + row * xs + col, left, v);
-    uint32_t m = 0;
+  constexpr int N = kAtOnce<T>;
+  Eight<T> in[N];
+  each_unit<N>(
+      g,
+      [&](int i, uint64_t row, uint32_t unit) {
+        const uint32_t col = unit * 8;
+        read8<VEC>(x + row * xs + col, col < h.cols ? h.cols - col : 0, in[i]);
+      },
+      [&](int i, uint64_t row, uint32_t unit) {
+        const uint32_t col = unit * 8, left = col < h.cols ? h.cols - col : 0;
+        float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-    const uint32_t lanes = 0xfu << (threadIdx.x & 28u);   // the four lanes of the block: rows are a multiple of four units
-    m = max(m, __shfl_xor_sync(lanes, m, 1));
-    m = max(m, __shfl_xor_sync(lanes, m, 2));
-    const uint32_t byte = scale_byte<FLOAT8>(m);
-    const float up = byte == kNanScale ? 0.0f : scale_up(byte);
-    uint2 w = make_uint2(encode4<FLOAT8>(v, up), encode4<FLOAT8>(v + 4, up));
-    if (byte == kNanScale) w = make_uint2(0, 0);
-    *reinterpret_cast<uint2*>(codes + row * h.width + col) = w;
-    if (unit % 4 == 0) {
-      uint8_t* s = scales + row * h.spitch + unit / 4;
-      *s = uint8_t(byte);
-      if (unit + 4 == g.per_row)
-        for (uint32_t b = g.per_row / 4; b < h.spitch; ++b) *++s = 0;
-    }
-    if (y) {
+        for (int k = 0; k < 8; ++k) v[k] = Elem<T>::get(in[i].v[k]);
+        uint32_t m = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = act_value<ACT>(v[i]);
-      write8<VEC>(y + row * ys + col, left, v);
-    }
-  });
+        for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(v[k]) & 0x7fffffffu);
+        const uint32_t lanes = 0xfu << (threadIdx.x & 28u);   // the four lanes of the block: rows are a multiple of four units
+        m = max(m, __shfl_xor_sync(lanes, m, 1));
+        m = max(m, __shfl_xor_sync(lanes, m, 2));
+        const uint32_t byte = scale_byte<FLOAT8>(m);
+        const float up = byte == kNanScale ? 0.0f : scale_up(byte);
+        uint2 w = make_uint2(encode4<FLOAT8>(v, up), encode4<FLOAT8>(v + 4, up));
+        if (byte == kNanScale) w = make_uint2(0, 0);
+        *reinterpret_cast<uint2*>(codes + row * h.width + col) = w;
+        if (unit % 4 == 0) {
+          uint8_t* s = scales + row * h.spitch + unit / 4;
+          *s = uint8_t(byte);
+          if (unit + 4 == g.per_row)
+            for (uint32_t b = g.per_row / 4; b < h.spitch; ++b) *++s = 0;
+        }
+        if (y) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = act_value<ACT, sizeof(T) == 2>(v[k]);
+          write8<VEC>(y + row * ys + col, left, v);
+        }
+      });
 }
 
+struct HeldUnit {
+  uint2 w;
+  uint32_t scale;
+};
+__device__ __forceinline__ void read_held(const Held& h, uint64_t row, uint32_t unit, HeldUnit& u) {
+  u.w = __ldg(reinterpret_cast<const uint2*>(h.codes + row * h.width + unit * 8));
+  u.scale = __ldg(h.scales + row * h.spitch + unit / 4);
+}
 template <bool FLOAT8>
-__device__ __forceinline__ void held8(const Held& h, uint64_t row, uint32_t unit, float* v) {
-  const uint2 w = *reinterpret_cast<const uint2*>(h.codes + row * h.width + unit * 8);
-  const float down = scale_down(h.scales[row * h.spitch + unit / 4]);
-  decode4<FLOAT8>(w.x, down, v);
-  decode4<FLOAT8>(w.y, down, v + 4);
+__device__ __forceinline__ void decode8(const HeldUnit& u, float* v) {
+  const float down = scale_down(u.scale);
+  decode4<FLOAT8>(u.w.x, down, v);
+  decode4<FLOAT8>(u.w.y, down, v + 4);
 }
 
 template <class T, bool FLOAT8, bool VEC>
 __global__ void __launch_bounds__(256) k_checkpoint_load(Held h, T* x, uint64_t xs, Units g) {
-  each_unit(g, [&](uint64_t row, uint32_t unit) {
-    const uint32_t col = unit * 8;
-    if (col >= h.cols) return;
-    float v[8];
-    held8<FLOAT8>(h, row, unit, v);
-    write8<VEC>(x + row * xs + col, h.cols - col, v);
-  });
+  HeldUnit in[4];
+  each_unit<4>(
+      g, [&](int i, uint64_t row, uint32_t unit) { read_held(h, row, unit, in[i]); },
+      [&](int i, uint64_t row, uint32_t unit) {
+        const uint32_t col = unit * 8;
+        if (col >= h.cols) return;
+        float v[8];
+        decode8<FLOAT8>(in[i], v);
+        write8<VEC>(x + row * xs + col, h.cols - col, v);
+      });
 }
 
 template <class T, bool FLOAT8, bool VEC, int ACT>
 __global__ void __launch_bounds__(256) k_activation_grad(Held h, const T* dy, uint64_t dys, T* dx, uint64_t dxs, Units g) {
-  each_unit(g, [&](uint64_t row, uint32_t unit) {
-    const uint32_t col = unit * 8;
-    if (col >= h.cols) return;
-    float v[8], d[8];
-    held8<FLOAT8>(h, row, unit, v);
-    read8<VEC>(dy + row * dys + col, h.cols - col, d);
+  constexpr int N = kAtOnce<T>;
+  HeldUnit in[N];
+  Eight<T> d[N];
+  each_unit<N>(
+      g,
+      [&](int i, uint64_t row, uint32_t unit) {
+        const uint32_t col = unit * 8;
+        read_held(h, row, unit, in[i]);
+        read8<VEC>(dy + row * dys + col, col < h.cols ? h.cols - col : 0, d[i]);
+      },
+      [&](int i, uint64_t row, uint32_t unit) {
+        const uint32_t col = unit * 8;
+        if (col >= h.cols) return;
+        float v[8];
+        decode8<FLOAT8>(in[i], v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) d[i] *= act_slope<ACT>(v[i]);
-    write8<VEC>(dx + row * dxs + col, h.cols - col, d);
-  });
+        for (int k = 0; k < 8; ++k) v[k] = Elem<T>::get(d[i].v[k]) * act_slope<ACT, sizeof(T) == 2>(v[k]);
+        write8<VEC>(dx + row * dxs + col, h.cols - col, v);
+      });
 }
 
 // ---- host side --------------------------------------------------------------------------------

@@ -14,7 +14,7 @@ constexpr uint32_t kAll = 0xffffffffu;
 struct RouteArgs {
   uint64_t stride;
   uint32_t tokens, experts, k, groups, group_size, kept, best, tiles;
-  bool sigmoid, renorm;
+  bool sigmoid, renorm, wide;
   float scale;
   const float* bias;
   uint32_t* expert;
@@ -22,17 +22,19 @@ struct RouteArgs {
   uint32_t* offsets;
   uint32_t* order;
   uint32_t* place;
-  uint32_t* counts;    // [experts + 1][tiles]: slots of a tile that belong to an expert; behind the last expert: empty slots
+  uint32_t* counts;    // [experts + 1][tiles]: slots of a tile that belong to an expert, then those of the tiles before; behind the last
+                       // expert: empty slots.  NULL: no lists, or a single tile
+  uint32_t* totals;    // [experts + 1]
 };
 
 // Numbers whose unsigned order is the order of the floats; 0 stands for "not there" (below -inf).
 __device__ __forceinline__ uint32_t sortable(float v) {
-  const uint32_t b = __float_as_uint(v + 0.0f);   // -0 and +0 are equal keys
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  const int b = __float_as_int(v + 0.0f);   // -0 and +0 are equal keys
+  return uint32_t(b ^ (b >> 31 | int(0x80000000)));
 }
 __device__ __forceinline__ unsigned long long sortable(double v) {
-  const unsigned long long b = (unsigned long long)__double_as_longlong(v + 0.0);
-  return b >> 63 ? ~b : b | 0x8000000000000000ull;
+  const long long b = __double_as_longlong(v + 0.0);
+  return (unsigned long long)(b ^ (b >> 63 | (long long)0x8000000000000000ull));
 }
 __device__ __forceinline__ float unsorted(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 __device__ __forceinline__ double unsorted(unsigned long long k) {
@@ -53,407 +55,555 @@ __device__ __forceinline__ R warp_sum(R v) {
   for (int d = 16; d; d /= 2) v += __shfl_xor_sync(kAll, v, d);
   return v;
 }
-
-// Expert 32 i + lane is element i of a lane: loads are coalesced, and ballots over the lanes give the experts' order.
-// Chooses the `count` largest of the keys that are not 0, ties to the lowest index: bit i of the result is element i.
-// low / next: the smallest key chosen and the largest one left.
-template <int PER, class K>
-__device__ __forceinline__ uint32_t choose(const K (&key)[PER], uint32_t count, K* low, K* next) {
-  K border = ~K(0);
-  uint32_t above = 0, level = 0;
-  for (;;) {   // the distinct keys in descending order until `count` are reached: at most `count` rounds
-    K m = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) m = key[i] < border && key[i] > m ? key[i] : m;
-    m = warp_max(m);
-    if (m == 0) break;   // fewer than `count` are there
-    border = m;
-    above += level;
-    level = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) level += __popc(__ballot_sync(kAll, key[i] == m));
-    if (above + level >= count) break;
-  }
-  uint32_t bits = 0, seen = 0;
-  K left = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const uint32_t at = __ballot_sync(kAll, key[i] == border);
-    const bool mine = key[i] != 0 && (key[i] > border ||
-                      (key[i] == border && above + seen + __popc(at & ((1u << (threadIdx.x & 31)) - 1)) < count));
-    bits |= uint32_t(mine) << i;
-    if (!mine && key[i] > left) left = key[i];
-    seen += __popc(at);
-  }
-  *low = border;
-  *next = warp_max(left);
-  return bits;
-}
-
-// The keys of the groups of one token, each lane keeping group `lane` (and lane + 32 and so on: GP of them); 0: no expert left in it.
-template <int PER, class R, class K>
-__device__ __forceinline__ K group_key(const K (&key)[PER], const RouteArgs& a, uint32_t g) {
-  const uint32_t lane = threadIdx.x & 31, lo = g * a.group_size, hi = lo + a.group_size;
-  K m = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const uint32_t e = 32 * i + lane;
-    if (32u * i < hi && 32u * i + 32 > lo && e >= lo && e < hi && key[i] > m) m = key[i];
-  }
-  const K first = warp_max(m);
-  if (first == 0 || a.best == 1) return first;
-  uint32_t equal = 0;
-  m = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const uint32_t e = 32 * i + lane;
-    const bool in = 32u * i < hi && 32u * i + 32 > lo && e >= lo && e < hi;
-    equal += __popc(__ballot_sync(kAll, in && key[i] == first));
-    if (in && key[i] != first && key[i] > m) m = key[i];
-  }
-  const K second = equal > 1 ? first : warp_max(m);
-  return second == 0 ? first : sortable(unsorted(first) + unsorted(second));
-}
-
-// Leaves only the keys of the kept groups.  close: the border between kept and dropped groups is nearer than `slack`
-// (relative to the larger key's size).
-template <int PER, class R, class K>
-__device__ __forceinline__ bool keep_groups(K (&key)[PER], const RouteArgs& a, R slack) {
+// Sum over the lanes before.
+__device__ __forceinline__ uint32_t lanes_before(uint32_t v) {
   const uint32_t lane = threadIdx.x & 31;
-  K mine[PER];   // at most as many groups as experts
-#pragma unroll
-  for (int i = 0; i < PER; ++i) mine[i] = 0;
-  for (uint32_t g = 0; g < a.groups; ++g) {
-    const K v = group_key<PER, R, K>(key, a, g);
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (32u * i + lane == g) mine[i] = v;
-  }
-  K low, next;
-  const uint32_t bits = choose<PER, K>(mine, a.kept, &low, &next);
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const uint32_t e = 32 * i + lane, g = e < a.experts ? e / a.group_size : 0;
-    uint32_t keep = 0;
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      if (32u * j >= a.groups) break;
-      const uint32_t b = __ballot_sync(kAll, bits >> j & 1);
-      if (g / 32 == uint32_t(j)) keep = b >> (g % 32) & 1;
-    }
-    if (!keep) key[i] = 0;
-  }
-  return next != 0 && R(unsorted(low)) - R(unsorted(next)) <= slack;
-}
-
-__device__ __forceinline__ float score_exp(float v) { return expf(v); }
-__device__ __forceinline__ double score_exp(double v) { return exp(v); }
-
-// Keys of one token in R arithmetic from its logits; free: bit i, element i is an expert that the token may have.  Returns what
-// no score exceeds.
-template <int PER, class R, class K>
-__device__ __forceinline__ R make_keys(const float (&z)[PER], uint32_t free, float top, const RouteArgs& a, K (&key)[PER]) {
-  const uint32_t lane = threadIdx.x & 31;
-  R s[PER];
-  R sum = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    s[i] = 0;
-    if (free >> i & 1) s[i] = a.sigmoid ? R(1) / (R(1) + score_exp(-R(z[i]))) : score_exp(R(z[i]) - R(top));
-    sum += s[i];
-  }
-  if (!a.sigmoid) {
-    sum = warp_sum(sum);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) s[i] = s[i] / sum;
-  }
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const R b = a.bias && (free >> i & 1) ? R(a.bias[32 * i + lane]) : R(0);
-    key[i] = free >> i & 1 ? sortable(s[i] + b) : K(0);
-  }
-  return a.sigmoid ? R(1) : R(1) / sum;
-}
-
-// The same choice in 64 bits, for tokens whose border 32 bits cannot tell: rare, and kept out of line.
-template <int PER>
-__device__ __noinline__ uint32_t choose_exactly(const float (&z)[PER], uint32_t free, float top, const RouteArgs& a) {
-  unsigned long long key[PER], low, next;
-  make_keys<PER, double>(z, free, top, a, key);
-  if (a.groups > 1) keep_groups<PER, double>(key, a, 0.0);
-  return choose<PER>(key, a.k, &low, &next);
-}
-
-// One warp per token, a tile of 64 tokens per CTA.  The token's logits stay in registers; the experts chosen are marked in a bit
-// mask per expert (bit = token of the tile), whose counts are what a later kernel needs to place the tile's slots.
-template <int PER, class T>
-__global__ void __launch_bounds__(kRouteWarps * 32) k_route(const T* logits, const __grid_constant__ RouteArgs a) {
-  extern __shared__ uint32_t mask[];   // [experts][2]
-  __shared__ uint32_t s_empty;
-  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  if (a.counts) {
-    for (uint32_t i = threadIdx.x; i < a.experts * 2; i += blockDim.x) mask[i] = 0;
-    if (threadIdx.x == 0) s_empty = 0;
-    __syncthreads();
-  }
-  for (uint32_t n = warp; n < kTile; n += kRouteWarps) {
-    const uint64_t t = uint64_t(blockIdx.x) * kTile + n;
-    if (t >= a.tokens) break;
-    const T* row = logits + t * a.stride;
-    float z[PER], top = -INFINITY;
-    uint32_t free = 0;
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const uint32_t e = 32 * i + lane;
-      z[i] = e < a.experts ? Elem<T>::get(row[e]) : -INFINITY;
-      bad |= !(z[i] < INFINITY);
-      free |= uint32_t(z[i] > -INFINITY) << i;
-      top = fmaxf(top, z[i]);
-    }
-    bad = __any_sync(kAll, bad);
-    top = unsorted(warp_max(sortable(top)));
-    uint32_t bits = 0;
-    if (!bad) {
-      uint32_t key[PER], low, next;
-      if (!a.bias && a.best == 1) {   // scores ascend with the logits: these are exact keys
-#pragma unroll
-        for (int i = 0; i < PER; ++i) key[i] = free >> i & 1 ? sortable(z[i]) : 0;
-        if (a.groups > 1) keep_groups<PER, float>(key, a, 0.0f);
-        bits = choose<PER>(key, a.k, &low, &next);
-      } else {
-        // How far two keys, or two sums of two keys, may be off together.  A softmax score is off by at most 41 roundings of itself (37 of
-        // them in the sum of up to 1024 terms), a sigmoid by 4; scores of a softmax add up to 1 at most, and a rounding is 2^-24: below
-        // 2^-17 of the largest score.  The additions: 12 roundings of at most the largest key, below 2^-20 of it.
-        const float most = make_keys<PER, float>(z, free, top, a, key);
-        float big = 0.0f;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-          if (key[i]) big = fmaxf(big, fabsf(unsorted(key[i])));
-        big = unsorted(warp_max(sortable(big)));
-        const float slack = (a.sigmoid ? 0x1p-19f : 0x1p-17f) * most + 0x1p-20f * big;
-        bool close = false;
-        if (a.groups > 1) close = keep_groups<PER, float>(key, a, slack);
-        bits = choose<PER>(key, a.k, &low, &next);
-        close |= next != 0 && unsorted(low) - unsorted(next) <= slack;
-        if (close) bits = choose_exactly<PER>(z, free, top, a);
-      }
-    }
-    // weights: scores of the chosen, taken relative to the largest where they are divided by their sum
-    float ref = top;   // sigmoid, renormalised: the largest min(z, 0) of the chosen
-    if (a.renorm) {
-      ref = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (bits >> i & 1) ref = fmaxf(ref, a.sigmoid ? fminf(z[i], 0.0f) : z[i]);
-      ref = unsorted(warp_max(sortable(ref)));
-    }
-    float s[PER], sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const bool counts = a.renorm ? bits >> i & 1 : (a.sigmoid ? bits >> i & 1 : free >> i & 1);
-      s[i] = 0.0f;
-      if (counts) s[i] = a.sigmoid ? expf(fminf(z[i], 0.0f) - (a.renorm ? ref : 0.0f)) / (1.0f + expf(-fabsf(z[i]))) : expf(z[i] - ref);
-      sum += s[i];
-    }
-    const float by = a.sigmoid && !a.renorm ? 1.0f : warp_sum(sum);
-    uint32_t base = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const uint32_t b = __ballot_sync(kAll, bits >> i & 1);
-      if (bits >> i & 1) {
-        const uint32_t e = 32 * i + lane, j = base + __popc(b & ((1u << lane) - 1));
-        a.expert[t * a.k + j] = e;
-        a.weight[t * a.k + j] = s[i] / by * a.scale;
-        if (a.counts) atomicOr(&mask[2 * e + n / 32], 1u << (n % 32));
-      }
-      base += __popc(b);
-    }
-    for (uint32_t j = base + lane; j < a.k; j += 32) {
-      a.expert[t * a.k + j] = DGS_NO_EXPERT;
-      a.weight[t * a.k + j] = bad ? NAN : 0.0f;
-    }
-    if (a.counts && lane == 0 && base < a.k) atomicAdd(&s_empty, a.k - base);
-  }
-  if (!a.counts) return;
-  __syncthreads();
-  for (uint32_t e = threadIdx.x; e < a.experts; e += blockDim.x)
-    a.counts[uint64_t(e) * a.tiles + blockIdx.x] = __popc(mask[2 * e]) + __popc(mask[2 * e + 1]);
-  if (threadIdx.x == 0) a.counts[uint64_t(a.experts) * a.tiles + blockIdx.x] = s_empty;
-}
-
-// One CTA per expert (and one for the empty slots): the counts of its tiles become sums over the tiles before, the total goes to offsets[e].
-__global__ void __launch_bounds__(256) k_route_sums(const __grid_constant__ RouteArgs a) {
-  __shared__ uint32_t warp_total[8];
-  uint32_t* c = a.counts + uint64_t(blockIdx.x) * a.tiles;
-  uint32_t before = 0;
-  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  for (uint32_t first = 0; first < a.tiles; first += 256) {
-    const uint32_t i = first + threadIdx.x, v = i < a.tiles ? c[i] : 0;
-    uint32_t sum = v;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const uint32_t o = __shfl_up_sync(kAll, sum, d);
-      if (lane >= uint32_t(d)) sum += o;
-    }
-    if (lane == 31) warp_total[warp] = sum;
-    __syncthreads();
-    uint32_t base = before;
-    for (uint32_t w = 0; w < 8; ++w) {
-      if (w < warp) base += warp_total[w];
-      before += warp_total[w];
-    }
-    if (i < a.tiles) c[i] = base + sum - v;
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) a.offsets[blockIdx.x < a.experts ? blockIdx.x + 1 : 0] = before;
-}
-
-// Places a tile's slots.  A slot's place is what lies before its expert's list, before the tile in that list and before the token in
-// the tile: the first from the experts' totals, the second from k_route_sums, the third from the bit mask.
-__global__ void __launch_bounds__(256) k_route_place(const __grid_constant__ RouteArgs a) {
-  extern __shared__ uint32_t shared[];
-  uint32_t* mask = shared;                     // [experts][2]
-  uint32_t* begin = shared + 2 * a.experts;    // [experts + 1]
-  __shared__ uint32_t warp_total[8], s_before;
-  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  for (uint32_t i = threadIdx.x; i < 2 * a.experts; i += 256) mask[i] = 0;
-  const uint32_t first = blockIdx.x * kTile, tokens = min(kTile, a.tokens - first), slots = tokens * a.k;
-  const uint32_t* expert = a.expert + uint64_t(first) * a.k;
-  // totals to sums over the experts before: offsets[e + 1] still holds the total of e, the first CTA to finish must not disturb it,
-  // so the sums are written by k_route_offsets behind this kernel
-  uint32_t before = 0;
-  for (uint32_t e0 = 0; e0 <= a.experts; e0 += 256) {
-    const uint32_t e = e0 + threadIdx.x, v = e < a.experts ? a.offsets[e + 1] : 0;
-    uint32_t sum = v;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const uint32_t o = __shfl_up_sync(kAll, sum, d);
-      if (lane >= uint32_t(d)) sum += o;
-    }
-    if (lane == 31) warp_total[warp] = sum;
-    __syncthreads();
-    uint32_t base = before;
-    for (uint32_t w = 0; w < 8; ++w) {
-      if (w < warp) base += warp_total[w];
-      before += warp_total[w];
-    }
-    if (e <= a.experts) begin[e] = base + sum - v;
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) s_before = begin[a.experts] + a.counts[uint64_t(a.experts) * a.tiles + blockIdx.x];
-  for (uint32_t i = threadIdx.x; i < slots; i += 256) {
-    const uint32_t e = expert[i], n = i / a.k;
-    if (e < a.experts) atomicOr(&mask[2 * e + n / 32], 1u << (n % 32));
-  }
-  __syncthreads();
-  for (uint32_t i = threadIdx.x; i < slots; i += 256) {
-    const uint32_t e = expert[i], n = i / a.k;
-    const uint64_t slot = uint64_t(first) * a.k + i;
-    if (e < a.experts) {
-      const uint32_t m0 = mask[2 * e], m1 = mask[2 * e + 1];
-      const uint32_t rank = n < 32 ? __popc(m0 & ((1u << n) - 1)) : __popc(m0) + __popc(m1 & ((1u << (n - 32)) - 1));
-      const uint32_t at = begin[e] + a.counts[uint64_t(e) * a.tiles + blockIdx.x] + rank;
-      a.order[at] = uint32_t(slot);
-      a.place[slot] = at;
-    } else {
-      a.place[slot] = DGS_NO_EXPERT;
-    }
-  }
-  // order behind the last list: as many entries as the tile has empty slots
-  const uint32_t from = s_before;
-  const uint32_t to = begin[a.experts] + (blockIdx.x + 1 < a.tiles ? a.counts[uint64_t(a.experts) * a.tiles + blockIdx.x + 1] : a.offsets[0]);
-  for (uint32_t i = from + threadIdx.x; i < to; i += 256) a.order[i] = DGS_NO_EXPERT;
-}
-
-// Totals to offsets, in place, by one CTA.
-__global__ void __launch_bounds__(1024) k_route_offsets(uint32_t* offsets, uint32_t experts) {
-  __shared__ uint32_t warp_total[32];
-  const uint32_t e = threadIdx.x, lane = e % 32, warp = e / 32;
-  uint32_t sum = e < experts ? offsets[e + 1] : 0;
+  uint32_t sum = v;
 #pragma unroll
   for (int d = 1; d < 32; d *= 2) {
     const uint32_t o = __shfl_up_sync(kAll, sum, d);
     if (lane >= uint32_t(d)) sum += o;
   }
-  if (lane == 31) warp_total[warp] = sum;
+  return sum - v;
+}
+
+// Lane l has experts l * PER to l * PER + PER - 1, in its registers: experts ascend with the lanes and in each.
+// Which of its keys a lane holds among the `count` largest of the warp (bit i: key i), ties to the lowest index.  low / next: the
+// smallest key chosen and the largest left.
+template <int PER, class K>
+__device__ __forceinline__ uint32_t choose(const K (&key)[PER], uint32_t count, K* low, K* next) {
+  K border = ~K(0);
+  uint32_t above = 0, level = 0;   // keys larger than the border, and equal to it
+  K left;
+  if constexpr (PER <= 8 && sizeof(K) == 4) {
+    // the lane's keys in descending order; round by round the largest of the lanes' first ones is taken off
+    K s[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) s[i] = key[i];
+#pragma unroll
+    for (int size = 2; size <= PER; size *= 2)
+#pragma unroll
+      for (int d = size / 2; d; d /= 2)
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if ((i & d) == 0) {
+            const K x = s[i], y = s[i + d];
+            const bool down = (i & size) == 0;
+            s[i] = down ? max(x, y) : min(x, y);
+            s[i + d] = down ? min(x, y) : max(x, y);
+          }
+    K m;
+    for (;;) {
+      m = warp_max(s[0]);
+      if (m == 0) break;   // fewer than `count` are there
+      const bool mine = s[0] == m;
+      const uint32_t taken = __popc(__ballot_sync(kAll, mine));
+      if (m != border) above += level, level = 0, border = m;
+      level += taken;
+      if (mine) {
+#pragma unroll
+        for (int i = 0; i + 1 < PER; ++i) s[i] = s[i + 1];
+        s[PER - 1] = 0;
+      }
+      if (above + level >= count) break;
+    }
+    left = s[0];
+    if (m != 0)   // more keys of the border's size may follow
+      for (;;) {
+        const bool mine = s[0] == border;
+        const uint32_t more = __popc(__ballot_sync(kAll, mine));
+        if (more == 0) break;
+        level += more;
+        if (mine) {
+#pragma unroll
+          for (int i = 0; i + 1 < PER; ++i) s[i] = s[i + 1];
+          s[PER - 1] = 0;
+        }
+      }
+  } else {
+    for (;;) {   // the distinct keys in descending order until `count` are reached: at most `count` rounds
+      K m = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) m = key[i] < border && key[i] > m ? key[i] : m;
+      m = warp_max(m);
+      if (m == 0) break;
+      border = m;
+      above += level;
+      level = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) level += __popc(__ballot_sync(kAll, key[i] == m));
+      if (above + level >= count) break;
+    }
+    left = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) left = key[i] < border && key[i] > left ? key[i] : left;
+  }
+  uint32_t bits = 0, ties = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    bits |= uint32_t(key[i] > border) << i;
+    ties |= uint32_t(key[i] == border) << i;
+  }
+  if (border == ~K(0)) bits = ties = 0;
+  *low = border;
+  if (above + level <= count) {
+    bits |= ties;
+    *next = warp_max(left);
+  } else {   // more keys of the border's size than are left to take
+    const uint32_t before = above + lanes_before(__popc(ties)), take = before < count ? count - before : 0;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if ((ties >> i & 1) && uint32_t(__popc(ties & ((1u << i) - 1))) < take) mine |= 1u << i;
+    bits |= mine;
+    *next = border;
+  }
+  return bits;
+}
+
+// A group's key from the two largest of its experts' keys; 0: no expert left in it.
+template <class R, class K>
+__device__ __forceinline__ K group_key(K first, K second, uint32_t best) {
+  return first == 0 || best == 1 || second == 0 ? first : sortable(unsorted(first) + unsorted(second));
+}
+
+// Leaves only the keys of the kept groups; true if the border between kept and dropped groups is no wider than `slack`.
+template <int PER, class R, class K>
+__device__ __forceinline__ bool keep_groups(K (&key)[PER], const RouteArgs& a, R slack) {
+  const uint32_t lane = threadIdx.x & 31;
+  const uint32_t lanes = a.group_size / PER;
+  K low, next;
+  if (lanes && a.group_size % PER == 0 && (lanes & (lanes - 1)) == 0 && a.groups <= 32) {
+    // groups of 1, 2, 4 .. lanes: the two largest by lane, then across them
+    K first = 0, second = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      second = max(second, min(first, key[i]));
+      first = max(first, key[i]);
+    }
+    for (uint32_t d = 1; d < lanes; d *= 2) {
+      const K f = __shfl_xor_sync(kAll, first, d), s = __shfl_xor_sync(kAll, second, d);
+      second = max(max(second, s), min(first, f));
+      first = max(first, f);
+    }
+    // lane g takes group g's, so that their order is the lanes'
+    const K mine = __shfl_sync(kAll, group_key<R, K>(first, second, a.best), (lane * lanes) & 31);
+    const K one[1] = {lane < a.groups ? mine : K(0)};
+    const uint32_t kept = __ballot_sync(kAll, choose<1, K>(one, a.kept, &low, &next));
+    if (!(kept >> (lane / lanes) & 1))
+#pragma unroll
+      for (int i = 0; i < PER; ++i) key[i] = 0;
+  } else {
+    K mine[PER];   // lane l has groups l * PER and so on: at most as many as experts
+#pragma unroll
+    for (int i = 0; i < PER; ++i) mine[i] = 0;
+    for (uint32_t g = 0; g < a.groups; ++g) {
+      const uint32_t lo = g * a.group_size, hi = lo + a.group_size;
+      K first = 0, second = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const uint32_t e = lane * PER + i;
+        const K v = e >= lo && e < hi ? key[i] : K(0);
+        second = max(second, min(first, v));
+        first = max(first, v);
+      }
+      const K top = warp_max(first);
+      const uint32_t at = __ballot_sync(kAll, first == top);
+      if (lane == uint32_t(__ffs(at)) - 1) first = second;   // the largest leaves once
+      const K v = group_key<R, K>(top, warp_max(first), a.best);
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (lane * PER + i == g) mine[i] = v;
+    }
+    const uint32_t bits = choose<PER, K>(mine, a.kept, &low, &next);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint32_t e = lane * PER + i, g = e < a.experts ? e / a.group_size : 0;
+      const uint32_t b = __shfl_sync(kAll, bits, g / PER);
+      if (!(b >> (g % PER) & 1)) key[i] = 0;
+    }
+  }
+  return next != 0 && R(unsorted(low)) - R(unsorted(next)) <= slack;
+}
+
+// Keys of one token in 64 bits, as their definition has them; free: bit i, key i is of an expert that the token may have.  For tokens whose
+// border 32 bits cannot tell: rare, and kept out of line.
+template <int PER>
+__device__ __noinline__ uint32_t choose_exactly(const float (&z)[PER], uint32_t free, float top, const RouteArgs& a) {
+  const uint32_t lane = threadIdx.x & 31;
+  double s[PER], sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    s[i] = 0.0;
+    if (free >> i & 1) s[i] = a.sigmoid ? 1.0 / (1.0 + exp(-double(z[i]))) : exp(double(z[i]) - double(top));
+    sum += s[i];
+  }
+  if (!a.sigmoid) sum = warp_sum(sum);
+  unsigned long long key[PER], low, next;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (!a.sigmoid) s[i] = s[i] / sum;
+    key[i] = free >> i & 1 ? sortable(s[i] + (a.bias ? double(a.bias[lane * PER + i]) : 0.0)) : 0;
+  }
+  if (a.groups > 1) keep_groups<PER, double>(key, a, 0.0);
+  return choose<PER>(key, a.k, &low, &next);
+}
+
+template <int PER, class T>
+__device__ __forceinline__ void read_logits(const T* row, const RouteArgs& a, float (&z)[PER]) {
+  const uint32_t e0 = (threadIdx.x & 31) * PER;
+  constexpr uint32_t bytes = PER * sizeof(T), width = bytes < 16 ? bytes : 16, each = width / sizeof(T);
+  if constexpr (PER > 1) {
+    if (a.wide && e0 + PER <= a.experts) {
+#pragma unroll
+      for (int i = 0; i < PER; i += each) {
+        T t[each];
+        if constexpr (width == 16) {
+          const uint4 w = __ldcs(reinterpret_cast<const uint4*>(row + e0 + i));
+          memcpy(t, &w, 16);
+        } else if constexpr (width == 8) {
+          const uint2 w = __ldcs(reinterpret_cast<const uint2*>(row + e0 + i));
+          memcpy(t, &w, 8);
+        } else {
+          const uint32_t w = __ldcs(reinterpret_cast<const uint32_t*>(row + e0 + i));
+          memcpy(t, &w, 4);
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < each; ++q) z[i + q] = Elem<T>::get(t[q]);
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) z[i] = e0 + i < a.experts ? Elem<T>::get(row[e0 + i]) : -INFINITY;
+}
+
+// Sums over the entries before, of n values that threads of a CTA hold in turns of 256: f(i, value, sum before) for each.
+template <class V, class F>
+__device__ __forceinline__ uint32_t sums_before(uint32_t n, V&& value, F&& f) {
+  __shared__ uint32_t warp_total[8];
+  uint32_t before = 0;
+  const uint32_t warp = threadIdx.x / 32;
+  for (uint32_t first = 0; first < n; first += 256) {
+    const uint32_t i = first + threadIdx.x, v = i < n ? value(i) : 0, sum = lanes_before(v);
+    if (threadIdx.x % 32 == 31) warp_total[warp] = sum + v;
+    __syncthreads();
+    uint32_t base = before;
+    for (uint32_t w = 0; w < 8; ++w) {
+      if (w < warp) base += warp_total[w];
+      before += warp_total[w];
+    }
+    if (i < n) f(i, v, base + sum);
+    __syncthreads();
+  }
+  return before;
+}
+
+// Places a tile's slots.  A slot's place is what lies before its expert's list (begin), before the tile in that list (earlier) and before the
+// token in the tile: the tokens that the expert's bit mask marks.
+template <class B>
+__device__ __forceinline__ void place_tile(const RouteArgs& a, uint32_t tile, const uint32_t* mask, B&& begin) {
+  const uint32_t first = tile * kTile, slots = min(kTile, a.tokens - first) * a.k;
+  const uint32_t* expert = a.expert + uint64_t(first) * a.k;
+  for (uint32_t i = threadIdx.x; i < slots; i += 256) {
+    const uint32_t e = expert[i], n = i / a.k;
+    const uint64_t slot = uint64_t(first) * a.k + i;
+    uint32_t at = DGS_NO_EXPERT;
+    if (e < a.experts) {
+      const uint32_t m0 = mask[2 * e], m1 = mask[2 * e + 1];
+      at = begin(e) + (n < 32 ? __popc(m0 & ((1u << n) - 1)) : __popc(m0) + __popc(m1 & ((1u << (n - 32)) - 1)));
+      a.order[at] = uint32_t(slot);
+    }
+    a.place[slot] = at;
+  }
+}
+
+// One warp per token, a tile of 64 tokens per CTA.  The token's logits stay in registers.  The experts chosen are marked in a bit mask per
+// expert (bit = token of the tile), whose counts are what a later kernel needs to place the tile's slots; a single tile is placed here.
+// Bound by instructions: about 450 a token of 256 experts with groups and a bias, where reading takes the time of 170.
+template <int PER, class T>
+__global__ void __launch_bounds__(kRouteWarps * 32) k_route(const T* logits, const __grid_constant__ RouteArgs a) {
+  extern __shared__ uint32_t mask[];   // [experts][2]
+  __shared__ uint32_t s_empty;
+  __shared__ uint2 s_slot[kRouteWarps][DGS_ROUTE_MAX_K];   // expert and logit of a token's slots
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const bool lists = a.offsets != nullptr;
+  if (lists) {
+    for (uint32_t i = threadIdx.x; i < a.experts * 2; i += blockDim.x) mask[i] = 0;
+    if (threadIdx.x == 0) s_empty = 0;
+    __syncthreads();
+  }
+  const bool exact = !a.bias && a.best == 1;   // scores ascend with the logits, which are then exact keys
+  float bias[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) bias[i] = a.bias && lane * PER + i < a.experts ? a.bias[lane * PER + i] : 0.0f;
+  for (uint32_t n = warp; n < kTile; n += kRouteWarps) {
+    const uint64_t t = uint64_t(blockIdx.x) * kTile + n;
+    if (t >= a.tokens) break;
+    float z[PER], top = -INFINITY;
+    read_logits<PER>(logits + t * a.stride, a, z);
+    uint32_t free = 0;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      bad |= !(z[i] < INFINITY);
+      free |= uint32_t(z[i] > -INFINITY) << i;
+      top = fmaxf(top, z[i]);
+    }
+    bad = __any_sync(kAll, bad);
+    const bool sums = !a.sigmoid && (!exact || !a.renorm);   // whether the softmax over all experts is needed
+    if (!a.sigmoid) top = unsorted(warp_max(sortable(top)));
+    float s[PER], sum = 0.0f;
+    if (sums) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) s[i] = free >> i & 1 ? expf(z[i] - top) : 0.0f, sum += s[i];
+      sum = warp_sum(sum);
+    }
+    uint32_t bits = 0;
+    if (!bad) {
+      uint32_t key[PER], low, next;
+      if (exact) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) key[i] = free >> i & 1 ? sortable(z[i]) : 0;
+        if (a.groups > 1) keep_groups<PER, float>(key, a, 0.0f);
+        bits = choose<PER>(key, a.k, &low, &next);
+      } else {
+        // Keys in 32 bits.  How far two of them, or two sums of two, may be off together: a softmax score by at most 44 roundings (2^-24) of
+        // itself, 37 of them in the sum of up to 1024 terms; a sigmoid by 8 (2 ulp each of __expf's exponential and of the approximate division, whose
+        // argument's rounding moves s by |z| s (1 - s) < 0.28 of one); the scores of a softmax add up to 1 at most.  So below 2^-17 of the
+        // largest score.  The additions: 12 roundings of at most the largest key, below 2^-20 of it.
+        float most, big = 0.0f;
+        if (a.sigmoid) {
+          most = 1.0f;
+#pragma unroll
+          for (int i = 0; i < PER; ++i) s[i] = __fdividef(1.0f, 1.0f + __expf(-z[i]));
+        } else {
+          most = 1.0f / sum;
+#pragma unroll
+          for (int i = 0; i < PER; ++i) s[i] *= most;
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const float v = s[i] + bias[i];
+          key[i] = free >> i & 1 ? sortable(v) : 0;
+          if (key[i]) big = fmaxf(big, fabsf(v));
+        }
+        big = __uint_as_float(warp_max(__float_as_uint(big)));
+        const float slack = 0x1p-17f * most + 0x1p-20f * big;
+        bool close = false;
+        if (a.groups > 1) close = keep_groups<PER, float>(key, a, slack);
+        bits = choose<PER>(key, a.k, &low, &next);
+        close |= next != 0 && unsorted(low) - unsorted(next) <= slack;
+        if (close) {
+          if (a.sigmoid) top = 0.0f;
+          bits = choose_exactly<PER>(z, free, top, a);
+        }
+      }
+    }
+    // the chosen, in order, one a lane
+    const uint32_t mine = __popc(bits), before = lanes_before(mine), chosen = __shfl_sync(kAll, before + mine, 31);
+    uint32_t rank = before;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (bits >> i & 1) s_slot[warp][rank++] = make_uint2(lane * PER + i, __float_as_uint(z[i]));
+    __syncwarp();
+    const uint2 slot = s_slot[warp][lane];
+    const bool there = lane < chosen;
+    const float zs = there ? __uint_as_float(slot.y) : -INFINITY;
+    __syncwarp();
+    // weights: relative to the largest where they are divided by their sum
+    float w = 0.0f;
+    if (a.sigmoid) {
+      float ref = 0.0f;
+      if (a.renorm) ref = unsorted(warp_max(sortable(fminf(zs, 0.0f))));
+      if (there) w = expf(fminf(zs, 0.0f) - ref) / (1.0f + expf(-fabsf(zs)));
+      if (a.renorm) w = w / warp_sum(w);
+    } else {
+      const float ref = a.renorm ? unsorted(warp_max(sortable(zs))) : top;
+      if (there) w = expf(zs - ref);
+      w = w / (a.renorm ? warp_sum(w) : sum);
+    }
+    if (lane < a.k) {
+      a.expert[t * a.k + lane] = there ? slot.x : DGS_NO_EXPERT;
+      a.weight[t * a.k + lane] = there ? w * a.scale : bad ? NAN : 0.0f;
+    }
+    if (lists) {
+      if (there) atomicOr(&mask[2 * slot.x + n / 32], 1u << (n % 32));
+      if (lane == 0 && chosen < a.k) atomicAdd(&s_empty, a.k - chosen);
+    }
+  }
+  if (!lists) return;
   __syncthreads();
-  for (uint32_t w = 0; w < warp; ++w) sum += warp_total[w];
-  if (e < experts) offsets[e + 1] = sum;
-  if (e == 0) offsets[0] = 0;
+  const auto count = [&](uint32_t e) { return __popc(mask[2 * e]) + __popc(mask[2 * e + 1]); };
+  if (a.counts) {
+    for (uint32_t e = threadIdx.x; e < a.experts; e += blockDim.x) a.counts[uint64_t(e) * a.tiles + blockIdx.x] = count(e);
+    if (threadIdx.x == 0) a.counts[uint64_t(a.experts) * a.tiles + blockIdx.x] = s_empty;
+  } else {
+    uint32_t* begin = mask + 2 * a.experts;
+    const uint32_t all = sums_before(a.experts, count, [&](uint32_t e, uint32_t, uint32_t sum) { begin[e] = a.offsets[e] = sum; });
+    if (threadIdx.x == 0) a.offsets[a.experts] = all;
+    __syncthreads();
+    place_tile(a, 0, mask, [&](uint32_t e) { return begin[e]; });
+    for (uint32_t i = all + threadIdx.x; i < a.tokens * a.k; i += 256) a.order[i] = DGS_NO_EXPERT;
+  }
+}
+
+// Starts before the kernel ahead of it has ended; what that one wrote is there after this.
+__device__ __forceinline__ void wait_for_last_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// One CTA per expert (and one for the empty slots): the counts of its tiles become sums over the tiles before.
+__global__ void __launch_bounds__(256) k_route_sums(const __grid_constant__ RouteArgs a) {
+  wait_for_last_kernel();
+  uint32_t* c = a.counts + uint64_t(blockIdx.x) * a.tiles;
+  const uint32_t all = sums_before(a.tiles, [&](uint32_t i) { return c[i]; }, [&](uint32_t i, uint32_t, uint32_t sum) { c[i] = sum; });
+  if (threadIdx.x == 0) a.totals[blockIdx.x] = all;
+}
+
+__global__ void __launch_bounds__(256) k_route_place(const __grid_constant__ RouteArgs a) {
+  extern __shared__ uint32_t mask[];           // [experts][2]
+  uint32_t* begin = mask + 2 * a.experts;      // [experts + 1]
+  for (uint32_t i = threadIdx.x; i < 2 * a.experts; i += 256) mask[i] = 0;
+  wait_for_last_kernel();
+  __syncthreads();
+  const uint32_t tile = blockIdx.x, first = tile * kTile, slots = min(kTile, a.tokens - first) * a.k;
+  const uint32_t* expert = a.expert + uint64_t(first) * a.k;
+  for (uint32_t i = threadIdx.x; i < slots; i += 256) {
+    const uint32_t e = expert[i], n = i / a.k;
+    if (e < a.experts) atomicOr(&mask[2 * e + n / 32], 1u << (n % 32));
+  }
+  const uint32_t all = sums_before(a.experts, [&](uint32_t e) { return a.totals[e]; }, [&](uint32_t e, uint32_t, uint32_t sum) {
+    begin[e] = sum + a.counts[uint64_t(e) * a.tiles + tile];
+    if (tile == 0) a.offsets[e] = sum;
+  });
+  if (tile == 0 && threadIdx.x == 0) a.offsets[a.experts] = all;
+  __syncthreads();
+  place_tile(a, tile, mask, [&](uint32_t e) { return begin[e]; });
+  // order behind the last list: as many entries as the tile has empty slots
+  const uint32_t* empty = a.counts + uint64_t(a.experts) * a.tiles;
+  const uint32_t from = all + empty[tile], to = all + (tile + 1 < a.tiles ? empty[tile + 1] : a.totals[a.experts]);
+  for (uint32_t i = from + threadIdx.x; i < to; i += 256) a.order[i] = DGS_NO_EXPERT;
 }
 
 // ---- gradient ---------------------------------------------------------------------------------
 // g_j = scale * dweight_j.  softmax: dz_e = s_e ([e chosen] g_e - sum_j g_j s_j); renormalised dz_l = p_l (g_l - sum g p) on the chosen only (p the
 // weights without scale); sigmoid: dz_l = g_l s_l (1 - s_l); renormalised: p_l (g_l - sum g p)(1 - s_l).
 template <int PER, class T>
+__device__ __forceinline__ void write_logits(T* row, const RouteArgs& a, const float (&z)[PER]) {
+  const uint32_t e0 = (threadIdx.x & 31) * PER;
+  constexpr uint32_t bytes = PER * sizeof(T), width = bytes < 16 ? bytes : 16, each = width / sizeof(T);
+  if constexpr (PER > 1) {
+    if (a.wide && e0 + PER <= a.experts) {
+#pragma unroll
+      for (int i = 0; i < PER; i += each) {
+        T t[each];
+#pragma unroll
+        for (uint32_t q = 0; q < each; ++q) t[q] = Elem<T>::put(z[i + q]);
+        if constexpr (width == 16) {
+          uint4 w;
+          memcpy(&w, t, 16);
+          __stcs(reinterpret_cast<uint4*>(row + e0 + i), w);
+        } else if constexpr (width == 8) {
+          uint2 w;
+          memcpy(&w, t, 8);
+          __stcs(reinterpret_cast<uint2*>(row + e0 + i), w);
+        } else {
+          uint32_t w;
+          memcpy(&w, t, 4);
+          __stcs(reinterpret_cast<uint32_t*>(row + e0 + i), w);
+        }
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (e0 + i < a.experts) row[e0 + i] = Elem<T>::put(z[i]);
+}
+
+// A slot a lane, then the dense row.  Everything but a softmax without renormalising leaves a row zero outside the chosen, so only
+// those are worked out; where an expert is listed twice its gradients add up.
+template <int PER, class T>
 __global__ void __launch_bounds__(256) k_route_grad(const T* logits, T* dlogits, uint64_t dstride, const uint32_t* expert, const float* dweight,
                                                     const __grid_constant__ RouteArgs a, int* status) {
-  const uint32_t lane = threadIdx.x % 32;
-  for (uint64_t t = uint64_t(blockIdx.x) * 8 + threadIdx.x / 32; t < a.tokens; t += uint64_t(gridDim.x) * 8) {
-    const T* row = logits + t * a.stride;
-    float z[PER], g[PER], top = -INFINITY;
+  __shared__ float s_row[8][PER * 32 + 1];
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  float* row = s_row[warp];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) row[lane * PER + i] = 0.0f;
+  __syncwarp();
+  for (uint64_t t = uint64_t(blockIdx.x) * 8 + warp; t < a.tokens; t += uint64_t(gridDim.x) * 8) {
+    const T* from = logits + t * a.stride;
+    uint32_t e = DGS_NO_EXPERT;
+    float g = 0.0f;
+    if (lane < a.k) {
+      e = expert[t * a.k + lane];
+      g = dweight[t * a.k + lane] * a.scale;
+      if (e >= a.experts && e != DGS_NO_EXPERT) report(status, DGS_EINVAL);
+    }
+    float z[PER];
+    read_logits<PER>(from, a, z);
+    float top = -INFINITY;
     bool bad = false;
-    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) bad |= !(z[i] < INFINITY), top = fmaxf(top, z[i]);
+    bad = __any_sync(kAll, bad);
+    const float ze = e < a.experts ? Elem<T>::get(from[e]) : -INFINITY;
+    const bool there = ze > -INFINITY && !bad;
+    // an expert listed twice: the first of its lanes takes the gradients of all
+    const uint32_t same = __match_any_sync(kAll, there ? e : 0x80000000u + lane);
+    const bool leads = there && uint32_t(__ffs(same)) - 1 == lane;
+    if (__any_sync(kAll, there && !leads)) {
+      float all = 0.0f;
+      for (uint32_t j = 0; j < 32; ++j) {
+        const float v = __shfl_sync(kAll, g, j);
+        if (same >> j & 1) all += v;
+      }
+      g = all;
+    }
+    float d = 0.0f;
+    if (a.sigmoid) {
+      const float q = expf(-fabsf(ze)), slope = (ze > 0.0f ? q : 1.0f) / (1.0f + q);   // 1 - s
+      if (a.renorm) {
+        const float ref = unsorted(warp_max(sortable(leads ? fminf(ze, 0.0f) : -INFINITY)));
+        float p = leads ? expf(fminf(ze, 0.0f) - ref) / (1.0f + q) : 0.0f;
+        const float sum = warp_sum(p);
+        p = sum > 0.0f ? p / sum : 0.0f;
+        const float pull = warp_sum(leads ? g * p : 0.0f);
+        d = p * (g - pull) * slope;
+      } else {
+        d = g * (ze > 0.0f ? 1.0f : q) / (1.0f + q) * slope;
+      }
+    } else if (a.renorm) {
+      const float ref = unsorted(warp_max(sortable(leads ? ze : -INFINITY)));
+      float p = leads ? expf(ze - ref) : 0.0f;
+      const float sum = warp_sum(p);
+      p = sum > 0.0f ? p / sum : 0.0f;
+      const float pull = warp_sum(leads ? g * p : 0.0f);
+      d = p * (g - pull);
+    } else {
+      top = unsorted(warp_max(sortable(top)));
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) z[i] = z[i] > -INFINITY ? expf(z[i] - top) : 0.0f, sum += z[i];
+      sum = warp_sum(sum);
+      const float by = sum > 0.0f ? 1.0f / sum : 0.0f, p = leads ? expf(ze - top) * by : 0.0f;
+      const float pull = warp_sum(leads ? g * p : 0.0f);
+      d = p * g;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) z[i] = -z[i] * by * pull;
+    }
+    if (leads) row[e] = d;
+    __syncwarp();
+    const bool dense = !a.sigmoid && !a.renorm;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const uint32_t e = 32 * i + lane;
-      z[i] = e < a.experts ? Elem<T>::get(row[e]) : -INFINITY;
-      bad |= !(z[i] < INFINITY);
-      top = fmaxf(top, z[i]);
-      g[i] = 0.0f;
-    }
-    bad = __any_sync(kAll, bad);
-    uint32_t mine = DGS_NO_EXPERT;
-    float grad = 0.0f;
-    if (lane < a.k) {
-      mine = expert[t * a.k + lane];
-      grad = dweight[t * a.k + lane] * a.scale;
-      if (mine >= a.experts && mine != DGS_NO_EXPERT) report(status, DGS_EINVAL);
-    }
-    for (uint32_t j = 0; j < a.k; ++j) {
-      const uint32_t e = __shfl_sync(kAll, mine, j);
-      const float v = __shfl_sync(kAll, grad, j);
-      if (e % 32 != lane) continue;
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (e / 32 == uint32_t(i) && z[i] > -INFINITY) g[i] += v, bits |= 1u << i;
+      const float v = row[lane * PER + i];
+      z[i] = bad ? NAN : dense ? z[i] + v : v;
     }
     __syncwarp();
-    float ref = top;
-    if (a.renorm) {
-      ref = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (bits >> i & 1) ref = fmaxf(ref, a.sigmoid ? fminf(z[i], 0.0f) : z[i]);
-    }
-    ref = unsorted(warp_max(sortable(ref)));
-    float p[PER], sum = 0.0f, pull = 0.0f;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const bool counts = a.renorm || a.sigmoid ? bits >> i & 1 : z[i] > -INFINITY;
-      p[i] = 0.0f;
-      if (counts) p[i] = a.sigmoid ? expf(fminf(z[i], 0.0f) - (a.renorm ? ref : 0.0f)) / (1.0f + expf(-fabsf(z[i]))) : expf(z[i] - ref);
-      sum += p[i];
-      pull += g[i] * p[i];
-    }
-    const bool plain = a.sigmoid && !a.renorm;
-    sum = plain ? 1.0f : warp_sum(sum);
-    pull = plain ? 0.0f : warp_sum(pull);
-    const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
-    pull *= by;
-    T* out = dlogits + t * dstride;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const uint32_t e = 32 * i + lane;
-      float d = p[i] * by * (g[i] - pull);
-      if (a.sigmoid && (bits >> i & 1)) {
-        const float q = expf(-fabsf(z[i]));
-        d *= (z[i] > 0.0f ? q : 1.0f) / (1.0f + q);
-      }
-      if (bad) d = NAN;
-      if (e < a.experts) out[e] = Elem<T>::put(d);
-    }
+    if (leads) row[e] = 0.0f;
+    __syncwarp();
+    write_logits<PER>(dlogits + t * dstride, a, z);
   }
 }
 
@@ -504,7 +654,8 @@ using namespace dgs;
 extern "C" int dgs_route_experts_bytes(const dgs_router* router, uint64_t tokens, uint32_t experts, uint64_t* out_bytes) {
   if (!out_bytes || !router_ok(router, tokens, experts)) return DGS_EINVAL;
   if (!route_fits(router, tokens)) return DGS_ELIMIT;
-  *out_bytes = (uint64_t(experts) + 1) * ((tokens + kTile - 1) / kTile) * 4;
+  const uint64_t tiles = (tokens + kTile - 1) / kTile;
+  *out_bytes = tiles > 1 ? (uint64_t(experts) + 1) * (tiles + 1) * 4 : 0;   // a single tile is placed by the kernel that routes it
   return DGS_OK;
 }
 
@@ -539,21 +690,33 @@ extern "C" int dgs_route_experts(const dgs_router* router, const dgs_matrix* log
   a.offsets = offsets;
   a.order = order;
   a.place = place;
-  a.counts = lists ? static_cast<uint32_t*>(workspace) : nullptr;
+  a.counts = need ? static_cast<uint32_t*>(workspace) : nullptr;
+  a.totals = need ? a.counts + (uint64_t(a.experts) + 1) * a.tiles : nullptr;
+  if (!lists) a.offsets = a.counts = nullptr;
   const int rc = with_type(logits->type, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
     return with_per(a.experts, [&](auto per) {
-      k_route<per.value, T><<<a.tiles, kRouteWarps * 32, a.experts * 8, st>>>(static_cast<const T*>(logits->data), a);
+      constexpr uint32_t width = per.value * sizeof(T) < 16 ? per.value * sizeof(T) : 16;
+      a.wide = aligned(logits->data, width) && logits->stride * sizeof(T) % width == 0;
+      k_route<per.value, T><<<a.tiles, kRouteWarps * 32, (lists ? 3 * a.experts : 0) * 4, st>>>(static_cast<const T*>(logits->data), a);
       return launched();
     });
   });
-  if (rc != DGS_OK || !lists) return rc;
-  k_route_sums<<<a.experts + 1, 256, 0, st>>>(a);
-  if (launched() != DGS_OK) return DGS_ECUDA;
-  k_route_place<<<a.tiles, 256, (3 * a.experts + 1) * 4, st>>>(a);
-  if (launched() != DGS_OK) return DGS_ECUDA;
-  k_route_offsets<<<1, 1024, 0, st>>>(offsets, a.experts);
-  return launched();
+  if (rc != DGS_OK || !a.counts) return rc;
+  // the next kernels are brought onto the SMs while the one before still runs
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c = {};
+  c.blockDim = dim3(256);
+  c.stream = st;
+  c.attrs = &early;
+  c.numAttrs = 1;
+  c.gridDim = dim3(a.experts + 1);
+  if (cudaLaunchKernelEx(&c, k_route_sums, a) != cudaSuccess) return DGS_ECUDA;
+  c.gridDim = dim3(a.tiles);
+  c.dynamicSmemBytes = (3 * a.experts + 1) * 4;
+  return cudaLaunchKernelEx(&c, k_route_place, a) == cudaSuccess ? DGS_OK : DGS_ECUDA;
 }
 
 extern "C" int dgs_route_experts_grad(const dgs_router* router, const dgs_matrix* logits, const uint32_t* expert, const float* dweight,
@@ -569,10 +732,13 @@ extern "C" int dgs_route_experts_grad(const dgs_router* router, const dgs_matrix
     return DGS_EINVAL;
   int* status = operator_status_word();
   if (!status) return DGS_ECUDA;
-  const RouteArgs a = route_args(router, logits);
+  RouteArgs a = route_args(router, logits);
   return with_type(logits->type, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
     return with_per(a.experts, [&](auto per) {
+      constexpr uint32_t width = per.value * sizeof(T) < 16 ? per.value * sizeof(T) : 16;
+      a.wide = aligned(logits->data, width) && logits->stride * sizeof(T) % width == 0 && aligned(dlogits->data, width) &&
+               dlogits->stride * sizeof(T) % width == 0;
       const uint32_t ctas = std::min<uint32_t>((a.tokens + 7) / 8, kSms * 16);
       k_route_grad<per.value, T><<<ctas, 256, 0, static_cast<cudaStream_t>(stream)>>>(
           static_cast<const T*>(logits->data), static_cast<T*>(dlogits->data), dlogits->stride, expert, dweight, a, status);

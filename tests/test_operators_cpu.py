@@ -38,7 +38,7 @@ def test_sizes():
             dgs.dgs_checkpoint_bytes(rows, cols)
         assert e.value.code == dgs.DGS_EINVAL
     assert dgs.dgs_route_experts_bytes(router(), 0, 8) == 0
-    assert dgs.dgs_route_experts_bytes(router(), 65, 8) == 9 * 2 * 4
+    assert dgs.dgs_route_experts_bytes(router(), 64, 8) == 0 and dgs.dgs_route_experts_bytes(router(), 65, 8) == 9 * 3 * 4
     assert dgs.lib().dgs_checkpoint_bytes(1, 1, None) == dgs.DGS_EINVAL
 
 
@@ -115,7 +115,7 @@ def test_routers_that_are_refused(bad):
 
 
 def test_route_refusals():
-    L, r, z = dgs.lib(), router(), matrix()
+    L, r, z = dgs.lib(), router(), matrix(rows=100)
     out = C.c_uint64(0)
     assert L.dgs_route_experts_bytes(r, 1 << 31, 64, C.byref(out)) == dgs.DGS_ELIMIT
     assert L.dgs_route_experts_bytes(r, 10, 1025, C.byref(out)) == dgs.DGS_EINVAL
@@ -123,15 +123,15 @@ def test_route_refusals():
         r, z, bias, e, w, of, o, p, ws, n, None)
     assert call(e=None) == dgs.DGS_EINVAL and call(w=None) == dgs.DGS_EINVAL and call(o=None) == dgs.DGS_EINVAL
     assert call(of=None) == dgs.DGS_EINVAL and call(p=None) == dgs.DGS_EINVAL and call(ws=None) == dgs.DGS_EINVAL
-    assert call(n=259) == dgs.DGS_ENOMEM and call(ws=P * 8 + 4) == dgs.DGS_EINVAL
+    assert call(n=65 * 3 * 4 - 1) == dgs.DGS_ENOMEM and call(ws=P * 8 + 4) == dgs.DGS_EINVAL
     assert call(e=P * 3 + 1) == dgs.DGS_EINVAL and call(bias=P * 9 + 2) == dgs.DGS_EINVAL
     assert call(w=P * 3) == dgs.DGS_EINVAL and call(e=P) == dgs.DGS_EINVAL and call(bias=P * 5) == dgs.DGS_EINVAL
-    assert call(z=matrix(cols=1025)) == dgs.DGS_EINVAL
-    g = lambda z=z, e=P * 3, w=P * 4, dz=None: L.dgs_route_experts_grad(r, z, e, w, dz or matrix(data=P * 5), None)   # noqa: E731
+    assert call(z=matrix(rows=100, cols=1025)) == dgs.DGS_EINVAL
+    g = lambda z=z, e=P * 3, w=P * 4, dz=None: L.dgs_route_experts_grad(r, z, e, w, dz or matrix(rows=100, data=P * 5), None)   # noqa: E731
     assert g(e=None) == dgs.DGS_EINVAL and g(w=None) == dgs.DGS_EINVAL
-    assert g(dz=matrix(data=P * 5, cols=63)) == dgs.DGS_EINVAL and g(dz=matrix(data=P * 5, kind=1)) == dgs.DGS_EINVAL
-    assert g(dz=matrix(data=P + 4)) == dgs.DGS_EINVAL and g(dz=matrix(data=P * 3)) == dgs.DGS_EINVAL
-    assert g(dz=matrix(data=P * 5, stride=0)) == dgs.DGS_EINVAL
+    assert g(dz=matrix(rows=100, data=P * 5, cols=63)) == dgs.DGS_EINVAL and g(dz=matrix(rows=100, data=P * 5, kind=1)) == dgs.DGS_EINVAL
+    assert g(dz=matrix(rows=100, data=P + 4)) == dgs.DGS_EINVAL and g(dz=matrix(rows=100, data=P * 3)) == dgs.DGS_EINVAL
+    assert g(dz=matrix(rows=100, data=P * 5, stride=0)) == dgs.DGS_EINVAL
 
 
 def test_torch_calls_refuse_what_is_not_on_a_gpu_or_not_known():
