@@ -9,150 +9,182 @@ namespace {
 __device__ int g_operator_status;
 
 // ---- activations and their slopes -------------------------------------------------------------
-// FAST is for results of 16 bits: the exponential and division of the hardware are off by 2^-20 at most where it counts, a rounding of the
-// result by 2^-9 or 2^-12.  (32768 x 2048 in bfloat16, gelu_tanh: 125 us exact, see the kernels for what it takes now.)
-template <bool FAST> __device__ __forceinline__ float exponential(float x) { return FAST ? __expf(x) : expf(x); }
-template <bool FAST> __device__ __forceinline__ float quotient(float a, float b) { return FAST ? __fdividef(a, b) : a / b; }
-// s = 1 / (1 + e^-u) and t = 1 - s, both from e^-|u|, which does not overflow: neither loses digits to the other.
-template <bool FAST> struct Sigmoid {
+// silu is x s(x), gelu_tanh x s(u) with u = 2 sqrt(2/pi) (x + 0.044715 x^3), s(u) = 1 / (1 + e^-u).  Slopes: s (1 + x u' (1 - s)).
+constexpr float kTanhA = 1.5957691216f, kTanhB = 0.0713548163f;   // u = x (A + B x^2)
+constexpr float kLog2e = 1.4426950409f;
+
+// For results in f32: s and t = 1 - s, both from e^-|u|, which does not overflow: neither loses digits to the other.
+struct Sigmoid {
   float s, t;
   __device__ __forceinline__ explicit Sigmoid(float u) {
-    const float q = exponential<FAST>(-fabsf(u)), r = quotient<FAST>(1.0f, 1.0f + q), p = q * r;
-    s = u > 0.0f ? r : p;
-    t = u > 0.0f ? p : r;
+    const float q = expf(-fabsf(u)), r = 1.0f / (1.0f + q);
+    s = u > 0.0f ? r : q * r;
+    t = u > 0.0f ? q * r : r;
   }
 };
-template <int ACT, bool FAST>
+template <int ACT>
 __device__ __forceinline__ float act_value(float x) {
   if constexpr (ACT == DGS_ACT_RELU) return x > 0.0f ? x : (x != x ? x : 0.0f);
-  if constexpr (ACT == DGS_ACT_SILU) return x * Sigmoid<FAST>(x).s;
+  if constexpr (ACT == DGS_ACT_SILU) return x * Sigmoid(x).s;
   if constexpr (ACT == DGS_ACT_GELU) return 0.5f * x * erfcf(-x * 0.70710678f);
-  if constexpr (ACT == DGS_ACT_GELU_TANH) return x * Sigmoid<FAST>(1.5957691f * x * fmaf(0.044715f * x, x, 1.0f)).s;
+  if constexpr (ACT == DGS_ACT_GELU_TANH) return x * Sigmoid(x * fmaf(kTanhB * x, x, kTanhA)).s;
   return x;
 }
-// d act / d x.  With s = 1 / (1 + e^-u): silu u = x, slope s (1 + x (1 - s)); gelu_tanh is x s(u), u = 2 sqrt(2/pi) (x + 0.044715 x^3),
-// slope s + x u' s (1 - s).
-template <int ACT, bool FAST>
+template <int ACT>
 __device__ __forceinline__ float act_slope(float x) {
   if constexpr (ACT == DGS_ACT_RELU) return x > 0.0f ? 1.0f : (x != x ? x : 0.0f);
-  if constexpr (ACT == DGS_ACT_GELU) return fmaf(0.3989422804f * x, exponential<FAST>(-0.5f * x * x), 0.5f * erfcf(-x * 0.70710678f));
+  if constexpr (ACT == DGS_ACT_GELU) return fmaf(0.3989422804f * x, expf(-0.5f * x * x), 0.5f * erfcf(-x * 0.70710678f));
   if constexpr (ACT == DGS_ACT_SILU) {
-    const Sigmoid<FAST> g(x);
+    const Sigmoid g(x);
     return g.s * fmaf(x, g.t, 1.0f);
   }
   if constexpr (ACT == DGS_ACT_GELU_TANH) {
     x = x > 30.0f ? 30.0f : x < -30.0f ? -30.0f : x;   // from there on 0 or 1; cubes beyond would overflow
-    const float x2 = x * x, u = 1.5957691f * x * fmaf(0.044715f, x2, 1.0f), du = 1.5957691f * fmaf(0.134145f, x2, 1.0f);
-    const Sigmoid<FAST> g(u);
-    return g.s * fmaf(x * du, g.t, 1.0f);
+    const Sigmoid g(x * fmaf(kTanhB * x, x, kTanhA));
+    return g.s * fmaf(x * fmaf(3.0f * kTanhB * x, x, kTanhA), g.t, 1.0f);
   }
   return 1.0f;
+}
+
+// For results of 16 bits, whose own rounding is 2^-9 or 2^-12 of them: the hardware's exponential and reciprocal, off by 2^-20 at most, two
+// numbers at a time where there is an instruction for it.  2^-24 e^-u takes the place of e^-u, so that r = 2^24 s is a normal number wherever x s is.
+// (32768 x 2048, gelu_tanh: 104 us with expf and divisions, which are 42 instructions a value; see the kernels for now.)
+__device__ __forceinline__ float clamp_nan(float x, float most) {   // NaN stays NaN
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(most));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(-most));
+  return x;
+}
+struct Scaled {   // q = 2^-24 e^-u, r = 2^24 s: 1 - s is q r
+  float2 q, r;
+  __device__ __forceinline__ explicit Scaled(float2 minus_u_log2_minus_24) {
+    q = make_float2(hardware_exp2(minus_u_log2_minus_24.x), hardware_exp2(minus_u_log2_minus_24.y));
+    const float2 d = add2(q, both(0x1p-24f));
+    r = make_float2(hardware_reciprocal(d.x), hardware_reciprocal(d.y));
+  }
+};
+template <int ACT>
+__device__ __forceinline__ float2 exponent(float2 x) {
+  if constexpr (ACT == DGS_ACT_SILU) return fma2(x, both(-kLog2e), both(-24.0f));
+  return fma2(x, fma2(mul2(x, x), both(-kLog2e * kTanhB), both(-kLog2e * kTanhA)), both(-24.0f));
+}
+template <int ACT, bool FAST>
+__device__ __forceinline__ void values_of(float2 (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (FAST && (ACT == DGS_ACT_SILU || ACT == DGS_ACT_GELU_TANH))
+      v[i] = mul2(mul2(v[i], both(0x1p-24f)), Scaled(exponent<ACT>(v[i])).r);
+    else
+      v[i] = make_float2(act_value<ACT>(v[i].x), act_value<ACT>(v[i].y));
+  }
+}
+template <int ACT, bool FAST>
+__device__ __forceinline__ float2 slope_of(float2 x) {
+  if constexpr (FAST && (ACT == DGS_ACT_SILU || ACT == DGS_ACT_GELU_TANH)) {
+    // past these magnitudes the slope is 0 or 1 to within 2^-126, and e^-u 2^-24 would overflow
+    constexpr float most = ACT == DGS_ACT_SILU ? 100.0f : 10.5f;
+    x = make_float2(clamp_nan(x.x, most), clamp_nan(x.y, most));
+    const Scaled g(exponent<ACT>(x));
+    const float2 xu = ACT == DGS_ACT_SILU ? x : mul2(x, fma2(mul2(x, x), both(3.0f * kTanhB), both(kTanhA)));
+    return mul2(mul2(g.r, both(0x1p-24f)), fma2(xu, mul2(g.q, g.r), both(1.0f)));
+  }
+  return make_float2(act_slope<ACT>(x.x), act_slope<ACT>(x.y));
 }
 
 // ---- eight columns at a time ------------------------------------------------------------------
 // A unit is eight columns of a row; four lanes next to one another hold a block.  VEC: rows begin on 16 bytes, so that a unit is one
 // or two wide accesses; otherwise it is read and written element by element (odd lengths and strides).  Units are read some at a time, so that
 // a thread has several reads under way, and stay in their type until they are used.
-template <class T> struct Eight {
-  T v[8];
-};
 template <bool VEC, class T>
 __device__ __forceinline__ void read8(const T* p, uint32_t left, Eight<T>& e) {
   if (VEC && left >= 8) {
-    uint4 w[sizeof(T) / 2];
 #pragma unroll
-    for (uint32_t i = 0; i < sizeof(T) / 2; ++i) w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
-    memcpy(e.v, w, sizeof(w));
+    for (uint32_t i = 0; i < sizeof(T) / 2; ++i) {
+      const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+      e.w[4 * i] = w.x, e.w[4 * i + 1] = w.y, e.w[4 * i + 2] = w.z, e.w[4 * i + 3] = w.w;
+    }
     return;
   }
+  T t[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) e.v[i] = uint32_t(i) < left ? p[i] : Elem<T>::put(0.0f);
+  for (int i = 0; i < 8; ++i) t[i] = uint32_t(i) < left ? p[i] : Elem<T>::put(0.0f);
+  memcpy(e.w, t, sizeof(t));
 }
 template <bool VEC, class T>
-__device__ __forceinline__ void write8(T* p, uint32_t left, const float* v) {
+__device__ __forceinline__ void write8(T* p, uint32_t left, const float2 (&v)[4]) {
   Eight<T> e;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) e.v[i] = Elem<T>::put(v[i]);
+  of_floats(v, e);
   if (VEC && left >= 8) {
-    uint4 w[sizeof(T) / 2];
-    memcpy(w, e.v, sizeof(w));
 #pragma unroll
-    for (uint32_t i = 0; i < sizeof(T) / 2; ++i) __stcs(reinterpret_cast<uint4*>(p) + i, w[i]);
+    for (uint32_t i = 0; i < sizeof(T) / 2; ++i)
+      __stcs(reinterpret_cast<uint4*>(p) + i, make_uint4(e.w[4 * i], e.w[4 * i + 1], e.w[4 * i + 2], e.w[4 * i + 3]));
     return;
   }
+  T t[8];
+  memcpy(t, e.w, sizeof(t));
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (uint32_t(i) < left) p[i] = e.v[i];
+    if (uint32_t(i) < left) p[i] = t[i];
 }
 
 struct Units {
-  uint64_t rows;
-  uint32_t per_row;        // units of a row: width / 8
-  uint64_t step_rows;      // what one stride of the grid is in rows and units
-  uint32_t step_units;
+  uint32_t rows, per_row;   // units of a row: width / 8
+  uint32_t groups;          // rows that the grid takes at a time: what its threads make up of whole rows, at least one
 };
 
-// Walks the units of all rows, a stride of the grid apart, N at a time: load(i, row, unit) for each, then done(i, row, unit).
+// Walks the units of all rows.  A thread stays in its column and goes down the rows, N of them at a time: load(i, row, unit) for each, then
+// done(i, row, unit).  (Units dealt out by number alone cost 50 instructions of addresses for 22 of decoding: 33 us where the bytes take 16.)
 template <int N, class L, class D>
 __device__ __forceinline__ void each_unit(const Units& g, L&& load, D&& done) {
-  const uint64_t first = uint64_t(blockIdx.x) * blockDim.x + threadIdx.x;
-  uint64_t row = first / g.per_row;
-  uint32_t unit = uint32_t(first - row * g.per_row);
-  while (row < g.rows) {
-    uint64_t r[N];
-    uint32_t u[N];
+  const uint32_t t = blockIdx.x * blockDim.x + threadIdx.x, group = t / g.per_row;
+  if (group >= g.groups) return;
+  for (uint32_t unit = t - group * g.per_row; unit < g.per_row; unit += gridDim.x * blockDim.x) {
+    uint32_t row = group;
+    for (; row < g.rows && g.rows - row > (N - 1) * g.groups; row += N * g.groups) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      r[i] = row;
-      u[i] = unit;
-      if (row < g.rows) load(i, row, unit);
-      row += g.step_rows;
-      unit += g.step_units;
-      if (unit >= g.per_row) unit -= g.per_row, ++row;
+      for (int i = 0; i < N; ++i) load(i, row + i * g.groups, unit);
+#pragma unroll
+      for (int i = 0; i < N; ++i) done(i, row + i * g.groups, unit);
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (r[i] < g.rows) done(i, r[i], u[i]);
+    for (; row < g.rows; row += g.groups) {
+      load(0, row, unit);
+      done(0, row, unit);
+      if (g.rows - row <= g.groups) break;   // rows may be near 2^32
+    }
   }
 }
+constexpr int kPerSm = 4, kLoadPerSm = 6;   // CTAs on an SM
 template <class T> constexpr int kAtOnce = sizeof(T) == 2 ? 4 : 2;
 
 template <class T, bool FLOAT8, bool VEC, int ACT>
-__global__ void __launch_bounds__(256) k_checkpoint_save(Held h, uint8_t* codes, uint8_t* scales, const T* x, uint64_t xs, T* y, uint64_t ys, Units g) {
+__global__ void __launch_bounds__(256, kPerSm) k_checkpoint_save(Held h, uint8_t* codes, uint8_t* scales, const T* x, uint64_t xs, T* y, uint64_t ys, Units g) {
   constexpr int N = kAtOnce<T>;
   Eight<T> in[N];
   each_unit<N>(
       g,
-      [&](int i, uint64_t row, uint32_t unit) {
+      [&](int i, uint32_t row, uint32_t unit) {
         const uint32_t col = unit * 8;
-        read8<VEC>(x + row * xs + col, col < h.cols ? h.cols - col : 0, in[i]);
+        read8<VEC>(x + uint64_t(row) * xs + col, col < h.cols ? h.cols - col : 0, in[i]);
       },
-      [&](int i, uint64_t row, uint32_t unit) {
+      [&](int i, uint32_t row, uint32_t unit) {
         const uint32_t col = unit * 8, left = col < h.cols ? h.cols - col : 0;
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = Elem<T>::get(in[i].v[k]);
-        uint32_t m = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(v[k]) & 0x7fffffffu);
+        float2 v[4];
+        floats_of(in[i], v);
+        uint32_t m = largest_bits(in[i]);
         const uint32_t lanes = 0xfu << (threadIdx.x & 28u);   // the four lanes of the block: rows are a multiple of four units
         m = max(m, __shfl_xor_sync(lanes, m, 1));
         m = max(m, __shfl_xor_sync(lanes, m, 2));
         const uint32_t byte = scale_byte<FLOAT8>(m);
-        const float up = byte == kNanScale ? 0.0f : scale_up(byte);
-        uint2 w = make_uint2(encode4<FLOAT8>(v, up), encode4<FLOAT8>(v + 4, up));
-        if (byte == kNanScale) w = make_uint2(0, 0);
-        *reinterpret_cast<uint2*>(codes + row * h.width + col) = w;
+        const uint2 w = encode8<FLOAT8>(v, byte);
+        *reinterpret_cast<uint2*>(codes + uint64_t(row) * h.width + col) = w;
         if (unit % 4 == 0) {
-          uint8_t* s = scales + row * h.spitch + unit / 4;
+          uint8_t* s = scales + uint64_t(row) * h.spitch + unit / 4;
           *s = uint8_t(byte);
           if (unit + 4 == g.per_row)
             for (uint32_t b = g.per_row / 4; b < h.spitch; ++b) *++s = 0;
         }
         if (y) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = act_value<ACT, sizeof(T) == 2>(v[k]);
-          write8<VEC>(y + row * ys + col, left, v);
+          values_of<ACT, sizeof(T) == 2>(v);
+          write8<VEC>(y + uint64_t(row) * ys + col, left, v);
         }
       });
 }
@@ -161,51 +193,45 @@ struct HeldUnit {
   uint2 w;
   uint32_t scale;
 };
-__device__ __forceinline__ void read_held(const Held& h, uint64_t row, uint32_t unit, HeldUnit& u) {
-  u.w = __ldg(reinterpret_cast<const uint2*>(h.codes + row * h.width + unit * 8));
-  u.scale = __ldg(h.scales + row * h.spitch + unit / 4);
+__device__ __forceinline__ void read_held(const Held& h, uint32_t row, uint32_t unit, HeldUnit& u) {
+  u.w = __ldg(reinterpret_cast<const uint2*>(h.codes + uint64_t(row) * h.width + unit * 8));
+  u.scale = __ldg(h.scales + uint64_t(row) * h.spitch + unit / 4);
 }
-template <bool FLOAT8>
-__device__ __forceinline__ void decode8(const HeldUnit& u, float* v) {
-  const float down = scale_down(u.scale);
-  decode4<FLOAT8>(u.w.x, down, v);
-  decode4<FLOAT8>(u.w.y, down, v + 4);
-}
-
 template <class T, bool FLOAT8, bool VEC>
-__global__ void __launch_bounds__(256) k_checkpoint_load(Held h, T* x, uint64_t xs, Units g) {
+__global__ void __launch_bounds__(256, kLoadPerSm) k_checkpoint_load(Held h, T* x, uint64_t xs, Units g) {
   HeldUnit in[4];
   each_unit<4>(
-      g, [&](int i, uint64_t row, uint32_t unit) { read_held(h, row, unit, in[i]); },
-      [&](int i, uint64_t row, uint32_t unit) {
+      g, [&](int i, uint32_t row, uint32_t unit) { read_held(h, row, unit, in[i]); },
+      [&](int i, uint32_t row, uint32_t unit) {
         const uint32_t col = unit * 8;
         if (col >= h.cols) return;
-        float v[8];
-        decode8<FLOAT8>(in[i], v);
-        write8<VEC>(x + row * xs + col, h.cols - col, v);
+        float2 v[4];
+        decode8<FLOAT8>(in[i].w, scale_down(in[i].scale), v);
+        write8<VEC>(x + uint64_t(row) * xs + col, h.cols - col, v);
       });
 }
 
 template <class T, bool FLOAT8, bool VEC, int ACT>
-__global__ void __launch_bounds__(256) k_activation_grad(Held h, const T* dy, uint64_t dys, T* dx, uint64_t dxs, Units g) {
+__global__ void __launch_bounds__(256, kPerSm) k_activation_grad(Held h, const T* dy, uint64_t dys, T* dx, uint64_t dxs, Units g) {
   constexpr int N = kAtOnce<T>;
   HeldUnit in[N];
   Eight<T> d[N];
   each_unit<N>(
       g,
-      [&](int i, uint64_t row, uint32_t unit) {
+      [&](int i, uint32_t row, uint32_t unit) {
         const uint32_t col = unit * 8;
         read_held(h, row, unit, in[i]);
-        read8<VEC>(dy + row * dys + col, col < h.cols ? h.cols - col : 0, d[i]);
+        read8<VEC>(dy + uint64_t(row) * dys + col, col < h.cols ? h.cols - col : 0, d[i]);
       },
-      [&](int i, uint64_t row, uint32_t unit) {
+      [&](int i, uint32_t row, uint32_t unit) {
         const uint32_t col = unit * 8;
         if (col >= h.cols) return;
-        float v[8];
-        decode8<FLOAT8>(in[i], v);
+        float2 v[4], dv[4];
+        decode8<FLOAT8>(in[i].w, scale_down(in[i].scale), v);
+        floats_of(d[i], dv);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = Elem<T>::get(d[i].v[k]) * act_slope<ACT, sizeof(T) == 2>(v[k]);
-        write8<VEC>(dx + row * dxs + col, h.cols - col, v);
+        for (int k = 0; k < 4; ++k) v[k] = mul2(dv[k], slope_of<ACT, sizeof(T) == 2>(v[k]));
+        write8<VEC>(dx + uint64_t(row) * dxs + col, h.cols - col, v);
       });
 }
 
@@ -214,14 +240,11 @@ struct Plan {
   Units g;
   uint32_t ctas;
 };
-void plan_units(uint64_t rows, uint32_t width, Plan* p) {
-  p->g.rows = rows;
+void plan_units(uint64_t rows, uint32_t width, uint32_t per_sm, Plan* p) {   // as many CTAs as run at a time: each has the same rows to do
+  p->g.rows = uint32_t(rows);
   p->g.per_row = width / 8;
-  const uint64_t units = rows * p->g.per_row;
-  p->ctas = uint32_t(std::min<uint64_t>((units + 255) / 256, uint64_t(kSms) * 8));
-  const uint64_t step = uint64_t(p->ctas) * 256;
-  p->g.step_rows = step / p->g.per_row;
-  p->g.step_units = uint32_t(step % p->g.per_row);
+  p->ctas = uint32_t(std::min<uint64_t>((rows * p->g.per_row + 255) / 256, uint64_t(kSms) * per_sm));
+  p->g.groups = std::max(1u, p->ctas * 256 / p->g.per_row);
 }
 
 template <class T>
@@ -275,7 +298,7 @@ extern "C" int dgs_checkpoint_save(const dgs_checkpoint* ckpt, const dgs_matrix*
   if (ckpt->rows == 0) return DGS_OK;
   const Held h = held_of(ckpt);
   Plan p;
-  plan_units(h.rows, h.width, &p);
+  plan_units(h.rows, h.width, kPerSm, &p);
   return with_type(x->type, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
     return with_bool(ckpt->format == DGS_FORMAT_E4M3, [&](auto f8) {
@@ -296,7 +319,7 @@ extern "C" int dgs_checkpoint_load(const dgs_checkpoint* ckpt, const dgs_matrix*
   if (ckpt->rows == 0) return DGS_OK;
   const Held h = held_of(ckpt);
   Plan p;
-  plan_units(h.rows, h.width, &p);
+  plan_units(h.rows, h.width, kLoadPerSm, &p);
   return with_type(x->type, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
     return with_bool(ckpt->format == DGS_FORMAT_E4M3, [&](auto f8) {
@@ -316,7 +339,7 @@ extern "C" int dgs_checkpoint_activation_grad(const dgs_checkpoint* ckpt, int ac
   if (ckpt->rows == 0) return DGS_OK;
   const Held h = held_of(ckpt);
   Plan p;
-  plan_units(h.rows, h.width, &p);
+  plan_units(h.rows, h.width, kPerSm, &p);
   return with_type(dy->type, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
     return with_bool(ckpt->format == DGS_FORMAT_E4M3, [&](auto f8) {

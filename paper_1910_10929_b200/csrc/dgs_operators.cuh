@@ -9,6 +9,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <cstring>
 #include <type_traits>
 
 namespace dgs {
@@ -124,40 +125,140 @@ __device__ __forceinline__ float scale_down(uint32_t byte) {
   return byte == kNanScale ? __uint_as_float(0x7fc00000u) : __uint_as_float(byte << 23);
 }
 
-// Four values to four codes.  The products with a power of two are exact (below the normal numbers they are zero's neighbours
+__device__ __forceinline__ float hardware_exp2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float hardware_reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// Two numbers at a time.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long&>(r)) : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long&>(r)) : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<unsigned long long&>(r))
+      : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)), "l"(reinterpret_cast<unsigned long long&>(c)));
+  return r;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// Eight values to eight codes.  The products with a power of two are exact (below the normal numbers they are zero's neighbours
 // and round to code 0 all the same), so a code is one rounding to nearest even away from its value.
 template <bool FLOAT8>
-__device__ __forceinline__ uint32_t encode4(const float* v, float up) {
+__device__ __forceinline__ uint2 encode8(const float2 (&v)[4], uint32_t byte) {
+  using K = Code<FLOAT8>;
+  if (byte == kNanScale) return make_uint2(0, 0);
+  const float up = scale_up(byte);
+  uint32_t w[2];
   if constexpr (FLOAT8) {
-    const float2 a = make_float2(v[0] * up, v[1] * up), b = make_float2(v[2] * up, v[3] * up);
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(a, __NV_SATFINITE, __NV_E4M3), hi = __nv_cvt_float2_to_fp8x2(b, __NV_SATFINITE, __NV_E4M3);
-    return lo | hi << 16;
-  } else {
-    uint32_t w = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      int q = __float2int_rn(v[i] * up);
-      q = q > 127 ? 127 : q < -127 ? -127 : q;   // beyond e = kMax only
-      w |= uint32_t(q & 255) << (8 * i);
+    for (int h = 0; h < 2; ++h)
+      w[h] = __nv_cvt_float2_to_fp8x2(mul2(v[2 * h], both(up)), __NV_SATFINITE, __NV_E4M3) |
+             uint32_t(__nv_cvt_float2_to_fp8x2(mul2(v[2 * h + 1], both(up)), __NV_SATFINITE, __NV_E4M3)) << 16;
+  } else {
+    // 1.5 * 2^23 + q: the addition rounds, and the low byte is the code
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float2 a = mul2(v[2 * h], both(up)), b = mul2(v[2 * h + 1], both(up));
+      if (byte == uint32_t(K::kMax + 127)) {   // beyond the largest scale only
+        a = make_float2(fminf(fmaxf(a.x, -127.0f), 127.0f), fminf(fmaxf(a.y, -127.0f), 127.0f));
+        b = make_float2(fminf(fmaxf(b.x, -127.0f), 127.0f), fminf(fmaxf(b.y, -127.0f), 127.0f));
+      }
+      a = add2(a, both(12582912.0f));
+      b = add2(b, both(12582912.0f));
+      w[h] = __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
     }
-    return w;
   }
+  return make_uint2(w[0], w[1]);
 }
-// Four codes to four values.
+// Eight codes to eight values.
 template <bool FLOAT8>
-__device__ __forceinline__ void decode4(uint32_t w, float down, float* v) {
-  if constexpr (FLOAT8) {
-    const __half2 lo(__nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(w & 0xffffu), __NV_E4M3));
-    const __half2 hi(__nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(w >> 16), __NV_E4M3));
-    const float2 a = __half22float2(lo), b = __half22float2(hi);
-    v[0] = a.x * down, v[1] = a.y * down, v[2] = b.x * down, v[3] = b.y * down;
-  } else {
-    const uint32_t u = w ^ 0x80808080u;   // code + 128 in the low bits of 2^23
+__device__ __forceinline__ void decode8(uint2 w, float down, float2 (&v)[4]) {
+  const uint32_t c[2] = {w.x, w.y};
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      v[i] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650u + i)) - 8388736.0f) * down;
+  for (int h = 0; h < 2; ++h) {
+    if constexpr (FLOAT8) {
+      const __half2 lo(__nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(c[h] & 0xffffu), __NV_E4M3));
+      const __half2 hi(__nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(c[h] >> 16), __NV_E4M3));
+      v[2 * h] = mul2(__half22float2(lo), both(down));
+      v[2 * h + 1] = mul2(__half22float2(hi), both(down));
+    } else {
+      const uint32_t u = c[h] ^ 0x80808080u;   // code + 128 in the low bits of 2^23
+      const float2 a = make_float2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7651)));
+      const float2 b = make_float2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7652)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7653)));
+      v[2 * h] = mul2(add2(a, both(-8388736.0f)), both(down));
+      v[2 * h + 1] = mul2(add2(b, both(-8388736.0f)), both(down));
+    }
   }
 }
+
+// Eight numbers of a type, and as floats.
+template <class T> struct Eight {
+  uint32_t w[sizeof(T) * 2];
+};
+__device__ __forceinline__ void floats_of(const Eight<float>& e, float2 (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(e.w[2 * i]), __uint_as_float(e.w[2 * i + 1]));
+}
+__device__ __forceinline__ void floats_of(const Eight<__nv_bfloat16>& e, float2 (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(e.w[i] << 16), __uint_as_float(e.w[i] & 0xffff0000u));
+}
+__device__ __forceinline__ void floats_of(const Eight<__half>& e, float2 (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    __half2 h;
+    memcpy(&h, &e.w[i], 4);
+    v[i] = __half22float2(h);
+  }
+}
+__device__ __forceinline__ void of_floats(const float2 (&v)[4], Eight<float>& e) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) e.w[2 * i] = __float_as_uint(v[i].x), e.w[2 * i + 1] = __float_as_uint(v[i].y);
+}
+__device__ __forceinline__ void of_floats(const float2 (&v)[4], Eight<__nv_bfloat16>& e) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 b = __float22bfloat162_rn(v[i]);
+    memcpy(&e.w[i], &b, 4);
+  }
+}
+__device__ __forceinline__ void of_floats(const float2 (&v)[4], Eight<__half>& e) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 b = __float22half2_rn(v[i]);
+    memcpy(&e.w[i], &b, 4);
+  }
+}
+// The bits of the largest magnitude as a float; infinities and NaN are larger than all others.
+__device__ __forceinline__ uint32_t largest_bits(const Eight<float>& e) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, e.w[i] & 0x7fffffffu);
+  return m;
+}
+template <class T>
+__device__ __forceinline__ uint32_t largest_half(const Eight<T>& e) {
+  uint32_t m = e.w[0] & 0x7fff7fffu;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) m = __vmaxu2(m, e.w[i] & 0x7fff7fffu);
+  return max(m >> 16, m & 0xffffu);
+}
+__device__ __forceinline__ uint32_t largest_bits(const Eight<__nv_bfloat16>& e) { return largest_half(e) << 16; }
+__device__ __forceinline__ uint32_t largest_bits(const Eight<__half>& e) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)largest_half(e)))); }
 
 __device__ __forceinline__ void report(int* status, int code) { atomicMin(status, code); }
 

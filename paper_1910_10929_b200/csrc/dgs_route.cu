@@ -70,13 +70,13 @@ __device__ __forceinline__ uint32_t lanes_before(uint32_t v) {
 // Lane l has experts l * PER to l * PER + PER - 1, in its registers: experts ascend with the lanes and in each.
 // Which of its keys a lane holds among the `count` largest of the warp (bit i: key i), ties to the lowest index.  low / next: the
 // smallest key chosen and the largest left.
+// sorted: PER * 32 words of the warp's own (PER of 2 to 8).
 template <int PER, class K>
-__device__ __forceinline__ uint32_t choose(const K (&key)[PER], uint32_t count, K* low, K* next) {
-  K border = ~K(0);
-  uint32_t above = 0, level = 0;   // keys larger than the border, and equal to it
-  K left;
+__device__ __forceinline__ uint32_t choose(const K (&key)[PER], uint32_t count, uint32_t* sorted, K* low, K* next) {
+  K border = ~K(0), left = 0;
   if constexpr (PER <= 8 && sizeof(K) == 4) {
-    // the lane's keys in descending order; round by round the largest of the lanes' first ones is taken off
+    // the lane's keys in descending order; round by round the largest of the lanes' first ones are taken off.  They are kept in shared memory:
+    // moved up through registers they make three times the code, and the kernel waits for instructions as it is.
     K s[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) s[i] = key[i];
@@ -92,35 +92,34 @@ __device__ __forceinline__ uint32_t choose(const K (&key)[PER], uint32_t count, 
             s[i] = down ? max(x, y) : min(x, y);
             s[i + d] = down ? min(x, y) : max(x, y);
           }
-    K m;
-    for (;;) {
-      m = warp_max(s[0]);
-      if (m == 0) break;   // fewer than `count` are there
-      const bool mine = s[0] == m;
-      const uint32_t taken = __popc(__ballot_sync(kAll, mine));
-      if (m != border) above += level, level = 0, border = m;
-      level += taken;
-      if (mine) {
+    uint32_t* behind = sorted + (threadIdx.x & 31);
+    if constexpr (PER > 1) {
 #pragma unroll
-        for (int i = 0; i + 1 < PER; ++i) s[i] = s[i + 1];
-        s[PER - 1] = 0;
-      }
-      if (above + level >= count) break;
+      for (int i = 1; i < PER; ++i) behind[i * 32 - 32] = s[i];
+      behind[PER * 32 - 32] = 0;
     }
-    left = s[0];
-    if (m != 0)   // more keys of the border's size may follow
-      for (;;) {
-        const bool mine = s[0] == border;
-        const uint32_t more = __popc(__ballot_sync(kAll, mine));
-        if (more == 0) break;
-        level += more;
-        if (mine) {
+    uint32_t taken = 0;
+    bool more = true;
+#pragma unroll 1
+    while (more) {
 #pragma unroll
-          for (int i = 0; i + 1 < PER; ++i) s[i] = s[i + 1];
-          s[PER - 1] = 0;
+      for (int q = 0; q < (PER > 1 ? 4 : 2); ++q) {   // rounds without a branch: those too many change nothing
+        const K m = warp_max(s[0]);
+        more = taken < count && m != 0;   // 0: fewer than `count` are there
+        const bool mine = more && s[0] == m;
+        border = more ? m : border;
+        taken += __popc(__ballot_sync(kAll, mine));
+        if constexpr (PER > 1) {
+          if (mine) s[0] = *behind;
+          behind += mine ? 32 : 0;
+        } else {
+          s[0] = mine ? K(0) : s[0];
         }
       }
+    }
+    left = s[0];
   } else {
+    uint32_t taken = 0;
     for (;;) {   // the distinct keys in descending order until `count` are reached: at most `count` rounds
       K m = 0;
 #pragma unroll
@@ -128,24 +127,25 @@ __device__ __forceinline__ uint32_t choose(const K (&key)[PER], uint32_t count, 
       m = warp_max(m);
       if (m == 0) break;
       border = m;
-      above += level;
-      level = 0;
+      uint32_t level = 0;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) level += __popc(__ballot_sync(kAll, key[i] == m));
-      if (above + level >= count) break;
+      for (int i = 0; i < PER; ++i) level += key[i] == m;
+      taken += __reduce_add_sync(kAll, level);
+      if (taken >= count) break;
     }
-    left = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) left = key[i] < border && key[i] > left ? key[i] : left;
   }
   uint32_t bits = 0, ties = 0;
+  if (border != ~K(0)) {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    bits |= uint32_t(key[i] > border) << i;
-    ties |= uint32_t(key[i] == border) << i;
+    for (int i = 0; i < PER; ++i) {
+      if (key[i] > border) bits |= 1u << i;
+      if (key[i] == border) ties |= 1u << i;
+    }
   }
-  if (border == ~K(0)) bits = ties = 0;
   *low = border;
+  const uint32_t above = __reduce_add_sync(kAll, uint32_t(__popc(bits))), level = __reduce_add_sync(kAll, uint32_t(__popc(ties)));
   if (above + level <= count) {
     bits |= ties;
     *next = warp_max(left);
@@ -169,7 +169,7 @@ __device__ __forceinline__ K group_key(K first, K second, uint32_t best) {
 
 // Leaves only the keys of the kept groups; true if the border between kept and dropped groups is no wider than `slack`.
 template <int PER, class R, class K>
-__device__ __forceinline__ bool keep_groups(K (&key)[PER], const RouteArgs& a, R slack) {
+__device__ __forceinline__ bool keep_groups(K (&key)[PER], const RouteArgs& a, R slack, uint32_t* sorted) {
   const uint32_t lane = threadIdx.x & 31;
   const uint32_t lanes = a.group_size / PER;
   K low, next;
@@ -189,7 +189,7 @@ __device__ __forceinline__ bool keep_groups(K (&key)[PER], const RouteArgs& a, R
     // lane g takes group g's, so that their order is the lanes'
     const K mine = __shfl_sync(kAll, group_key<R, K>(first, second, a.best), (lane * lanes) & 31);
     const K one[1] = {lane < a.groups ? mine : K(0)};
-    const uint32_t kept = __ballot_sync(kAll, choose<1, K>(one, a.kept, &low, &next));
+    const uint32_t kept = __ballot_sync(kAll, choose<1, K>(one, a.kept, sorted, &low, &next));
     if (!(kept >> (lane / lanes) & 1))
 #pragma unroll
       for (int i = 0; i < PER; ++i) key[i] = 0;
@@ -215,7 +215,7 @@ __device__ __forceinline__ bool keep_groups(K (&key)[PER], const RouteArgs& a, R
       for (int i = 0; i < PER; ++i)
         if (lane * PER + i == g) mine[i] = v;
     }
-    const uint32_t bits = choose<PER, K>(mine, a.kept, &low, &next);
+    const uint32_t bits = choose<PER, K>(mine, a.kept, sorted, &low, &next);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const uint32_t e = lane * PER + i, g = e < a.experts ? e / a.group_size : 0;
@@ -226,27 +226,37 @@ __device__ __forceinline__ bool keep_groups(K (&key)[PER], const RouteArgs& a, R
   return next != 0 && R(unsorted(low)) - R(unsorted(next)) <= slack;
 }
 
-// Keys of one token in 64 bits, as their definition has them; free: bit i, key i is of an expert that the token may have.  For tokens whose
-// border 32 bits cannot tell: rare, and kept out of line.
+// Keys of one token in 64 bits, as their definition has them; which: bit i, key i is wanted (0 for the others).
 template <int PER>
-__device__ __noinline__ uint32_t choose_exactly(const float (&z)[PER], uint32_t free, float top, const RouteArgs& a) {
+__device__ __forceinline__ void exact_keys(const float* z, uint32_t free, uint32_t which, float top, const RouteArgs& a, unsigned long long (&key)[PER]) {
   const uint32_t lane = threadIdx.x & 31;
-  double s[PER], sum = 0.0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    s[i] = 0.0;
-    if (free >> i & 1) s[i] = a.sigmoid ? 1.0 / (1.0 + exp(-double(z[i]))) : exp(double(z[i]) - double(top));
-    sum += s[i];
+  double sum = 1.0;
+  if (!a.sigmoid) {
+    sum = 0.0;
+    for (int i = 0; i < PER; ++i)
+      if (free >> i & 1) sum += exp(double(z[i]) - double(top));
+    sum = warp_sum(sum);
   }
-  if (!a.sigmoid) sum = warp_sum(sum);
+  for (int i = 0; i < PER; ++i) {
+    key[i] = 0;
+    if (which >> i & 1) {
+      const double s = a.sigmoid ? 1.0 / (1.0 + exp(-double(z[i]))) : exp(double(z[i]) - double(top)) / sum;
+      key[i] = sortable(s + (a.bias ? double(a.bias[lane * PER + i]) : 0.0));
+    }
+  }
+}
+// For tokens whose border 32 bits cannot tell: rare, and kept out of line.  Where the groups are told apart (sure), only the keys near the
+// border are worked out again: what is above them is chosen for certain, what is below is not.
+template <int PER>
+__device__ __noinline__ uint32_t choose_exactly(const float* z, uint32_t free, uint32_t sure, uint32_t near, bool groups_close, float top, const RouteArgs& a) {
   unsigned long long key[PER], low, next;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    if (!a.sigmoid) s[i] = s[i] / sum;
-    key[i] = free >> i & 1 ? sortable(s[i] + (a.bias ? double(a.bias[lane * PER + i]) : 0.0)) : 0;
+  if (groups_close) {
+    exact_keys<PER>(z, free, free, top, a, key);
+    keep_groups<PER, double>(key, a, 0.0, nullptr);
+    return choose<PER>(key, a.k, nullptr, &low, &next);
   }
-  if (a.groups > 1) keep_groups<PER, double>(key, a, 0.0);
-  return choose<PER>(key, a.k, &low, &next);
+  exact_keys<PER>(z, free, near, top, a, key);
+  return sure | choose<PER>(key, a.k - __reduce_add_sync(kAll, uint32_t(__popc(sure))), nullptr, &low, &next);
 }
 
 template <int PER, class T>
@@ -322,11 +332,13 @@ __device__ __forceinline__ void place_tile(const RouteArgs& a, uint32_t tile, co
 // expert (bit = token of the tile), whose counts are what a later kernel needs to place the tile's slots; a single tile is placed here.
 // Bound by instructions: about 450 a token of 256 experts with groups and a bias, where reading takes the time of 170.
 template <int PER, class T>
-__global__ void __launch_bounds__(kRouteWarps * 32) k_route(const T* logits, const __grid_constant__ RouteArgs a) {
+__global__ void __launch_bounds__(kRouteWarps * 32, PER <= 8 ? 4 : 1) k_route(const T* logits, const __grid_constant__ RouteArgs a) {
   extern __shared__ uint32_t mask[];   // [experts][2]
   __shared__ uint32_t s_empty;
-  __shared__ uint2 s_slot[kRouteWarps][DGS_ROUTE_MAX_K];   // expert and logit of a token's slots
+  __shared__ uint32_t s_slot[kRouteWarps][DGS_ROUTE_MAX_K];   // the experts of a token's slots
+  __shared__ uint32_t s_sorted[kRouteWarps][PER <= 8 ? PER * 32 : 1];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  uint32_t* const sorted = s_sorted[warp];
   const bool lists = a.offsets != nullptr;
   if (lists) {
     for (uint32_t i = threadIdx.x; i < a.experts * 2; i += blockDim.x) mask[i] = 0;
@@ -337,20 +349,22 @@ __global__ void __launch_bounds__(kRouteWarps * 32) k_route(const T* logits, con
   float bias[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) bias[i] = a.bias && lane * PER + i < a.experts ? a.bias[lane * PER + i] : 0.0f;
+  float most_bias = 0.0f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) most_bias = fmaxf(most_bias, fabsf(bias[i]));
+  most_bias = __uint_as_float(warp_max(__float_as_uint(most_bias)));
   for (uint32_t n = warp; n < kTile; n += kRouteWarps) {
     const uint64_t t = uint64_t(blockIdx.x) * kTile + n;
     if (t >= a.tokens) break;
     float z[PER], top = -INFINITY;
     read_logits<PER>(logits + t * a.stride, a, z);
     uint32_t free = 0;
-    bool bad = false;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      bad |= !(z[i] < INFINITY);
-      free |= uint32_t(z[i] > -INFINITY) << i;
-      top = fmaxf(top, z[i]);
+      if (z[i] > -INFINITY) free |= 1u << i;
+      asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(z[i]));
     }
-    bad = __any_sync(kAll, bad);
+    const bool bad = __any_sync(kAll, !(top < INFINITY));
     const bool sums = !a.sigmoid && (!exact || !a.renorm);   // whether the softmax over all experts is needed
     if (!a.sigmoid) top = unsorted(warp_max(sortable(top)));
     float s[PER], sum = 0.0f;
@@ -365,51 +379,53 @@ __global__ void __launch_bounds__(kRouteWarps * 32) k_route(const T* logits, con
       if (exact) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) key[i] = free >> i & 1 ? sortable(z[i]) : 0;
-        if (a.groups > 1) keep_groups<PER, float>(key, a, 0.0f);
-        bits = choose<PER>(key, a.k, &low, &next);
+        if (a.groups > 1) keep_groups<PER, float>(key, a, 0.0f, sorted);
+        bits = choose<PER>(key, a.k, sorted, &low, &next);
       } else {
-        // Keys in 32 bits.  How far two of them, or two sums of two, may be off together: a softmax score by at most 44 roundings (2^-24) of
-        // itself, 37 of them in the sum of up to 1024 terms; a sigmoid by 8 (2 ulp each of __expf's exponential and of the approximate division, whose
-        // argument's rounding moves s by |z| s (1 - s) < 0.28 of one); the scores of a softmax add up to 1 at most.  So below 2^-17 of the
-        // largest score.  The additions: 12 roundings of at most the largest key, below 2^-20 of it.
-        float most, big = 0.0f;
+        // Keys in 32 bits.  How far two of them, or two sums of two, may be off together, in roundings (2^-24).  Sigmoid: 2 ulp of the
+        // hardware's exponential q move s by 4 s (1 - s) <= 1, its argument's roundings by 1.5 |z| s (1 - s) < 0.4, 1 + q is off by 1 s and the
+        // reciprocal by 2 s: 4.4, below 2^-20 for two and 2^-19 for four of them.  Softmax: 44 of the score itself, 37 of them in the sum of up
+        // to 1024 terms, and two scores are at most 1 together: below 2^-17 of the largest.  The additions: 2, or 12 for two sums, of at most 1 + the
+        // largest bias.
+        float most = 1.0f;
         if (a.sigmoid) {
-          most = 1.0f;
 #pragma unroll
-          for (int i = 0; i < PER; ++i) s[i] = __fdividef(1.0f, 1.0f + __expf(-z[i]));
+          for (int i = 0; i < PER; ++i) s[i] = hardware_reciprocal(1.0f + hardware_exp2(z[i] * -1.4426950409f));
         } else {
           most = 1.0f / sum;
 #pragma unroll
           for (int i = 0; i < PER; ++i) s[i] *= most;
         }
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const float v = s[i] + bias[i];
-          key[i] = free >> i & 1 ? sortable(v) : 0;
-          if (key[i]) big = fmaxf(big, fabsf(v));
-        }
-        big = __uint_as_float(warp_max(__float_as_uint(big)));
-        const float slack = 0x1p-17f * most + 0x1p-20f * big;
-        bool close = false;
-        if (a.groups > 1) close = keep_groups<PER, float>(key, a, slack);
-        bits = choose<PER>(key, a.k, &low, &next);
-        close |= next != 0 && unsorted(low) - unsorted(next) <= slack;
-        if (close) {
-          if (a.sigmoid) top = 0.0f;
-          bits = choose_exactly<PER>(z, free, top, a);
+        for (int i = 0; i < PER; ++i) key[i] = free >> i & 1 ? sortable(s[i] + bias[i]) : 0;
+        const float slack = a.sigmoid ? 0x1p-20f + 0x1p-23f * (1.0f + most_bias) : 0x1p-17f * most + 0x1p-23f * (most + most_bias);
+        const float group_slack = a.sigmoid ? 0x1p-19f + 0x1p-20f * (1.0f + most_bias) : 0x1p-17f * most + 0x1p-20f * (most + most_bias);
+        bool groups_close = false;
+        if (a.groups > 1) groups_close = keep_groups<PER, float>(key, a, group_slack, sorted);
+        bits = choose<PER>(key, a.k, sorted, &low, &next);
+        if (groups_close || (next != 0 && unsorted(low) - unsorted(next) <= slack)) {
+          uint32_t sure = 0, near = 0;
+#pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            const float d = key[i] ? unsorted(key[i]) - unsorted(low) : -INFINITY;
+            if (d > slack) sure |= 1u << i;
+            else if (d >= -slack) near |= 1u << i;
+          }
+          float copy[PER];
+#pragma unroll
+          for (int i = 0; i < PER; ++i) copy[i] = z[i];
+          bits = choose_exactly<PER>(copy, free, sure, near, groups_close, top, a);
         }
       }
     }
     // the chosen, in order, one a lane
     const uint32_t mine = __popc(bits), before = lanes_before(mine), chosen = __shfl_sync(kAll, before + mine, 31);
-    uint32_t rank = before;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (bits >> i & 1) s_slot[warp][rank++] = make_uint2(lane * PER + i, __float_as_uint(z[i]));
+    uint32_t* to = s_slot[warp] + before;
+    for (uint32_t left = bits; left; left &= left - 1) *to++ = lane * PER + __ffs(left) - 1;
     __syncwarp();
-    const uint2 slot = s_slot[warp][lane];
     const bool there = lane < chosen;
-    const float zs = there ? __uint_as_float(slot.y) : -INFINITY;
+    const uint32_t slot = there ? s_slot[warp][lane] : DGS_NO_EXPERT;
+    const float zs = there ? Elem<T>::get(logits[t * a.stride + slot]) : -INFINITY;   // still in the first cache
     __syncwarp();
     // weights: relative to the largest where they are divided by their sum
     float w = 0.0f;
@@ -424,11 +440,11 @@ __global__ void __launch_bounds__(kRouteWarps * 32) k_route(const T* logits, con
       w = w / (a.renorm ? warp_sum(w) : sum);
     }
     if (lane < a.k) {
-      a.expert[t * a.k + lane] = there ? slot.x : DGS_NO_EXPERT;
+      a.expert[t * a.k + lane] = slot;
       a.weight[t * a.k + lane] = there ? w * a.scale : bad ? NAN : 0.0f;
     }
     if (lists) {
-      if (there) atomicOr(&mask[2 * slot.x + n / 32], 1u << (n % 32));
+      if (there) atomicOr(&mask[2 * slot + n / 32], 1u << (n % 32));
       if (lane == 0 && chosen < a.k) atomicAdd(&s_empty, a.k - chosen);
     }
   }
@@ -521,7 +537,7 @@ __device__ __forceinline__ void write_logits(T* row, const RouteArgs& a, const f
 }
 
 // A slot a lane, then the dense row.  Everything but a softmax without renormalising leaves a row zero outside the chosen, so only
-// those are worked out; where an expert is listed twice its gradients add up.
+// their logits are read; where an expert is listed twice its gradients add up.
 template <int PER, class T>
 __global__ void __launch_bounds__(256) k_route_grad(const T* logits, T* dlogits, uint64_t dstride, const uint32_t* expert, const float* dweight,
                                                     const __grid_constant__ RouteArgs a, int* status) {
@@ -540,14 +556,16 @@ __global__ void __launch_bounds__(256) k_route_grad(const T* logits, T* dlogits,
       g = dweight[t * a.k + lane] * a.scale;
       if (e >= a.experts && e != DGS_NO_EXPERT) report(status, DGS_EINVAL);
     }
-    float z[PER];
-    read_logits<PER>(from, a, z);
-    float top = -INFINITY;
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) bad |= !(z[i] < INFINITY), top = fmaxf(top, z[i]);
-    bad = __any_sync(kAll, bad);
     const float ze = e < a.experts ? Elem<T>::get(from[e]) : -INFINITY;
+    const bool dense = !a.sigmoid && !a.renorm;
+    float z[PER], top = -INFINITY;
+    bool bad = !(ze < INFINITY);
+    if (dense || !__any_sync(kAll, ze > -INFINITY)) {   // a token without experts may be one with a NaN
+      read_logits<PER>(from, a, z);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) bad |= !(z[i] < INFINITY), top = fmaxf(top, z[i]);
+    }
+    bad = __any_sync(kAll, bad);
     const bool there = ze > -INFINITY && !bad;
     // an expert listed twice: the first of its lanes takes the gradients of all
     const uint32_t same = __match_any_sync(kAll, there ? e : 0x80000000u + lane);
@@ -594,7 +612,6 @@ __global__ void __launch_bounds__(256) k_route_grad(const T* logits, T* dlogits,
     }
     if (leads) row[e] = d;
     __syncwarp();
-    const bool dense = !a.sigmoid && !a.renorm;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const float v = row[lane * PER + i];

@@ -91,9 +91,9 @@ __device__ __forceinline__ void tmem_load32(uint32_t at, float (&v)[32]) {
       : "r"(at));
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
-// Two sums at a time.
-__device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
-  asm("{\n .reg .b64 s, t;\n mov.b64 s, {%0, %1};\n mov.b64 t, {%2, %3};\n add.rn.f32x2 s, s, t;\n mov.b64 {%0, %1}, s;\n}\n" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+__device__ __forceinline__ void add_to(float& a, float& b, float x, float y) {   // two sums at a time
+  const float2 s = add2(make_float2(a, b), make_float2(x, y));
+  a = s.x, b = s.y;
 }
 
 // ---- tiles in shared memory ---------------------------------------------------------------------
@@ -212,16 +212,11 @@ __global__ void __launch_bounds__(256) k_weight_decode(const __grid_constant__ W
       if (src != ~0ull) {
         const uint2 w = __ldg(reinterpret_cast<const uint2*>(a.h.codes + src * a.h.width + unit * 8));
         const float down = scale_down(__ldg(a.h.scales + src * a.h.spitch + unit / 4));
-        float v[8];
-        decode4<FLOAT8>(w.x, down, v);
-        decode4<FLOAT8>(w.y, down, v + 4);
-        uint32_t p[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-          memcpy(&p[k], &b, 4);
-        }
-        out = make_uint4(p[0], p[1], p[2], p[3]);
+        float2 v[4];
+        decode8<FLOAT8>(w, down, v);
+        Eight<__nv_bfloat16> e;
+        of_floats(v, e);
+        out = make_uint4(e.w[0], e.w[1], e.w[2], e.w[3]);
       }
     }
     *reinterpret_cast<uint4*>(a.decoded + (at + r) * a.h.width + unit * 8) = out;
@@ -233,10 +228,10 @@ __global__ void __launch_bounds__(256) k_weight_decode(const __grid_constant__ W
 // 16 behind them; what lies at a row's end, or so near an end of the matrix that a whole word would reach past it, is read element by
 // element.
 __device__ __forceinline__ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-template <class T> struct Eight {
+template <class T> struct Word {
   uint4 a;
 };
-template <> struct Eight<float> {
+template <> struct Word<float> {
   uint4 a, b;
 };
 template <class T>
@@ -253,7 +248,7 @@ __device__ __forceinline__ bool grads_whole(const T* p, uint32_t left, const T* 
   return left >= 8 && (word == at || (word >= reinterpret_cast<uintptr_t>(lo) && word + 32 <= reinterpret_cast<uintptr_t>(hi)));
 }
 template <class T>
-__device__ __forceinline__ void grads_load(Eight<T>& r, const T* p, uint32_t left, const T* lo, const T* hi) {
+__device__ __forceinline__ void grads_load(Word<T>& r, const T* p, uint32_t left, const T* lo, const T* hi) {
   r.a = make_uint4(0, 0, 0, 0);
   if constexpr (sizeof(T) == 4) {
     r.b = make_uint4(0, 0, 0, 0);
@@ -292,7 +287,7 @@ __device__ __forceinline__ uint32_t next_word(uint32_t own, uint32_t edge, uint3
 }
 // Two-byte types: the eight elements.
 template <class T>
-__device__ __forceinline__ uint4 grads_words(const Eight<T>& r, const T* p, uint32_t left, const T* lo, const T* hi) {
+__device__ __forceinline__ uint4 grads_words(const Word<T>& r, const T* p, uint32_t left, const T* lo, const T* hi) {
   if (left == 0) return make_uint4(0, 0, 0, 0);
   if (!grads_whole(p, left, lo, hi)) return grads_single(p, left);
   const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15u;
@@ -303,7 +298,7 @@ __device__ __forceinline__ void bias_add(const uint4& w, float (&bias)[8]) {   /
   const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    add2(bias[2 * i], bias[2 * i + 1], __uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xffff0000u));
+    add_to(bias[2 * i], bias[2 * i + 1], __uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xffff0000u));
   }
 }
 // The bfloat16 number that a float's upper half is, and what it leaves: exact.  Infinities and NaN go into the first part alone.
@@ -352,7 +347,7 @@ __device__ __forceinline__ void grads_split(const uint4& q, uint32_t at, bool mi
   }
 }
 template <class T>
-__device__ __forceinline__ void grads_store(const Eight<T>& r, const T* from, uint32_t left, const T* lo, const T* hi, uint32_t at, bool mine, float (&bias)[8]) {
+__device__ __forceinline__ void grads_store(const Word<T>& r, const T* from, uint32_t left, const T* lo, const T* hi, uint32_t at, bool mine, float (&bias)[8]) {
   if constexpr (sizeof(T) == 4) {
     float v[8] = {__uint_as_float(r.a.x), __uint_as_float(r.a.y), __uint_as_float(r.a.z), __uint_as_float(r.a.w),
                   __uint_as_float(r.b.x), __uint_as_float(r.b.y), __uint_as_float(r.b.z), __uint_as_float(r.b.w)};
@@ -532,7 +527,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
     constexpr auto grad_row = [](uint32_t u) { return u % 2 * 4 + u / 2 * 16; };
     const uint32_t grad_left = go + gv * 8 < a.outputs ? a.outputs - go - gv * 8 : 0;
     const T* const grad_at = dy + (first + gr) * a.dy_stride + go + gv * 8;
-    Eight<T> grad[GR];
+    Word<T> grad[GR];
     // Two-byte types: where every lane's eight elements lie in whole words in every row (mostly), a lane takes one word of a row and gets the next
     // from its neighbour; the seventeenth word of a row goes to one lane for each row.
     constexpr bool WORDS = sizeof(T) == 2 && !TMA;
@@ -592,7 +587,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
           float v[32];
           tmem_load32(tmem + (quarter * 32 << 16) + buf * 256 + group * 128 + g * 32, v);
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) add2(acc[g * 32 + i], acc[g * 32 + i + 1], v[i], v[i + 1]);
+          for (int i = 0; i < 32; i += 2) add_to(acc[g * 32 + i], acc[g * 32 + i + 1], v[i], v[i + 1]);
         }
       }
       tmem_before();
