@@ -226,39 +226,6 @@ __device__ __forceinline__ bool keep_groups(K (&key)[PER], const RouteArgs& a, R
   return next != 0 && R(unsorted(low)) - R(unsorted(next)) <= slack;
 }
 
-// Keys of one token in 64 bits, as their definition has them; which: bit i, key i is wanted (0 for the others).
-template <int PER>
-__device__ __forceinline__ void exact_keys(const float* z, uint32_t free, uint32_t which, float top, const RouteArgs& a, unsigned long long (&key)[PER]) {
-  const uint32_t lane = threadIdx.x & 31;
-  double sum = 1.0;
-  if (!a.sigmoid) {
-    sum = 0.0;
-    for (int i = 0; i < PER; ++i)
-      if (free >> i & 1) sum += exp(double(z[i]) - double(top));
-    sum = warp_sum(sum);
-  }
-  for (int i = 0; i < PER; ++i) {
-    key[i] = 0;
-    if (which >> i & 1) {
-      const double s = a.sigmoid ? 1.0 / (1.0 + exp(-double(z[i]))) : exp(double(z[i]) - double(top)) / sum;
-      key[i] = sortable(s + (a.bias ? double(a.bias[lane * PER + i]) : 0.0));
-    }
-  }
-}
-// For tokens whose border 32 bits cannot tell: rare, and kept out of line.  Where the groups are told apart (sure), only the keys near the
-// border are worked out again: what is above them is chosen for certain, what is below is not.
-template <int PER>
-__device__ __noinline__ uint32_t choose_exactly(const float* z, uint32_t free, uint32_t sure, uint32_t near, bool groups_close, float top, const RouteArgs& a) {
-  unsigned long long key[PER], low, next;
-  if (groups_close) {
-    exact_keys<PER>(z, free, free, top, a, key);
-    keep_groups<PER, double>(key, a, 0.0, nullptr);
-    return choose<PER>(key, a.k, nullptr, &low, &next);
-  }
-  exact_keys<PER>(z, free, near, top, a, key);
-  return sure | choose<PER>(key, a.k - __reduce_add_sync(kAll, uint32_t(__popc(sure))), nullptr, &low, &next);
-}
-
 template <int PER, class T>
 __device__ __forceinline__ void read_logits(const T* row, const RouteArgs& a, float (&z)[PER]) {
   const uint32_t e0 = (threadIdx.x & 31) * PER;
@@ -286,6 +253,33 @@ __device__ __forceinline__ void read_logits(const T* row, const RouteArgs& a, fl
   }
 #pragma unroll
   for (int i = 0; i < PER; ++i) z[i] = e0 + i < a.experts ? Elem<T>::get(row[e0 + i]) : -INFINITY;
+}
+
+// The choice in 64 bits, as it is defined, for tokens whose border 32 bits cannot tell: rare, and kept out of line.
+template <int PER, class T>
+__device__ __noinline__ uint32_t choose_exactly(const T* row, const RouteArgs& a, float* top) {
+  const uint32_t lane = threadIdx.x & 31;
+  float z[PER];
+  read_logits<PER>(row, a, z);
+  float most = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) most = fmaxf(most, z[i]);
+  *top = unsorted(warp_max(sortable(most)));
+  double sum = 1.0;
+  if (!a.sigmoid) {
+    sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum += exp(double(z[i]) - double(*top));
+    sum = warp_sum(sum);
+  }
+  unsigned long long key[PER], low, next;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const double s = a.sigmoid ? 1.0 / (1.0 + exp(-double(z[i]))) : exp(double(z[i]) - double(*top)) / sum;
+    key[i] = z[i] > -INFINITY ? sortable(s + (a.bias ? double(a.bias[lane * PER + i]) : 0.0)) : 0;
+  }
+  if (a.groups > 1) keep_groups<PER, double>(key, a, 0.0, nullptr);
+  return choose<PER>(key, a.k, nullptr, &low, &next);
 }
 
 // Sums over the entries before, of n values that threads of a CTA hold in turns of 256: f(i, value, sum before) for each.
@@ -353,6 +347,39 @@ __global__ void __launch_bounds__(kRouteWarps * 32, PER <= 8 ? 4 : 1) k_route(co
 #pragma unroll
   for (int i = 0; i < PER; ++i) most_bias = fmaxf(most_bias, fabsf(bias[i]));
   most_bias = __uint_as_float(warp_max(__float_as_uint(most_bias)));
+  // Slots, weights and marks of a token whose choice is made.
+  const auto finish = [&](uint32_t n, uint64_t t, uint32_t bits, bool bad, float top, float sum) {
+    // the chosen, in order, one a lane
+    const uint32_t mine = __popc(bits), before = lanes_before(mine), chosen = __shfl_sync(kAll, before + mine, 31);
+    uint32_t* to = s_slot[warp] + before;
+    for (uint32_t left = bits; left; left &= left - 1) *to++ = lane * PER + __ffs(left) - 1;
+    __syncwarp();
+    const bool there = lane < chosen;
+    const uint32_t slot = there ? s_slot[warp][lane] : DGS_NO_EXPERT;
+    const float zs = there ? Elem<T>::get(logits[t * a.stride + slot]) : -INFINITY;   // still in the first cache
+    __syncwarp();
+    // weights: relative to the largest where they are divided by their sum
+    float w = 0.0f;
+    if (a.sigmoid) {
+      float ref = 0.0f;
+      if (a.renorm) ref = unsorted(warp_max(sortable(fminf(zs, 0.0f))));
+      if (there) w = expf(fminf(zs, 0.0f) - ref) / (1.0f + expf(-fabsf(zs)));
+      if (a.renorm) w = w / warp_sum(w);
+    } else {
+      const float ref = a.renorm ? unsorted(warp_max(sortable(zs))) : top;
+      if (there) w = expf(zs - ref);
+      w = w / (a.renorm ? warp_sum(w) : sum);
+    }
+    if (lane < a.k) {
+      a.expert[t * a.k + lane] = slot;
+      a.weight[t * a.k + lane] = there ? w * a.scale : bad ? NAN : 0.0f;
+    }
+    if (lists) {
+      if (there) atomicOr(&mask[2 * slot + n / 32], 1u << (n % 32));
+      if (lane == 0 && chosen < a.k) atomicAdd(&s_empty, a.k - chosen);
+    }
+  };
+  uint32_t again = 0;   // the warp's tokens to be chosen for in 64 bits
   for (uint32_t n = warp; n < kTile; n += kRouteWarps) {
     const uint64_t t = uint64_t(blockIdx.x) * kTile + n;
     if (t >= a.tokens) break;
@@ -404,49 +431,26 @@ __global__ void __launch_bounds__(kRouteWarps * 32, PER <= 8 ? 4 : 1) k_route(co
         if (a.groups > 1) groups_close = keep_groups<PER, float>(key, a, group_slack, sorted);
         bits = choose<PER>(key, a.k, sorted, &low, &next);
         if (groups_close || (next != 0 && unsorted(low) - unsorted(next) <= slack)) {
-          uint32_t sure = 0, near = 0;
-#pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            const float d = key[i] ? unsorted(key[i]) - unsorted(low) : -INFINITY;
-            if (d > slack) sure |= 1u << i;
-            else if (d >= -slack) near |= 1u << i;
-          }
-          float copy[PER];
-#pragma unroll
-          for (int i = 0; i < PER; ++i) copy[i] = z[i];
-          bits = choose_exactly<PER>(copy, free, sure, near, groups_close, top, a);
+          again |= 1u << (n / kRouteWarps);   // afterwards: a call from here would cost every token its registers
+          continue;
         }
       }
     }
-    // the chosen, in order, one a lane
-    const uint32_t mine = __popc(bits), before = lanes_before(mine), chosen = __shfl_sync(kAll, before + mine, 31);
-    uint32_t* to = s_slot[warp] + before;
-    for (uint32_t left = bits; left; left &= left - 1) *to++ = lane * PER + __ffs(left) - 1;
-    __syncwarp();
-    const bool there = lane < chosen;
-    const uint32_t slot = there ? s_slot[warp][lane] : DGS_NO_EXPERT;
-    const float zs = there ? Elem<T>::get(logits[t * a.stride + slot]) : -INFINITY;   // still in the first cache
-    __syncwarp();
-    // weights: relative to the largest where they are divided by their sum
-    float w = 0.0f;
-    if (a.sigmoid) {
-      float ref = 0.0f;
-      if (a.renorm) ref = unsorted(warp_max(sortable(fminf(zs, 0.0f))));
-      if (there) w = expf(fminf(zs, 0.0f) - ref) / (1.0f + expf(-fabsf(zs)));
-      if (a.renorm) w = w / warp_sum(w);
-    } else {
-      const float ref = a.renorm ? unsorted(warp_max(sortable(zs))) : top;
-      if (there) w = expf(zs - ref);
-      w = w / (a.renorm ? warp_sum(w) : sum);
+    finish(n, t, bits, bad, top, sum);
+  }
+  for (; again; again &= again - 1) {
+    const uint32_t n = (__ffs(again) - 1) * kRouteWarps + warp;
+    const uint64_t t = uint64_t(blockIdx.x) * kTile + n;
+    float top, sum = 0.0f;
+    const uint32_t bits = choose_exactly<PER, T>(logits + t * a.stride, a, &top);
+    if (!a.sigmoid && !a.renorm) {
+      float z[PER];
+      read_logits<PER>(logits + t * a.stride, a, z);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) sum += expf(z[i] - top);
+      sum = warp_sum(sum);
     }
-    if (lane < a.k) {
-      a.expert[t * a.k + lane] = slot;
-      a.weight[t * a.k + lane] = there ? w * a.scale : bad ? NAN : 0.0f;
-    }
-    if (lists) {
-      if (there) atomicOr(&mask[2 * slot + n / 32], 1u << (n % 32));
-      if (lane == 0 && chosen < a.k) atomicAdd(&s_empty, a.k - chosen);
-    }
+    finish(n, t, bits, false, top, sum);
   }
   if (!lists) return;
   __syncthreads();
