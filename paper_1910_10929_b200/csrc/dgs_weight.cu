@@ -101,28 +101,24 @@ __device__ __forceinline__ void add_to(float& a, float& b, float x, float y) {  
 // 64 or 128 rows is cut into blocks of 64 columns, each row of them 128 bytes with its 16-byte pieces exchanged by the row's
 // number (128-byte swizzle).  Descriptor: how far blocks of 64 columns lie apart, and groups of 8 rows (1024 bytes).
 constexpr uint32_t kCols = 128;                // columns of either operand that a CTA brings, at most
-// A gradient's type: how many bfloat16 numbers add up to one of its values; rows of a step (waits and signals cost 0.45 us a step, the
-// products of 64 rows and one part 0.34); stages of shared memory; steps between two sums in registers; rows that a group of warps takes through
-// its registers at a time.
-template <class T> struct Grad;
-template <> struct Grad<__nv_bfloat16> { static constexpr uint32_t kParts = 1, kRows = 128, kStages = 3, kChunk = 4, kBatch = 64; };
-template <> struct Grad<__half> { static constexpr uint32_t kParts = 2, kRows = 64, kStages = 4, kChunk = 8, kBatch = 64; };
-template <> struct Grad<float> { static constexpr uint32_t kParts = 3, kRows = 64, kStages = 3, kChunk = 4, kBatch = 32; };
-template <class T> struct Shape {
-  static constexpr uint32_t kColBlock = Grad<T>::kRows * 128;   // bytes of 64 columns
+// P: how many bfloat16 numbers add up to one value of the gradient.  Rows of a step (waits and signals cost 0.45 us a step, the products of
+// 64 rows and one part 0.34); stages of shared memory; steps between two sums in registers.
+template <uint32_t P> struct Shape {
+  static constexpr uint32_t kRows = P == 1 ? 128 : 64, kStages = P == 2 ? 4 : 3, kChunk = P == 2 ? 8 : 4;
+  static constexpr uint32_t kColBlock = kRows * 128;   // bytes of 64 columns
   static constexpr uint32_t kTile = kCols / 64 * kColBlock;
-  static constexpr uint32_t kStage = kTile * (1 + Grad<T>::kParts), kSmem = 1024 + Grad<T>::kStages * kStage;
+  static constexpr uint32_t kStage = kTile * (1 + P), kSmem = 1024 + kStages * kStage;
 };
-// Two groups of four warps keep the sums (and bring gradients), four warps do the rest and leave them their registers.
+// Eight warps keep the sums, four do the rest and leave them their registers.
 constexpr uint32_t kThreads = 384, kRegsLaunch = 168, kRegsSum = 232, kRegsRest = 40;
 static_assert(kRegsSum * 256 + kRegsRest * 128 <= kRegsLaunch * kThreads, "setmaxnreg draws on the launch's registers");
-template <class T>
+template <uint32_t P>
 __device__ __forceinline__ uint32_t tile_at(uint32_t row, uint32_t piece) {   // piece: eight columns
-  return (piece >> 3) * Shape<T>::kColBlock + row * 128 + (((piece ^ row) & 7) << 4);
+  return (piece >> 3) * Shape<P>::kColBlock + row * 128 + (((piece ^ row) & 7) << 4);
 }
-template <class T>
+template <uint32_t P>
 __device__ __forceinline__ uint64_t tile_desc(uint32_t at) {
-  return uint64_t(at >> 4 & 0x3fff) | uint64_t(Shape<T>::kColBlock >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+  return uint64_t(at >> 4 & 0x3fff) | uint64_t(Shape<P>::kColBlock >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
 }
 // f32 += bf16 x bf16, 256 rows in a pair, both operands with the contracted dimension outermost
 constexpr uint32_t kIdesc = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (256u >> 4) << 24;
@@ -132,11 +128,11 @@ constexpr uint32_t kTmemCols = 512;            // two accumulators of 256 column
 
 struct WeightArgs {
   Held h;
-  const void* dy;
-  uint64_t dy_rows, dy_stride;
+  const __nv_bfloat16* dy;    // [P][plane rows][stride]: parts of the gradient, rows on 16 bytes
+  uint64_t dy_rows, dy_stride, plane_rows;
   uint32_t inputs, outputs, code_tiles, grad_tiles, splits, experts, rows_per;
   uint32_t n;           // columns of the operand that the pair shares out: 64 .. 256
-  uint32_t in_out, bias_tiles, step_rows;
+  uint32_t in_out, bias_tiles, step_rows, tiles;
   const uint32_t* offsets;
   const uint32_t* rows;
   __nv_bfloat16* decoded;   // [rows][h.width]: the checkpoint's values in dy's order, an expert's from expert_at(...) on
@@ -223,49 +219,18 @@ __global__ void __launch_bounds__(256) k_weight_decode(const __grid_constant__ W
   }
 }
 
-// ---- eight gradients ------------------------------------------------------------------------------
-// Rows may begin on any element.  Two-byte types read the aligned 16 bytes that the first of eight elements lies in and put them together with the
-// 16 behind them; what lies at a row's end, or so near an end of the matrix that a whole word would reach past it, is read element by
-// element.
-__device__ __forceinline__ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-template <class T> struct Word {
-  uint4 a;
-};
-template <> struct Word<float> {
-  uint4 a, b;
-};
-template <class T>
-__device__ __forceinline__ uint4 grads_single(const T* p, uint32_t left) {   // two-byte types
-  uint32_t v[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = uint32_t(i) < left ? __ldg(reinterpret_cast<const unsigned short*>(p) + i) : 0u;
-  return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+// ---- gradients as bfloat16 numbers ------------------------------------------------------------------
+// The bfloat16 number that a float's upper half is, and what it leaves: exact.  Infinities and NaN go into the first part alone.
+__device__ __forceinline__ uint32_t upper(float v, float* rest) {
+  uint32_t b = __float_as_uint(v);
+  const bool finite = (b & 0x7f800000u) != 0x7f800000u;
+  if (!finite && (b & 0x7fffffu)) b |= 0x400000u;
+  b &= 0xffff0000u;
+  *rest = finite ? v - __uint_as_float(b) : 0.0f;
+  return b;
 }
-// Whether eight elements at p can be had from whole words.
-template <class T>
-__device__ __forceinline__ bool grads_whole(const T* p, uint32_t left, const T* lo, const T* hi) {
-  const uintptr_t at = reinterpret_cast<uintptr_t>(p), word = at & ~uintptr_t(15);
-  return left >= 8 && (word == at || (word >= reinterpret_cast<uintptr_t>(lo) && word + 32 <= reinterpret_cast<uintptr_t>(hi)));
-}
-template <class T>
-__device__ __forceinline__ void grads_load(Word<T>& r, const T* p, uint32_t left, const T* lo, const T* hi) {
-  r.a = make_uint4(0, 0, 0, 0);
-  if constexpr (sizeof(T) == 4) {
-    r.b = make_uint4(0, 0, 0, 0);
-    if (left >= 8 && aligned16(p)) {
-      r.a = __ldg(reinterpret_cast<const uint4*>(p));
-      r.b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
-    } else if (left) {
-      uint32_t v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = uint32_t(i) < left ? __ldg(reinterpret_cast<const uint32_t*>(p) + i) : 0u;
-      r.a = make_uint4(v[0], v[1], v[2], v[3]);
-      r.b = make_uint4(v[4], v[5], v[6], v[7]);
-    }
-  } else {
-    if (grads_whole(p, left, lo, hi)) r.a = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t(15)));
-  }
-}
+template <class T> constexpr uint32_t kParts = std::is_same_v<T, float> ? 3 : std::is_same_v<T, __half> ? 2 : 1;
+
 // 16 bytes from the off-th on of two words.
 __device__ __forceinline__ uint4 words_from(const uint4& a, const uint4& b, uint32_t off) {
   uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -280,19 +245,56 @@ __device__ __forceinline__ uint4 words_from(const uint4& a, const uint4& b, uint
   for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], s);
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// The next lane's word; the last lanes of a row's sixteen have theirs in another.
-__device__ __forceinline__ uint32_t next_word(uint32_t own, uint32_t edge, uint32_t from_lane) {
-  const uint32_t n = __shfl_down_sync(0xffffffffu, own, 1), e = __shfl_sync(0xffffffffu, edge, from_lane);
-  return (threadIdx.x & 15u) == 15u ? e : n;
-}
-// Two-byte types: the eight elements.
+// Writes a gradient as kParts<T> planes of bfloat16 numbers whose sum it is exactly, with rows on 16 bytes and zeros up to `stride` and `plane_rows`.  For
+// gradients of 16 and 32 bits other than bfloat16, and for bfloat16 ones whose rows begin anywhere: TMA copies start on 16 bytes, and shifting words
+// into place on their way to the products took 3.0 us a step of 128 rows where the products take 0.8 (8192 x 768 x 50257: 1560 us).  Eight columns a
+// thread; what a row's alignment splits is in the first cache for the neighbour.
 template <class T>
-__device__ __forceinline__ uint4 grads_words(const Word<T>& r, const T* p, uint32_t left, const T* lo, const T* hi) {
-  if (left == 0) return make_uint4(0, 0, 0, 0);
-  if (!grads_whole(p, left, lo, hi)) return grads_single(p, left);
-  const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15u;
-  if (off == 0) return r.a;
-  return words_from(r.a, __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t(15)) + 1), off);
+__global__ void __launch_bounds__(256) k_weight_parts(const T* dy, uint64_t rows, uint32_t cols, uint64_t from_stride, __nv_bfloat16* out, uint32_t stride,
+                                                      uint64_t plane_rows) {
+  constexpr uint32_t P = kParts<T>;
+  const uint32_t unit = blockIdx.x * 256 + threadIdx.x, col = unit * 8;
+  if (col >= stride) return;
+  for (uint64_t row = blockIdx.y; row < plane_rows; row += gridDim.y) {
+    Eight<T> e;
+    const T* p = dy + row * from_stride + col;
+    const uint32_t left = row < rows && col < cols ? cols - col : 0;
+    if (left >= 8 && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+#pragma unroll
+      for (uint32_t i = 0; i < sizeof(T) / 2; ++i) {
+        const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+        e.w[4 * i] = w.x, e.w[4 * i + 1] = w.y, e.w[4 * i + 2] = w.z, e.w[4 * i + 3] = w.w;
+      }
+    } else {
+      // two-byte types: the words that the eight elements lie in, where neither reaches past an end of the matrix
+      const uintptr_t at = reinterpret_cast<uintptr_t>(p), word = at & ~uintptr_t(15);
+      if (sizeof(T) == 2 && left >= 8 && word >= reinterpret_cast<uintptr_t>(dy) && word + 32 <= reinterpret_cast<uintptr_t>(dy + (rows - 1) * from_stride + cols)) {
+        const uint4 w = words_from(__ldg(reinterpret_cast<const uint4*>(word)), __ldg(reinterpret_cast<const uint4*>(word) + 1), uint32_t(at - word));
+        e.w[0] = w.x, e.w[1] = w.y, e.w[2] = w.z, e.w[3] = w.w;
+      } else {
+        T t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = uint32_t(i) < left ? p[i] : Elem<T>::put(0.0f);
+        memcpy(e.w, t, sizeof(t));
+      }
+    }
+    uint4 w[P];
+    if constexpr (P == 1) {
+      w[0] = make_uint4(e.w[0], e.w[1], e.w[2], e.w[3]);
+    } else {
+      float2 v[4];
+      floats_of(e, v);
+#pragma unroll
+      for (uint32_t q = 0; q < P; ++q) {
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = upper(v[i].x, &v[i].x) >> 16 | upper(v[i].y, &v[i].y);
+        w[q] = make_uint4(o[0], o[1], o[2], o[3]);
+      }
+    }
+#pragma unroll
+    for (uint32_t q = 0; q < P; ++q) *reinterpret_cast<uint4*>(out + (q * plane_rows + row) * stride + col) = w[q];
+  }
 }
 __device__ __forceinline__ void bias_add(const uint4& w, float (&bias)[8]) {   // eight bfloat16 numbers
   const uint32_t v[4] = {w.x, w.y, w.z, w.w};
@@ -301,120 +303,74 @@ __device__ __forceinline__ void bias_add(const uint4& w, float (&bias)[8]) {   /
     add_to(bias[2 * i], bias[2 * i + 1], __uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xffff0000u));
   }
 }
-// The bfloat16 number that a float's upper half is, and what it leaves: exact.  Infinities and NaN go into the first part alone.
-__device__ __forceinline__ uint32_t upper(float v, float* rest) {
-  uint32_t b = __float_as_uint(v);
-  const bool finite = (b & 0x7f800000u) != 0x7f800000u;
-  if (!finite && (b & 0x7fffffu)) b |= 0x400000u;
-  b &= 0xffff0000u;
-  *rest = finite ? v - __uint_as_float(b) : 0.0f;
-  return b;
-}
-// Eight values in their parts to shared memory.
-template <class T>
-__device__ __forceinline__ void grads_put(float (&v)[8], uint32_t at, bool mine, float (&bias)[8]) {
-  constexpr uint32_t P = Grad<T>::kParts;
-  if (mine)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) bias[i] += v[i];
-#pragma unroll
-  for (uint32_t p = 0; p < P; ++p) {
-    uint32_t out[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t x = upper(v[2 * i], &v[2 * i]), y = upper(v[2 * i + 1], &v[2 * i + 1]);
-      out[i] = x >> 16 | y;
-    }
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + p * Shape<T>::kTile), "r"(out[0]), "r"(out[1]), "r"(out[2]), "r"(out[3]) : "memory");
-  }
-}
-template <class T>
-__device__ __forceinline__ void grads_split(const uint4& q, uint32_t at, bool mine, float (&bias)[8]) {   // two-byte types
-  if constexpr (Grad<T>::kParts == 1) {
-    if (mine) bias_add(q, bias);
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
-  } else {
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      __half2 h;
-      memcpy(&h, &w[i], 4);
-      const float2 f = __half22float2(h);
-      v[2 * i] = f.x, v[2 * i + 1] = f.y;
-    }
-    grads_put<T>(v, at, mine, bias);
-  }
-}
-template <class T>
-__device__ __forceinline__ void grads_store(const Word<T>& r, const T* from, uint32_t left, const T* lo, const T* hi, uint32_t at, bool mine, float (&bias)[8]) {
-  if constexpr (sizeof(T) == 4) {
-    float v[8] = {__uint_as_float(r.a.x), __uint_as_float(r.a.y), __uint_as_float(r.a.z), __uint_as_float(r.a.w),
-                  __uint_as_float(r.b.x), __uint_as_float(r.b.y), __uint_as_float(r.b.z), __uint_as_float(r.b.w)};
-    grads_put<T>(v, at, mine, bias);
-  } else {
-    grads_split<T>(grads_words(r, from, left, lo, hi), at, mine, bias);
-  }
-}
 
 // ---- the kernel -----------------------------------------------------------------------------------
-// A pair of CTAs forms a tile of 256 x n (n <= 256) over a run of an expert's rows, 64 rows a step.  Each CTA brings 128 columns of one operand and
-// n / 2 of the other to its shared memory; the products of the pair read both (tcgen05, cta_group::2), and each CTA's tensor memory takes
+// A pair of CTAs forms tiles of 256 x n (n <= 256), each over a run of an expert's rows, 64 or 128 rows a step.  Each CTA brings 128 columns of one
+// operand and n / 2 of the other to its shared memory; the products of the pair read both (tcgen05, cta_group::2), and each CTA's tensor memory takes
 // 128 rows of the result.  The dimension of dw that is contiguous in memory goes on those rows (lanes), so that a warp's stores are
 // coalesced wherever the layer's slice begins: inputs for [outputs][inputs], outputs for [inputs][outputs]; only the operands' roles change.
 //
-// Warps: 0 to 7 keep the sums; 8 issues products, 9 TMA copies, 10 passes on that copies have landed, and 10 and 11 sum the bias from them.
-// Gradients that a TMA copy cannot bring - those of several parts, on odd addresses, and the last rows of an expert, where the next expert's
-// would come along - come by warps 0 to 7 (TMA = false: all of them, in two groups that take turns, since a step's waits and signals cost a
-// warp several hundred cycles whatever it does in between).
+// Warps: 0 to 7 keep the sums; 8 issues products, 9 TMA copies, 10 passes on that copies have landed, and 10 and 11 sum the bias from them.  The gradients of an
+// expert's last rows, where the next expert's would come along with a copy, are brought by warps 0 to 3, with zeros behind them.
 // Sums: the tensor cores add to their accumulator with bits cut off, which over 8192 rows leaves an error of 5.5e-6; so every kChunk steps the
 // accumulators go to registers of the eight warps and are added up there with rounding (2.1e-7), while the products go on in the other half of
 // tensor memory.  Each step's part of db is summed by one of the CTAs that hold the same gradients.
-template <class T, bool TMA>
+// One pair of CTAs per pair of SMs takes tile after tile, so that the copies and products of the next run while a tile is written out (a CTA per
+// tile: 10 us around the steps of each).  Bound by what comes from the second cache: 64 KB a CTA and step of 128 rows, 0.8 us.
+struct TileOf {
+  uint64_t first, held_first;   // the tile's rows of the gradient, and of the decoded values
+  uint32_t i0, o0, ci, go;      // first input and output of the tile, and of what the CTA brings
+  uint32_t ct, split, expert;
+  uint32_t count, steps, tma_steps;
+  bool bias;
+};
+template <uint32_t R>
+__device__ __forceinline__ TileOf tile_of(const WeightArgs& a, uint32_t tile, uint32_t rank) {
+  TileOf t;
+  t.ct = tile % a.code_tiles;
+  tile /= a.code_tiles;
+  const uint32_t gt = tile % a.grad_tiles;
+  tile /= a.grad_tiles;
+  t.split = tile % a.splits;
+  t.expert = tile / a.splits;
+  t.i0 = t.ct * (a.in_out ? a.n : 256);
+  t.o0 = gt * (a.in_out ? 256 : a.n);
+  t.ci = t.i0 + rank * (a.in_out ? a.n / 2 : kCols);
+  t.go = t.o0 + rank * (a.in_out ? kCols : a.n / 2);
+  uint64_t first, last;
+  expert_rows(a, t.expert, &first, &last, false);
+  t.held_first = a.offsets ? expert_at(first, t.expert, R) : 0;
+  const uint64_t all = (last - first + R - 1) / R, each = (all + a.splits - 1) / a.splits, from = min(first + t.split * each * R, last);
+  last = min(from + each * R, last);
+  t.held_first += from - first;
+  t.first = from;
+  t.count = uint32_t(last - from);
+  t.steps = (t.count + (R - 1)) / R;
+  // the last step's gradients come by TMA only where nothing but the end of the matrix follows
+  t.tma_steps = t.count % R == 0 || last == a.dy_rows ? t.steps : t.steps - 1;
+  t.bias = a.db != nullptr && t.ct < a.bias_tiles;
+  return t;
+}
+
+template <uint32_t P>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUtensorMap held_map, const __grid_constant__ CUtensorMap grad_map) {
-  using G = Grad<T>;
-  constexpr uint32_t P = G::kParts, R = G::kRows, ST = G::kStages, CH = G::kChunk, STAGE = Shape<T>::kStage, kTile = Shape<T>::kTile, kColBlock = Shape<T>::kColBlock;
-  constexpr uint32_t SUMS = TMA ? 12 : 16;   // rows of the table that db's parts are put in
+  using S = Shape<P>;
+  constexpr uint32_t R = S::kRows, ST = S::kStages, CH = S::kChunk, STAGE = S::kStage, TILE = S::kTile, BLOCK = S::kColBlock;
   extern __shared__ unsigned char raw[];
-  __shared__ __align__(8) uint64_t s_full[ST], s_empty[ST], s_loaded[ST], s_sum_full[2], s_sum_empty[2], s_tail, s_done;
+  __shared__ __align__(8) uint64_t s_full[ST], s_empty[ST], s_loaded[ST], s_sum_full[2], s_sum_empty[2], s_tail, s_bias_done, s_done;
   __shared__ uint32_t s_tmem;
-  __shared__ float s_bias[SUMS * kCols];
-  const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = cta_rank();
+  __shared__ float s_bias[12 * kCols];   // rows 0 to 3: sums of the steps that came by TMA, 4 to 11: of the last step
+  const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = cta_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   const uint32_t tiles = (smem_at(raw) + 1023u) & ~1023u;
-
-  uint32_t b = blockIdx.x / 2;
-  const uint32_t ct = b % a.code_tiles;
-  b /= a.code_tiles;
-  const uint32_t gt = b % a.grad_tiles;
-  b /= a.grad_tiles;
-  const uint32_t split = b % a.splits, expert = b / a.splits;
-  // what the pair's tile covers, and what this CTA brings of it
-  const uint32_t i0 = ct * (a.in_out ? a.n : 256), o0 = gt * (a.in_out ? 256 : a.n);
   const uint32_t code_cols = a.in_out ? a.n / 2 : kCols, grad_cols = a.in_out ? kCols : a.n / 2;
-  const uint32_t ci = i0 + rank * code_cols, go = o0 + rank * grad_cols;
-
-  uint64_t first, last;
-  expert_rows(a, expert, &first, &last, false);
-  uint64_t held_first = a.offsets ? expert_at(first, expert, R) : 0;
-  {
-    const uint64_t steps = (last - first + R - 1) / R, each = (steps + a.splits - 1) / a.splits;
-    const uint64_t from = min(first + split * each * R, last);
-    last = min(from + each * R, last);
-    held_first += from - first;
-    first = from;
-  }
-  const uint32_t count = uint32_t(last - first), steps = (count + (R - 1)) / R, chunks = (steps + CH - 1) / CH;
-  // the last step's gradients come by TMA only where nothing but the end of the matrix follows
-  const uint32_t tma_steps = !TMA ? 0 : count % R == 0 || last == a.dy_rows ? steps : steps - 1;
-  const bool bias_here = a.db != nullptr && ct < a.bias_tiles;
 
   if (warp == 8) {
     tmem_alloc(&s_tmem, kTmemCols);
     if (lane == 0) {
       for (uint32_t s = 0; s < ST; ++s) {
-        bar_init(smem_at(&s_full[s]), TMA ? 2 : 2 + 8);   // that copies landed, of both CTAs; their warps that brought gradients
-        bar_init(smem_at(&s_empty[s]), TMA ? 3 : 1);      // products done; the bias' warps
+        bar_init(smem_at(&s_full[s]), 2);     // that copies landed, of both CTAs
+        bar_init(smem_at(&s_empty[s]), 3);    // products done; the bias' warps
         bar_init(smem_at(&s_loaded[s]), 1);
       }
       for (uint32_t i = 0; i < 2; ++i) {
@@ -422,42 +378,47 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
         bar_init(smem_at(&s_sum_empty[i]), 16);
       }
       bar_init(smem_at(&s_tail), 4);
+      bar_init(smem_at(&s_bias_done), 1);
       bar_init(smem_at(&s_done), 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
   }
-  for (uint32_t i = tid; i < SUMS * kCols; i += kThreads) s_bias[i] = 0.0f;
   tmem_before();
   __syncthreads();
   pair_sync();
   tmem_after();
   const uint32_t tmem = s_tmem;
 
+  // Every role goes through the tiles by itself; it counts steps and chunks over all of them, which is what the barriers' phases go by.
   __syncwarp();
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
-    if (warp == 8 && lane == 0 && rank == 0 && steps) {
+    if (warp == 8 && lane == 0 && rank == 0) {
       bool alive = true;
-      for (uint32_t s = 0; s < steps; ++s) {
-        const uint32_t st = s % ST, code = tiles + st * STAGE, grad = code + kTile, chunk = s / CH, acc = tmem + (chunk & 1) * 256;
-        if (s % CH == 0 && chunk >= 2) alive = bar_wait(smem_at(&s_sum_empty[chunk & 1]), (chunk / 2 - 1) & 1);
-        alive = alive && bar_wait(smem_at(&s_full[st]), s / ST & 1);
-        if (!alive) break;
-        tmem_after();
-        const uint32_t groups = min(R / 16, (count - s * R + 15) / 16);   // of sixteen rows: the last step may have fewer
+      uint32_t it = 0, chunk = 0;
+      for (uint32_t tile = pair; tile < a.tiles && alive; tile += pairs) {
+        const TileOf w = tile_of<R>(a, tile, rank);
+        for (uint32_t s = 0; s < w.steps; ++s, ++it) {
+          const uint32_t st = it % ST, code = tiles + st * STAGE, grad = code + TILE, acc = tmem + (chunk & 1) * 256;
+          if (s % CH == 0 && chunk >= 2) alive = bar_wait(smem_at(&s_sum_empty[chunk & 1]), (chunk / 2 - 1) & 1);
+          alive = alive && bar_wait(smem_at(&s_full[st]), it / ST & 1);
+          if (!alive) break;
+          tmem_after();
+          const uint32_t groups = min(R / 16, (w.count - s * R + 15) / 16);   // of sixteen rows: the last step may have fewer
 #pragma unroll
-        for (uint32_t k = 0; k < R / 16; ++k) {
-          if (k >= groups) break;
-          const uint64_t cd = tile_desc<T>(code + k * 2048);
+          for (uint32_t k = 0; k < R / 16; ++k) {
+            if (k >= groups) break;
+            const uint64_t cd = tile_desc<P>(code + k * 2048);
 #pragma unroll
-          for (uint32_t p = 0; p < P; ++p) {
-            const uint64_t gd = tile_desc<T>(grad + p * kTile + k * 2048);
-            mma(acc, a.in_out ? gd : cd, a.in_out ? cd : gd, kIdesc | idesc_cols(a.n), s % CH || k || p);
+            for (uint32_t p = 0; p < P; ++p) {
+              const uint64_t gd = tile_desc<P>(grad + p * TILE + k * 2048);
+              mma(acc, a.in_out ? gd : cd, a.in_out ? cd : gd, kIdesc | idesc_cols(a.n), s % CH || k || p);
+            }
           }
+          mma_commit(smem_at(&s_empty[st]));
+          if (s % CH == CH - 1 || s == w.steps - 1) mma_commit(smem_at(&s_sum_full[chunk++ & 1]));
         }
-        mma_commit(smem_at(&s_empty[st]));
-        if (s % CH == CH - 1 || s == steps - 1) mma_commit(smem_at(&s_sum_full[chunk & 1]));
       }
       mma_commit(smem_at(&s_done));   // nothing is under way when tensor memory is given back
       if (!(bar_wait(smem_at(&s_done), 0) && alive)) report(a.status, DGS_ETIMEOUT);
@@ -465,214 +426,160 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
     if (warp == 9 && lane == 0) {
       const uint32_t code_blocks = (code_cols + 63) / 64, grad_blocks = (grad_cols + 63) / 64;
       bool alive = true;
-      uint32_t s = 0;
-      for (; s < steps; ++s) {
-        const uint32_t st = s % ST, to = tiles + st * STAGE, bar = smem_at(&s_loaded[st]), grads = TMA && s < tma_steps ? grad_blocks : 0;
-        if (s >= ST && !(alive = bar_wait(smem_at(&s_empty[st]), (s / ST - 1) & 1))) break;
-        bar_expect(bar, (code_blocks + grads) * kColBlock);
-        for (uint32_t c = 0; c < code_blocks; ++c) tma_load(to + c * kColBlock, &held_map, int(ci + c * 64), int(held_first + uint64_t(s) * R), bar);
-        if constexpr (TMA)
-          for (uint32_t c = 0; c < grads; ++c) tma_load(to + kTile + c * kColBlock, &grad_map, int(go + c * 64), int(first + uint64_t(s) * R), bar);
+      uint32_t it = 0;
+      for (uint32_t tile = pair; tile < a.tiles && alive; tile += pairs) {
+        const TileOf w = tile_of<R>(a, tile, rank);
+        for (uint32_t s = 0; s < w.steps; ++s, ++it) {
+          const uint32_t st = it % ST, to = tiles + st * STAGE, bar = smem_at(&s_loaded[st]), grads = s < w.tma_steps ? grad_blocks : 0;
+          if (it >= ST && !(alive = bar_wait(smem_at(&s_empty[st]), (it / ST - 1) & 1))) break;
+          bar_expect(bar, (code_blocks + P * grads) * BLOCK);
+          for (uint32_t c = 0; c < code_blocks; ++c) tma_load(to + c * BLOCK, &held_map, int(w.ci + c * 64), int(w.held_first + uint64_t(s) * R), bar);
+#pragma unroll
+          for (uint32_t p = 0; p < P; ++p)
+            for (uint32_t c = 0; c < grads; ++c)
+              tma_load(to + (1 + p) * TILE + c * BLOCK, &grad_map, int(w.go + c * 64), int(p * a.plane_rows + w.first + uint64_t(s) * R), bar);
+        }
       }
       if (!alive) {   // copies that nobody waits for any more
         report(a.status, DGS_ETIMEOUT);
-        for (uint32_t i = s > ST ? s - ST : 0; i < s; ++i) bar_wait(smem_at(&s_loaded[i % ST]), i / ST & 1);
+        for (uint32_t i = it > ST ? it - ST : 0; i < it; ++i) bar_wait(smem_at(&s_loaded[i % ST]), i / ST & 1);
       }
     }
-    if (warp == 10 || (TMA && warp == 11)) {
+    if (warp >= 10) {
       // 64 threads: eight columns of every fourth row
       const uint32_t t = tid - 320, br = t / 16, bv = t % 16;
-      float bias[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
       bool alive = true;
-      for (uint32_t s = 0; s < steps; ++s) {
-        const uint32_t st = s % ST;
-        if (!(alive = warp_wait(smem_at(&s_loaded[st]), s / ST & 1))) break;
-        if (TMA && s >= tma_steps && !(alive = warp_wait(smem_at(&s_tail), 0))) break;
-        if (warp == 10 && lane == 0) bar_arrive_cluster(in_leader(smem_at(&s_full[st])));
-        if constexpr (TMA) {
-          if (bias_here && s < tma_steps && s % a.bias_tiles == ct) {
+      uint32_t it = 0, tails = 0;
+      for (uint32_t tile = pair; tile < a.tiles && alive; tile += pairs) {
+        const TileOf w = tile_of<R>(a, tile, rank);
+        float bias[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
+        for (uint32_t s = 0; s < w.steps; ++s, ++it) {
+          const uint32_t st = it % ST;
+          if (!(alive = warp_wait(smem_at(&s_loaded[st]), it / ST & 1))) break;
+          if (s >= w.tma_steps && warp == 10 && !(alive = warp_wait(smem_at(&s_tail), tails++ & 1))) break;
+          if (warp == 10 && lane == 0) bar_arrive_cluster(in_leader(smem_at(&s_full[st])));
+          if (w.bias && s < w.tma_steps && s % a.bias_tiles == w.ct) {
 #pragma unroll 4
             for (uint32_t r = br; r < R; r += 4) {
-              uint4 w;
-              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
-                           : "r"(tiles + st * STAGE + kTile + tile_at<T>(r, bv)));
-              bias_add(w, bias);
+#pragma unroll
+              for (uint32_t p = 0; p < P; ++p) {
+                uint4 v;
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                             : "r"(tiles + st * STAGE + (1 + p) * TILE + tile_at<P>(r, bv)));
+                bias_add(v, bias);
+              }
             }
           }
           __syncwarp();
           if (lane == 0) bar_arrive(smem_at(&s_empty[st]));
         }
+        if (w.bias && alive) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s_bias[br * kCols + bv * 8 + i] = bias[i];
+          asm volatile("bar.sync 1, 64;" ::: "memory");
+          const uint32_t rows = w.tma_steps < w.steps && (w.steps - 1) % a.bias_tiles == w.ct ? 12 : 4;
+          for (uint32_t c = t; c < grad_cols && w.go + c < a.outputs; c += 64) {
+            float v = 0.0f;
+            for (uint32_t i = 0; i < rows; ++i) v += s_bias[i * kCols + c];
+            float* p = a.db + (uint64_t(w.split * a.bias_tiles + w.ct) * a.experts + w.expert) * a.outputs + w.go + c;
+            *p = a.add_b ? *p + v : v;
+          }
+          asm volatile("bar.sync 1, 64;" ::: "memory");
+        }
+        if (warp == 10 && lane == 0) bar_arrive(smem_at(&s_bias_done));
       }
       if (!alive && lane == 0) report(a.status, DGS_ETIMEOUT);
-      if constexpr (TMA)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s_bias[br * kCols + bv * 8 + i] = bias[i];
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSum));
-    const T* dy = static_cast<const T*>(a.dy);
-    const T* dy_end = dy + ((a.dy_rows - 1) * a.dy_stride + a.outputs);   // read where dy_rows > 0 only
-    const uint32_t quarter = warp % 4, group = warp / 4, t = tid % 128;
-    float acc[128];
-#pragma unroll
-    for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
+    const uint32_t quarter = warp % 4, group = warp / 4;
     bool alive = true;
-
-    // Gradients: eight columns a thread, of rows that leave the same remainder by 8 in a warp (by 4, two in turn): rows 8 apart begin on the
-    // same bytes of a word.  A batch of rows goes through the registers at a time.
-    constexpr uint32_t BATCH = TMA ? 16 : G::kBatch, GR = BATCH / 8;
-    const uint32_t gr = t / 32 + (lane / 16) * 8, gv = t % 16;
-    constexpr auto grad_row = [](uint32_t u) { return u % 2 * 4 + u / 2 * 16; };
-    const uint32_t grad_left = go + gv * 8 < a.outputs ? a.outputs - go - gv * 8 : 0;
-    const T* const grad_at = dy + (first + gr) * a.dy_stride + go + gv * 8;
-    Word<T> grad[GR];
-    // Two-byte types: where every lane's eight elements lie in whole words in every row (mostly), a lane takes one word of a row and gets the next
-    // from its neighbour; the seventeenth word of a row goes to one lane for each row.
-    constexpr bool WORDS = sizeof(T) == 2 && !TMA;
-    bool fast = false;
-    uint4 edge = make_uint4(0, 0, 0, 0);
-    auto fetch_grads = [&](uint32_t from) {
-      const T* p = grad_at + uint64_t(from) * a.dy_stride;
-      if constexpr (WORDS) {
-        const uintptr_t low = reinterpret_cast<uintptr_t>(p) & ~uintptr_t(15), high = (reinterpret_cast<uintptr_t>(p + grad_row(GR - 1) * a.dy_stride) & ~uintptr_t(15)) + 32;
-        fast = __all_sync(0xffffffffu, grad_left >= 8 && from + BATCH <= count && low >= reinterpret_cast<uintptr_t>(dy) && high <= reinterpret_cast<uintptr_t>(dy_end));
-        if (fast) {
+    uint32_t it = 0, drained = 0, ordinal = 0;
+    for (uint32_t tile = pair; tile < a.tiles && alive; tile += pairs, ++ordinal) {
+      const TileOf w = tile_of<R>(a, tile, rank);
+      const uint32_t chunks = (w.steps + CH - 1) / CH;
+      float acc[128];
 #pragma unroll
-          for (uint32_t u = 0; u < GR; ++u)
-            grad[u].a = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p + grad_row(u) * a.dy_stride) & ~uintptr_t(15)));
-          if (gv < GR) edge = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p + grad_row(gv) * a.dy_stride + kCols - gv * 8) & ~uintptr_t(15)));
-          return;
-        }
-      }
-#pragma unroll
-      for (uint32_t u = 0; u < GR; ++u)
-        grads_load<T>(grad[u], p + grad_row(u) * a.dy_stride, from + gr + grad_row(u) < count ? grad_left : 0, dy, dy_end);
-    };
-    auto store_grads = [&](uint32_t from, uint32_t to, uint32_t row, bool mine, float (&bias)[8]) {
-      const T* p = grad_at + uint64_t(from) * a.dy_stride;
-      if constexpr (WORDS) {
-        if (fast) {
-#pragma unroll
-          for (uint32_t u = 0; u < GR; ++u) {
-            const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p + grad_row(u) * a.dy_stride)) & 15u;   // the same in all lanes
-            uint4 w = grad[u].a;
-            if (off) {
-              uint4 next;
-              const uint32_t from_lane = (lane & 16u) + u;
-              next.x = next_word(w.x, edge.x, from_lane);
-              next.y = next.z = next.w = 0;
-              if (off > 4) next.y = next_word(w.y, edge.y, from_lane);
-              if (off > 8) next.z = next_word(w.z, edge.z, from_lane), next.w = next_word(w.w, edge.w, from_lane);
-              w = words_from(w, next, off);
-            }
-            grads_split<T>(w, to + tile_at<T>(row + gr + grad_row(u), gv), mine, bias);
-          }
-          return;
-        }
-      }
-#pragma unroll
-      for (uint32_t u = 0; u < GR; ++u)
-        grads_store<T>(grad[u], p + grad_row(u) * a.dy_stride, from + gr + grad_row(u) < count ? grad_left : 0, dy, dy_end, to + tile_at<T>(row + gr + grad_row(u), gv), mine, bias);
-    };
-    uint32_t drained = 0;
-    auto drain = [&]() {
-      const uint32_t buf = drained & 1;
-      if (!(alive = warp_wait(smem_at(&s_sum_full[buf]), drained / 2 & 1))) return;
-      tmem_after();
-#pragma unroll
-      for (uint32_t g = 0; g < 4; ++g) {
-        if (group * 128 + g * 32 < a.n) {
-          float v[32];
-          tmem_load32(tmem + (quarter * 32 << 16) + buf * 256 + group * 128 + g * 32, v);
-#pragma unroll
-          for (int i = 0; i < 32; i += 2) add_to(acc[g * 32 + i], acc[g * 32 + i + 1], v[i], v[i + 1]);
-        }
-      }
-      tmem_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive_cluster(in_leader(smem_at(&s_sum_empty[buf])));
-      ++drained;
-    };
-    if constexpr (TMA) {
-      while (alive && drained < chunks) {
-        if (drained + 1 == chunks && tma_steps < steps && group == 0) {
-          // an expert's last rows: a batch at a time, zeros behind them
-          const uint32_t s = steps - 1, at = tiles + s % ST * STAGE + kTile;
-          if (s >= ST && !(alive = warp_wait(smem_at(&s_empty[s % ST]), (s / ST - 1) & 1))) break;
+      for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
+      for (uint32_t c = 0; c < chunks; ++c, ++drained) {
+        if (c + 1 == chunks && w.tma_steps < w.steps && group == 0) {
+          // an expert's last rows: eight columns of every eighth row a thread, zeros behind them
+          const uint32_t last = it + w.steps - 1, at = tiles + last % ST * STAGE + TILE, gr = tid / 16, gv = tid % 16, col = w.go + gv * 8;
+          if (last >= ST && !(alive = warp_wait(smem_at(&s_empty[last % ST]), (last / ST - 1) & 1))) break;
+          if (ordinal && !(alive = warp_wait(smem_at(&s_bias_done), (ordinal - 1) & 1))) break;   // the table is free
           float bias[8] = {};
-#pragma unroll 1
-          for (uint32_t row = 0; row < R; row += BATCH) {
-            fetch_grads(s * R + row);
-            store_grads(s * R + row, at, row, bias_here && s % a.bias_tiles == ct, bias);
+#pragma unroll 2
+          for (uint32_t r = gr; r < R; r += 8) {
+            const uint32_t j = (w.steps - 1) * R + r;
+#pragma unroll
+            for (uint32_t p = 0; p < P; ++p) {
+              uint4 v = make_uint4(0, 0, 0, 0);
+              if (j < w.count && col < a.outputs) {
+                const __nv_bfloat16* from = a.dy + (p * a.plane_rows + w.first + j) * a.dy_stride + col;
+                if (col + 8 <= a.outputs) {
+                  v = __ldg(reinterpret_cast<const uint4*>(from));
+                } else {
+                  uint32_t e[8];
+#pragma unroll
+                  for (uint32_t i = 0; i < 8; ++i) e[i] = col + i < a.outputs ? __ldg(reinterpret_cast<const unsigned short*>(from) + i) : 0u;
+                  v = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+                }
+              }
+              bias_add(v, bias);
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + p * TILE + tile_at<P>(r, gv)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+            }
           }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s_bias[(4 + gr) * kCols + gv * 8 + i] = bias[i];
           writes_to_async_proxy();
           __syncwarp();
           if (lane == 0) bar_arrive(smem_at(&s_tail));
+        }
+        const uint32_t buf = drained & 1;
+        if (!(alive = warp_wait(smem_at(&s_sum_full[buf]), drained / 2 & 1))) break;
+        tmem_after();
 #pragma unroll
-          for (int i = 0; i < 8; ++i) s_bias[(4 + t / 16) * kCols + gv * 8 + i] = bias[i];   // behind the rows of the TMA steps' sums
+        for (uint32_t g = 0; g < 4; ++g) {
+          if (group * 128 + g * 32 < a.n) {
+            float v[32];
+            tmem_load32(tmem + (quarter * 32 << 16) + buf * 256 + group * 128 + g * 32, v);
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) add_to(acc[g * 32 + i], acc[g * 32 + i + 1], v[i], v[i + 1]);
+          }
         }
-        drain();
-      }
-    } else {
-      float bias[8] = {};
-      // what follows a batch: the next of this step or the first of the group's next step
-      auto after = [&](uint32_t from) { return (from / BATCH + 1) % (R / BATCH) ? from + BATCH : from / R * R + 2 * R; };
-      if (steps) fetch_grads(group * R);
-      for (uint32_t s = group; s < steps; s += 2) {
-        const uint32_t st = s % ST, at = tiles + st * STAGE + kTile;
-        if (s >= ST && !(alive = warp_wait(smem_at(&s_empty[st]), (s / ST - 1) & 1))) break;
-        const bool mine = bias_here && s % a.bias_tiles == ct;
-#pragma unroll 1
-        for (uint32_t row = 0; row < R; row += BATCH) {
-          store_grads(s * R + row, at, row, mine, bias);
-          fetch_grads(after(s * R + row));
-        }
-        writes_to_async_proxy();
+        tmem_before();
         __syncwarp();
-        if (lane == 0) bar_arrive_cluster(in_leader(smem_at(&s_full[st])));
-        // the wait above said that step s - ST is done
-        if (s >= ST && s - ST >= CH * (drained + 1) - 1) {
-          drain();
-          if (!alive) break;
+        if (lane == 0) bar_arrive_cluster(in_leader(smem_at(&s_sum_empty[buf])));
+      }
+      it += w.steps;
+      // results to memory
+      const uint32_t row = rank * 128 + quarter * 32 + lane;
+      const uint32_t lane_at = (a.in_out ? w.o0 : w.i0) + row, lane_end = a.in_out ? a.outputs : a.inputs;
+      const uint32_t col_at = (a.in_out ? w.i0 : w.o0) + group * 128, col_end = min(a.in_out ? a.inputs : a.outputs, (a.in_out ? w.i0 : w.o0) + a.n);
+      if (alive && lane_at < lane_end) {
+        float* p = a.dw + (uint64_t(w.split) * a.experts + w.expert) * a.inputs * a.outputs + uint64_t(col_at) * lane_end + lane_at;
+#pragma unroll
+        for (uint32_t g = 0; g < 4; ++g) {
+          if (a.add_w) {
+            float old[32];
+#pragma unroll
+            for (uint32_t i = 0; i < 32; ++i) old[i] = col_at + g * 32 + i < col_end ? p[uint64_t(g * 32 + i) * lane_end] : 0.0f;
+#pragma unroll
+            for (uint32_t i = 0; i < 32; ++i) acc[g * 32 + i] += old[i];
+          }
+#pragma unroll
+          for (uint32_t i = 0; i < 32; ++i)
+            if (col_at + g * 32 + i < col_end) p[uint64_t(g * 32 + i) * lane_end] = acc[g * 32 + i];
         }
       }
-      while (alive && drained < chunks) drain();
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s_bias[(group * 8 + t / 16) * kCols + gv * 8 + i] = bias[i];
     }
     if (!alive && lane == 0) report(a.status, DGS_ETIMEOUT);
-
-    // results to memory
-    const uint32_t row = rank * 128 + quarter * 32 + lane;
-    const uint32_t lane_at = (a.in_out ? o0 : i0) + row, lane_end = a.in_out ? a.outputs : a.inputs;
-    const uint32_t col_at = (a.in_out ? i0 : o0) + group * 128, col_end = min(a.in_out ? a.inputs : a.outputs, (a.in_out ? i0 : o0) + a.n);
-    if (alive && lane_at < lane_end) {
-      float* p = a.dw + (uint64_t(split) * a.experts + expert) * a.inputs * a.outputs + uint64_t(col_at) * lane_end + lane_at;
-#pragma unroll
-      for (uint32_t g = 0; g < 8; ++g) {
-        if (a.add_w) {
-          float old[16];
-#pragma unroll
-          for (uint32_t i = 0; i < 16; ++i) old[i] = col_at + g * 16 + i < col_end ? p[uint64_t(g * 16 + i) * lane_end] : 0.0f;
-#pragma unroll
-          for (uint32_t i = 0; i < 16; ++i) acc[g * 16 + i] += old[i];
-        }
-#pragma unroll
-        for (uint32_t i = 0; i < 16; ++i)
-          if (col_at + g * 16 + i < col_end) p[uint64_t(g * 16 + i) * lane_end] = acc[g * 16 + i];
-      }
-    }
   }
+  __syncwarp();
   tmem_before();
   __syncthreads();
-  if (bias_here && tid < grad_cols && go + tid < a.outputs) {
-    float v = 0.0f;
-    for (uint32_t i = 0; i < SUMS; ++i) v += s_bias[i * kCols + tid];
-    float* p = a.db + (uint64_t(split * a.bias_tiles + ct) * a.experts + expert) * a.outputs + go + tid;
-    *p = a.add_b ? *p + v : v;
-  }
   pair_sync();
   if (warp == 8) {
     __syncwarp();
@@ -699,9 +606,9 @@ __global__ void __launch_bounds__(256) k_weight_sum(float* dw, float* db, const 
 
 // ---- host side --------------------------------------------------------------------------------
 struct WeightPlan {
-  uint32_t code_tiles, grad_tiles, n, splits, bias_tiles, experts;
-  uint32_t step_rows;
-  uint64_t nw, nb, decoded, bytes;
+  uint32_t parts, code_tiles, grad_tiles, n, splits, bias_tiles, experts, step_rows, stride;
+  bool direct;                       // the gradient is read as it is
+  uint64_t nw, nb, plane_rows, decoded, planes, bytes;
 };
 
 bool lists_ok(const dgs_row_lists* l) {
@@ -713,21 +620,23 @@ uint32_t ceil_div(uint64_t a, uint64_t b) { return uint32_t((a + b - 1) / b); }
 int plan_weight(const dgs_checkpoint* c, const dgs_matrix* dy, const dgs_row_lists* lists, uint32_t flags, WeightPlan* p) {
   if (!checkpoint_ok(c) || !matrix_ok(dy, false) || !lists_ok(lists) || (lists ? c->rows == 0 && dy->rows : dy->rows != c->rows))
     return DGS_EINVAL;
-  const uint32_t parts = dy->type == DGS_TYPE_BF16 ? 1 : dy->type == DGS_TYPE_FP16 ? 2 : 3;
+  p->parts = dy->type == DGS_TYPE_BF16 ? 1 : dy->type == DGS_TYPE_FP16 ? 2 : 3;
+  p->step_rows = p->parts == 1 ? Shape<1>::kRows : Shape<3>::kRows;
+  static_assert(Shape<2>::kRows == Shape<3>::kRows, "");
   const bool in_out = flags & DGS_WEIGHT_IN_OUT;
   p->experts = lists ? lists->experts : 1;
-  if (uint64_t(c->cols) * dy->cols > kMostElements / p->experts || dy->rows >= (1u << 31) - 1025 * 128) return DGS_ELIMIT;
+  // rows and columns are 31-bit coordinates of TMA copies, with all parts' rows in one
+  if (uint64_t(c->cols) * dy->cols > kMostElements / p->experts || dy->rows >= (1u << 31) / p->parts - 1026 * 128 || dy->cols > (1u << 30)) return DGS_ELIMIT;
   p->nw = uint64_t(c->cols) * dy->cols * p->experts;
   p->nb = uint64_t(dy->cols) * p->experts;
-  // The tile's width and the split of a tile's rows among pairs: whatever ends soonest.  74 pairs run at a time; a round takes the steps of a pair
-  // and about 4 us around them, and partial results cost their way through the second cache and another launch.
-  const uint32_t steps = std::max(1u, ceil_div(dy->rows / p->experts, 64));   // of 64 rows, whatever the kernel's are
-  p->step_rows = dy->type == DGS_TYPE_BF16 ? Grad<__nv_bfloat16>::kRows : Grad<float>::kRows;
-  static_assert(Grad<__half>::kRows == Grad<float>::kRows, "");
+  // The tile's width and the split of a tile's rows among pairs: whatever ends soonest.  74 pairs run at a time; 64 rows take 0.3 us and 0.1 by the
+  // width, a tile about 4 us besides, and partial results cost their way through the second cache and another launch.  (8192 x 768 x 2304: 54
+  // tiles of 128 columns 57 us, 27 of 256 in two runs of rows each 37.)
+  const uint32_t steps = std::max(1u, ceil_div(dy->rows / p->experts, 64));
   double best = 1e300;
   for (uint32_t n = 256; n >= 64; n -= 64) {
     const uint64_t tiles = uint64_t(ceil_div(in_out ? c->cols : dy->cols, n)) * ceil_div(in_out ? dy->cols : c->cols, 256) * p->experts;
-    const double step_us = parts * (0.10 + 0.28 * n / 256);
+    const double step_us = p->parts * (0.30 + 0.10 * n / 256);
     for (uint32_t s = 1; s <= 32 && s <= steps; ++s) {
       const double us = double(ceil_div(tiles * s, kSms / 2)) * (ceil_div(steps, s) * step_us + 4.0) + (s > 1 ? 3.0 + double(p->nw) * 4e-6 * (s + 1) / 2.5 : 0.0);
       if (us < best) best = us, p->splits = s, p->n = n;
@@ -739,8 +648,12 @@ int plan_weight(const dgs_checkpoint* c, const dgs_matrix* dy, const dgs_row_lis
   // few steps: the bias costs less in one CTA than another launch does
   p->bias_tiles = p->splits > 1 || steps > 8 ? p->code_tiles : 1;
   const uint32_t parts_b = p->splits * p->bias_tiles;
+  p->direct = p->parts == 1 && aligned(dy->data, 16) && dy->stride % 8 == 0 && dy->stride >= dy->cols;
+  p->stride = (dy->cols + 7) / 8 * 8;
+  p->plane_rows = p->direct ? dy->rows : (dy->rows + p->step_rows - 1) / p->step_rows * p->step_rows + p->step_rows;   // a step may begin on the last row
+  p->planes = p->direct ? 0 : p->parts * p->plane_rows * p->stride * 2;
   p->decoded = dy->rows ? decoded_rows(dy->rows, lists ? p->experts : 0, p->step_rows) * held_width(c->cols) * 2 : 0;
-  p->bytes = p->decoded + (p->splits > 1 ? p->nw * p->splits * 4 : 0) + (parts_b > 1 ? p->nb * parts_b * 4 : 0);
+  p->bytes = p->decoded + p->planes + (p->splits > 1 ? p->nw * p->splits * 4 : 0) + (parts_b > 1 ? p->nb * parts_b * 4 : 0);
   return DGS_OK;
 }
 
@@ -748,20 +661,19 @@ constexpr int kMaxDevices = 64;
 std::mutex g_weight_mu;
 bool g_weight_ready[kMaxDevices];
 PFN_cuTensorMapEncodeTiled_v12000 g_encode;   // written once, under the mutex
-template <class T, bool TMA>
+template <uint32_t P>
 bool weight_setup() {
   cudaFuncAttributes f;
   // the split of the registers counts on what the launch brings
-  return cudaFuncGetAttributes(&f, k_weight_grad<T, TMA>) == cudaSuccess && uint32_t(f.numRegs) >= kRegsLaunch &&
-         cudaFuncSetAttribute(k_weight_grad<T, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<T>::kSmem) == cudaSuccess;
+  return cudaFuncGetAttributes(&f, k_weight_grad<P>) == cudaSuccess && uint32_t(f.numRegs) >= kRegsLaunch &&
+         cudaFuncSetAttribute(k_weight_grad<P>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<P>::kSmem) == cudaSuccess;
 }
 int weight_ready() {   // once per device
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return DGS_ECUDA;
   std::lock_guard<std::mutex> lock(g_weight_mu);
   if (!g_weight_ready[dev]) {
-    if (!weight_setup<float, false>() || !weight_setup<__half, false>() || !weight_setup<__nv_bfloat16, false>() || !weight_setup<__nv_bfloat16, true>())
-      return DGS_ECUDA;
+    if (!weight_setup<1>() || !weight_setup<2>() || !weight_setup<3>()) return DGS_ECUDA;
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult found;
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess || !fn) return DGS_ECUDA;
@@ -771,22 +683,18 @@ int weight_ready() {   // once per device
   return DGS_OK;
 }
 
-// A TMA copy takes blocks of 64 columns of bfloat16 numbers from rows that begin on 16 bytes.
-bool tma_fits(const dgs_matrix* dy) {
-  return dy->type == DGS_TYPE_BF16 && aligned(dy->data, 16) && dy->stride % 8 == 0 && dy->stride >= dy->cols && dy->cols < (1u << 31);
-}
-int make_map(void* data, uint64_t rows, uint64_t cols, uint64_t stride, uint32_t box_rows, CUtensorMap* map) {
+int make_map(const void* data, uint64_t rows, uint64_t cols, uint64_t stride, uint32_t box_rows, CUtensorMap* map) {
   const cuuint64_t dims[2] = {cols, rows}, strides[1] = {stride * 2};
   const cuuint32_t box[2] = {64, box_rows}, each[2] = {1, 1};
-  return g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, data, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+  return g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(data), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? DGS_OK
              : DGS_ECUDA;
 }
 
-template <class T, bool TMA>
-int launch(const WeightArgs& a, const CUtensorMap& held, const CUtensorMap& grad, uint32_t ctas, cudaStream_t st) {
-  k_weight_grad<T, TMA><<<ctas, kThreads, Shape<T>::kSmem, st>>>(a, held, grad);
+template <uint32_t P>
+int launch(const WeightArgs& a, const CUtensorMap& held, const CUtensorMap& grad, cudaStream_t st) {
+  k_weight_grad<P><<<std::min(a.tiles, kSms / 2) * 2, kThreads, Shape<P>::kSmem, st>>>(a, held, grad);
   return cudaGetLastError() == cudaSuccess ? DGS_OK : DGS_ECUDA;
 }
 
@@ -823,17 +731,20 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
   rc = weight_ready();
   if (rc != DGS_OK) return rc;
   const uint32_t parts_b = p.splits * p.bias_tiles;
+  char* const work = static_cast<char*>(workspace);
   WeightArgs a = {};
   a.h = held_of(ckpt);
-  a.dy = dy->data;
+  a.dy = static_cast<const __nv_bfloat16*>(p.direct ? dy->data : work + p.decoded);
   a.dy_rows = dy->rows;
-  a.dy_stride = dy->stride;
+  a.dy_stride = p.direct ? dy->stride : p.stride;
+  a.plane_rows = p.plane_rows;
   a.inputs = ckpt->cols;
   a.outputs = dy->cols;
   a.code_tiles = p.code_tiles;
   a.grad_tiles = p.grad_tiles;
   a.splits = p.splits;
   a.experts = p.experts;
+  a.tiles = p.code_tiles * p.grad_tiles * p.splits * p.experts;
   a.rows_per = lists ? lists->rows_per : 1;
   a.n = p.n;
   a.in_out = flags & DGS_WEIGHT_IN_OUT ? 1 : 0;
@@ -841,8 +752,8 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
   a.step_rows = p.step_rows;
   a.offsets = lists ? lists->offsets : nullptr;
   a.rows = lists ? lists->rows : nullptr;
-  a.decoded = static_cast<__nv_bfloat16*>(workspace);
-  float* const part_w = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.decoded);
+  a.decoded = reinterpret_cast<__nv_bfloat16*>(work);
+  float* const part_w = reinterpret_cast<float*>(work + p.decoded + p.planes);
   float* const part_b = part_w + (p.splits > 1 ? p.nw * p.splits : 0);
   a.dw = p.splits > 1 ? part_w : dw;
   a.db = !db ? nullptr : parts_b > 1 ? part_b : db;
@@ -853,11 +764,10 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
   if (!a.status) return DGS_ECUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   CUtensorMap held = {}, grad = {};
-  const bool tma = dy->rows && tma_fits(dy);
   if (dy->rows) {
     const uint64_t rows = p.decoded / (2 * uint64_t(a.h.width));
     rc = make_map(a.decoded, rows, a.h.width, a.h.width, p.step_rows, &held);
-    if (rc == DGS_OK && tma) rc = make_map(dy->data, dy->rows, dy->cols, dy->stride, p.step_rows, &grad);
+    if (rc == DGS_OK) rc = make_map(a.dy, p.parts * p.plane_rows, dy->cols, a.dy_stride, p.step_rows, &grad);
     if (rc != DGS_OK) return rc;
     const uint32_t ctas = ceil_div(rows, kDecodeRows);
     if (ckpt->format == DGS_FORMAT_E4M3)
@@ -865,14 +775,18 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
     else
       k_weight_decode<false><<<ctas, 256, 0, st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return DGS_ECUDA;
+    if (!p.direct) {
+      const uint32_t across = ceil_div(p.stride, 2048);
+      const dim3 grid(across, uint32_t(std::min<uint64_t>(p.plane_rows, std::max(1u, kSms * 16 / across))));
+      rc = with_type(dy->type, [&](auto* t) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        k_weight_parts<T><<<grid, 256, 0, st>>>(static_cast<const T*>(dy->data), dy->rows, dy->cols, dy->stride, const_cast<__nv_bfloat16*>(a.dy), p.stride, p.plane_rows);
+        return cudaGetLastError() == cudaSuccess ? int(DGS_OK) : int(DGS_ECUDA);
+      });
+      if (rc != DGS_OK) return rc;
+    }
   }
-  const uint32_t ctas = p.code_tiles * p.grad_tiles * p.splits * p.experts * 2;
-  rc = with_type(dy->type, [&](auto* t) {
-    using T = std::remove_pointer_t<decltype(t)>;
-    if constexpr (std::is_same_v<T, __nv_bfloat16>)
-      if (tma) return launch<T, true>(a, held, grad, ctas, st);
-    return launch<T, false>(a, held, grad, ctas, st);
-  });
+  rc = p.parts == 1 ? launch<1>(a, held, grad, st) : p.parts == 2 ? launch<2>(a, held, grad, st) : launch<3>(a, held, grad, st);
   const uint64_t nw = p.splits > 1 ? p.nw : 0, nb = db && parts_b > 1 ? p.nb : 0;
   if (rc != DGS_OK || nw + nb == 0) return rc;
   k_weight_sum<<<uint32_t(std::min<uint64_t>((nw + nb + 255) / 256, kSms * 8)), 256, 0, st>>>(dw, db, part_w, part_b, nw, nb, p.splits, parts_b, add);

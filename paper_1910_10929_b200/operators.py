@@ -8,6 +8,7 @@ is enqueued, what the library refuses raises DgsError.
 """
 from __future__ import annotations
 
+import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -29,6 +30,9 @@ def _pick(table, key, what):
         raise ValueError(f"{what} is one of {sorted(map(str, table))}: got {key!r}") from None
 
 
+_device_now, _stream_now = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream   # what torch.cuda's own calls end in
+
+
 def _on_gpu(t, what):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{what} must be a CUDA tensor: this library has no CPU path")
@@ -37,18 +41,23 @@ def _on_gpu(t, what):
 def _matrix(t: torch.Tensor, what: str) -> "dgs.dgs_matrix":
     """The last dimension as columns, all others as rows that lie evenly spaced."""
     _on_gpu(t, what)
-    if t.dtype not in _TYPE:
+    kind = _TYPE.get(t.dtype)
+    if kind is None:
         raise ValueError(f"{what} must be float32, bfloat16 or float16: got {t.dtype}")
-    if t.dim() < 1:
-        raise ValueError(f"{what} needs a last dimension")
-    cols = t.shape[-1]
-    if t.dim() != 2:
-        if t.dim() > 2 and not t.is_contiguous():
+    shape = t.shape
+    if len(shape) == 2:
+        rows, cols = shape
+        stride, step = t.stride()
+    else:
+        if not shape:
+            raise ValueError(f"{what} needs a last dimension")
+        if len(shape) > 2 and not t.is_contiguous():
             raise ValueError(f"{what} has more than two dimensions and is not contiguous")
-        t = t.view(t.numel() // cols if cols else 0, cols)
-    if cols > 1 and t.shape[0] and t.stride(1) != 1:
-        raise ValueError(f"{what}: neighbours in the last dimension must be neighbours in memory (stride {t.stride(1)})")
-    return dgs.dgs_matrix(t.data_ptr(), t.shape[0], t.stride(0) if t.shape[0] > 1 else cols, cols, _TYPE[t.dtype])
+        cols = shape[-1]
+        rows, stride, step = t.numel() // cols if cols else 0, cols, t.stride(-1)
+    if step != 1 and cols > 1 and rows:
+        raise ValueError(f"{what}: neighbours in the last dimension must be neighbours in memory (stride {step})")
+    return dgs.dgs_matrix(t.data_ptr(), rows, stride if rows > 1 else cols, cols, kind)
 
 
 def _plain(t: Optional[torch.Tensor], what: str, dtype: torch.dtype, numel: int, device) -> int:
@@ -67,15 +76,21 @@ def _same_device(device, *tensors) -> None:
             raise ValueError(f"tensors of one call must be on one device: {device} and {t.device}")
 
 
-def _stream(device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+def _enqueue(device, call, *args) -> None:
+    """call(*args, stream) with the device current and its current stream."""
+    index = device.index
+    if index == _device_now():
+        call(*args, _stream_now(index))
+    else:
+        with torch.cuda.device(device):
+            call(*args, _stream_now(index))
 
 
 def operator_status(device=None) -> int:
     """Waits for the device's current stream; the lowest status (0, DGS_EINVAL, DGS_ETIMEOUT) that kernels of these
     operators have left on the device since the last call."""
     with torch.cuda.device(device):
-        return dgs.dgs_operator_status(_stream(device))
+        return dgs.dgs_operator_status(_stream_now(_device_now()))
 
 
 class Checkpoint:
@@ -86,12 +101,14 @@ class Checkpoint:
         code = _pick(_FORMAT, format, "format")
         if self.rows < 0 or self.cols < 1:
             raise ValueError(f"a checkpoint has rows >= 0 and cols >= 1: got {rows} x {cols}")
-        size = dgs.dgs_checkpoint_bytes(self.rows, self.cols)
+        size = self.rows * (-(-self.cols // 32) * 32 + -(-self.cols // 128) * 4)
+        if self.rows >= 1 << 32 or self.cols > 1 << 30 or self.rows * self.cols > 1 << 40:
+            size = dgs.dgs_checkpoint_bytes(self.rows, self.cols)   # raises what the library says
         if data is None:
             data = torch.empty(size, dtype=torch.uint8, device="cuda" if device is None else device)
-        _on_gpu(data, "data")
-        if device is not None and data.device != torch.empty(0, device=device).device:
+        elif device is not None and torch.device(device) not in (data.device, torch.device(data.device.type)):
             raise ValueError(f"data is on {data.device}, not on {device}")
+        _on_gpu(data, "data")
         self.device = data.device
         self._held = dgs.dgs_checkpoint(_plain(data, "data", torch.uint8, size, data.device), self.rows, self.cols, code)
         self.data = data
@@ -114,8 +131,7 @@ class Checkpoint:
         my = None
         if out is not None:
             my = self._fit(out, "out")
-        with torch.cuda.device(self.device):
-            dgs.dgs_checkpoint_save(self._held, mx, act, my, _stream(self.device))
+        _enqueue(self.device, dgs.dgs_checkpoint_save, self._held, mx, act, my)
         return out
 
     def load(self, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -123,8 +139,7 @@ class Checkpoint:
         if out is None:
             out = torch.empty(self.rows, self.cols, dtype=dtype, device=self.device)
         m = self._fit(out, "out")
-        with torch.cuda.device(self.device):
-            dgs.dgs_checkpoint_load(self._held, m, _stream(self.device))
+        _enqueue(self.device, dgs.dgs_checkpoint_load, self._held, m)
         return out
 
     def activation_grad(self, dy: torch.Tensor, activation: str, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -134,8 +149,7 @@ class Checkpoint:
         if out is None:
             out = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
         mx = self._fit(out, "out")
-        with torch.cuda.device(self.device):
-            dgs.dgs_checkpoint_activation_grad(self._held, act, my, mx, _stream(self.device))
+        _enqueue(self.device, dgs.dgs_checkpoint_activation_grad, self._held, act, my, mx)
         return out
 
     def weight_grad(self, dy: torch.Tensor, dw: torch.Tensor, db: Optional[torch.Tensor] = None, *, layout: str = "out_in",
@@ -161,10 +175,9 @@ class Checkpoint:
             raise ValueError(f"dy must have {self.rows} rows: got {m.rows}")
         pw = _plain(dw, "dw", torch.float32, experts * self.cols * m.cols, self.device)
         pb = _plain(db, "db", torch.float32, experts * m.cols, self.device)
-        with torch.cuda.device(self.device):
-            need = dgs.dgs_checkpoint_weight_grad_bytes(self._held, m, lists, flags)
-            work = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-            dgs.dgs_checkpoint_weight_grad(self._held, m, lists, pw, pb, flags, work.data_ptr() if need else 0, need, _stream(self.device))
+        need = dgs.dgs_checkpoint_weight_grad_bytes(self._held, m, lists, flags)
+        work = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        _enqueue(self.device, dgs.dgs_checkpoint_weight_grad, self._held, m, lists, pw, pb, flags, work.data_ptr() if need else 0, need)
 
 
 class Route(NamedTuple):
@@ -176,6 +189,7 @@ class Route(NamedTuple):
     place: torch.Tensor     # [tokens, k]: where in order a slot stands
 
 
+@functools.lru_cache(maxsize=64)
 def _router(k, score, groups, groups_kept, group_best, renormalise, scale) -> "dgs.dgs_router":
     for v, what in ((k, "k"), (groups, "groups"), (groups_kept, "groups_kept"), (group_best, "group_best")):
         if int(v) != v or not 0 < v < 1 << 31:
@@ -191,15 +205,15 @@ def route_experts(logits: torch.Tensor, k: int, *, score: str = "softmax", bias:
     router = _router(k, score, groups, groups_kept, group_best, renormalise, scale)
     tokens, experts, device = m.rows, m.cols, logits.device
     pb = _plain(bias, "bias", torch.float32, experts, device)
-    with torch.cuda.device(device):
-        need = dgs.dgs_route_experts_bytes(router, tokens, experts)
-        slots = tokens * router.k
-        whole = torch.empty(3 * slots + experts + 1, dtype=torch.int32, device=device)
-        expert, order, place, offsets = whole.split([slots, slots, slots, experts + 1])
-        weight = torch.empty(tokens, router.k, dtype=torch.float32, device=device)
-        work = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
-        dgs.dgs_route_experts(router, m, pb, expert.data_ptr(), weight.data_ptr(), offsets.data_ptr(), order.data_ptr(), place.data_ptr(),
-                              work.data_ptr(), need, _stream(device))
+    need = dgs.dgs_route_experts_bytes(router, tokens, experts)
+    slots = tokens * router.k
+    # one piece of memory for the outputs of four bytes and the workspace, which begins on a multiple of 16
+    whole = torch.empty(-(-(3 * slots + experts + 1) // 4) * 4 + need // 4, dtype=torch.int32, device=device)
+    expert, order, place, offsets, _ = whole.split([slots, slots, slots, experts + 1, whole.numel() - 3 * slots - experts - 1])
+    weight = torch.empty(tokens, router.k, dtype=torch.float32, device=device)
+    at = whole.data_ptr()
+    _enqueue(device, dgs.dgs_route_experts, router, m, pb, at, weight.data_ptr(), at + 12 * slots, at + 4 * slots, at + 8 * slots,
+             at + 4 * (whole.numel() - need // 4) if need else 0, need)
     return Route(expert.view(tokens, router.k), weight, offsets, order, place.view(tokens, router.k))
 
 
@@ -217,6 +231,5 @@ def route_experts_grad(logits: torch.Tensor, expert: torch.Tensor, dweight: torc
         out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     mo = _matrix(out, "out")
     _same_device(logits.device, out)
-    with torch.cuda.device(logits.device):
-        dgs.dgs_route_experts_grad(router, m, pe, pw, mo, _stream(logits.device))
+    _enqueue(logits.device, dgs.dgs_route_experts_grad, router, m, pe, pw, mo)
     return out
