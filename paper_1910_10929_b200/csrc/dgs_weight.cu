@@ -135,6 +135,7 @@ struct WeightArgs {
   uint32_t in_out, bias_tiles, step_rows, tiles;
   const uint32_t* offsets;
   const uint32_t* rows;
+  uint32_t* order;          // experts by their number of rows, the longest first
   __nv_bfloat16* decoded;   // [rows][h.width]: the checkpoint's values in dy's order, an expert's from expert_at(...) on
   float* dw;          // or the splits' partial results, [splits][experts][inputs * outputs]
   float* db;          // likewise, [splits * bias_tiles][experts][outputs]; NULL: not wanted
@@ -168,6 +169,20 @@ template <bool FLOAT8>
 __global__ void __launch_bounds__(256) k_weight_decode(const __grid_constant__ WeightArgs a) {
   const uint64_t at = uint64_t(blockIdx.x) * kDecodeRows;   // row of the decoded values
   uint64_t first = 0, last = a.dy_rows, begin = 0;
+  if (a.offsets && blockIdx.x == gridDim.x - 1) {   // one CTA more: who comes before whom
+    __shared__ uint32_t s_rows[DGS_ROUTE_MAX_EXPERTS];
+    for (uint32_t e = threadIdx.x; e < a.experts; e += 256) {
+      expert_rows(a, e, &first, &last, true);
+      s_rows[e] = uint32_t(last - first);
+    }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < a.experts; e += 256) {
+      uint32_t rank = 0;
+      for (uint32_t o = 0; o < a.experts; ++o) rank += s_rows[o] > s_rows[e] || (s_rows[o] == s_rows[e] && o < e);
+      a.order[rank] = e;
+    }
+    return;
+  }
   if (a.offsets) {
     // the last expert that begins at or before this row: as many as do, since each begins behind the one before
     __shared__ uint32_t s_begun;
@@ -176,7 +191,7 @@ __global__ void __launch_bounds__(256) k_weight_decode(const __grid_constant__ W
     uint32_t begun = 0;
     for (uint32_t e = threadIdx.x; e < a.experts; e += 256) {
       uint64_t f, l;
-      expert_rows(a, e, &f, &l, blockIdx.x == 0);
+      expert_rows(a, e, &f, &l, false);
       begun += expert_at(f, e, a.step_rows) <= at;
     }
     if (begun) atomicAdd(&s_begun, begun);
@@ -188,34 +203,43 @@ __global__ void __launch_bounds__(256) k_weight_decode(const __grid_constant__ W
   // rows behind the expert's last are zero up to the end of its last step
   const uint64_t row0 = at - begin, rows = last - first;
   if (row0 >= (rows + a.step_rows - 1) / a.step_rows * a.step_rows) return;
-  const uint32_t units = a.h.width / 8;
-#pragma unroll 4
-  for (uint32_t i = threadIdx.x; i < kDecodeRows * units; i += 256) {
-    const uint32_t r = i / units, unit = i - r * units;
-    uint4 out = make_uint4(0, 0, 0, 0);
-    if (row0 + r < rows) {
-      uint64_t src = first + row0 + r;
-      if (a.offsets) {
+  const uint32_t units = a.h.width / 8, total = kDecodeRows * units;
+  for (uint32_t i0 = threadIdx.x; i0 < total; i0 += 4 * 256) {
+    uint2 w[4];
+    uint32_t scale[4], row[4], unit[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {   // four units on their way together
+      const uint32_t i = min(i0 + k * 256, total - 1);
+      row[k] = i / units;
+      unit[k] = i - row[k] * units;
+      uint64_t src = first + row0 + row[k];
+      bool there = row0 + row[k] < rows;
+      if (a.offsets && there) {
         if (a.rows) {
           const uint32_t v = a.rows[src];
           src = a.rows_per == 1 ? v : v / a.rows_per;
         }
         if (src >= a.h.rows) {
           report(a.status, DGS_EINVAL);
-          src = ~0ull;
+          there = false;
         }
       }
-      if (src != ~0ull) {
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(a.h.codes + src * a.h.width + unit * 8));
-        const float down = scale_down(__ldg(a.h.scales + src * a.h.spitch + unit / 4));
-        float2 v[4];
-        decode8<FLOAT8>(w, down, v);
-        Eight<__nv_bfloat16> e;
-        of_floats(v, e);
-        out = make_uint4(e.w[0], e.w[1], e.w[2], e.w[3]);
+      w[k] = make_uint2(0, 0);
+      scale[k] = 0;
+      if (there) {
+        w[k] = __ldg(reinterpret_cast<const uint2*>(a.h.codes + src * a.h.width + unit[k] * 8));
+        scale[k] = __ldg(a.h.scales + src * a.h.spitch + unit[k] / 4);
       }
     }
-    *reinterpret_cast<uint4*>(a.decoded + (at + r) * a.h.width + unit * 8) = out;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (i0 + k * 256 >= total) break;
+      float2 v[4];
+      decode8<FLOAT8>(w[k], scale_down(scale[k]), v);   // rows that are not there: codes and scale of zero
+      Eight<__nv_bfloat16> e;
+      of_floats(v, e);
+      *reinterpret_cast<uint4*>(a.decoded + (at + row[k]) * a.h.width + unit[k] * 8) = make_uint4(e.w[0], e.w[1], e.w[2], e.w[3]);
+    }
   }
 }
 
@@ -311,7 +335,7 @@ __device__ __forceinline__ void bias_add(const uint4& w, float (&bias)[8]) {   /
 // coalesced wherever the layer's slice begins: inputs for [outputs][inputs], outputs for [inputs][outputs]; only the operands' roles change.
 //
 // Warps: 0 to 7 keep the sums; 8 issues products, 9 TMA copies, 10 passes on that copies have landed, and 10 and 11 sum the bias from them.  The gradients of an
-// expert's last rows, where the next expert's would come along with a copy, are brought by warps 0 to 3, with zeros behind them.
+// expert's last rows, where the next expert's would come along with a copy, are brought by warps 0 to 7, with zeros behind them.
 // Sums: the tensor cores add to their accumulator with bits cut off, which over 8192 rows leaves an error of 5.5e-6; so every kChunk steps the
 // accumulators go to registers of the eight warps and are added up there with rounding (2.1e-7), while the products go on in the other half of
 // tensor memory.  Each step's part of db is summed by one of the CTAs that hold the same gradients.
@@ -324,6 +348,11 @@ struct TileOf {
   uint32_t count, steps, tma_steps;
   bool bias;
 };
+// The tiles of a pair of CTAs: to and fro over the pairs, so that with the experts in the order of their rows all pairs get about as much
+// (16 experts of 55 to 8761 rows: 111 to 126 steps for the longest pair, 166 to 178 in the experts' own order, 101 the mean).
+__device__ __forceinline__ uint32_t tile_in_round(uint32_t round, uint32_t pair, uint32_t pairs) {
+  return round * pairs + (round & 1 ? pairs - 1 - pair : pair);
+}
 template <uint32_t R>
 __device__ __forceinline__ TileOf tile_of(const WeightArgs& a, uint32_t tile, uint32_t rank) {
   TileOf t;
@@ -333,6 +362,7 @@ __device__ __forceinline__ TileOf tile_of(const WeightArgs& a, uint32_t tile, ui
   tile /= a.grad_tiles;
   t.split = tile % a.splits;
   t.expert = tile / a.splits;
+  if (a.order) t.expert = a.order[t.expert];
   t.i0 = t.ct * (a.in_out ? a.n : 256);
   t.o0 = gt * (a.in_out ? 256 : a.n);
   t.ci = t.i0 + rank * (a.in_out ? a.n / 2 : kCols);
@@ -360,8 +390,8 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
   extern __shared__ unsigned char raw[];
   __shared__ __align__(8) uint64_t s_full[ST], s_empty[ST], s_loaded[ST], s_sum_full[2], s_sum_empty[2], s_tail, s_bias_done, s_done;
   __shared__ uint32_t s_tmem;
-  __shared__ float s_bias[12 * kCols];   // rows 0 to 3: sums of the steps that came by TMA, 4 to 11: of the last step
-  const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = cta_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+  __shared__ float s_bias[20 * kCols];   // rows 0 to 3: sums of the steps that came by TMA, 4 to 19: of the last step
+  const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = cta_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2, rounds = (a.tiles + pairs - 1) / pairs;
   const uint32_t tiles = (smem_at(raw) + 1023u) & ~1023u;
   const uint32_t code_cols = a.in_out ? a.n / 2 : kCols, grad_cols = a.in_out ? kCols : a.n / 2;
 
@@ -377,7 +407,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
         bar_init(smem_at(&s_sum_full[i]), 1);
         bar_init(smem_at(&s_sum_empty[i]), 16);
       }
-      bar_init(smem_at(&s_tail), 4);
+      bar_init(smem_at(&s_tail), 8);
       bar_init(smem_at(&s_bias_done), 1);
       bar_init(smem_at(&s_done), 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -397,7 +427,9 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
     if (warp == 8 && lane == 0 && rank == 0) {
       bool alive = true;
       uint32_t it = 0, chunk = 0;
-      for (uint32_t tile = pair; tile < a.tiles && alive; tile += pairs) {
+      for (uint32_t round = 0; round < rounds && alive; ++round) {
+        const uint32_t tile = tile_in_round(round, pair, pairs);
+        if (tile >= a.tiles) break;   // in the last round only
         const TileOf w = tile_of<R>(a, tile, rank);
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           const uint32_t st = it % ST, code = tiles + st * STAGE, grad = code + TILE, acc = tmem + (chunk & 1) * 256;
@@ -427,7 +459,9 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
       const uint32_t code_blocks = (code_cols + 63) / 64, grad_blocks = (grad_cols + 63) / 64;
       bool alive = true;
       uint32_t it = 0;
-      for (uint32_t tile = pair; tile < a.tiles && alive; tile += pairs) {
+      for (uint32_t round = 0; round < rounds && alive; ++round) {
+        const uint32_t tile = tile_in_round(round, pair, pairs);
+        if (tile >= a.tiles) break;   // in the last round only
         const TileOf w = tile_of<R>(a, tile, rank);
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           const uint32_t st = it % ST, to = tiles + st * STAGE, bar = smem_at(&s_loaded[st]), grads = s < w.tma_steps ? grad_blocks : 0;
@@ -450,7 +484,9 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
       const uint32_t t = tid - 320, br = t / 16, bv = t % 16;
       bool alive = true;
       uint32_t it = 0, tails = 0;
-      for (uint32_t tile = pair; tile < a.tiles && alive; tile += pairs) {
+      for (uint32_t round = 0; round < rounds && alive; ++round) {
+        const uint32_t tile = tile_in_round(round, pair, pairs);
+        if (tile >= a.tiles) break;   // in the last round only
         const TileOf w = tile_of<R>(a, tile, rank);
         float bias[8];
 #pragma unroll
@@ -479,7 +515,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
 #pragma unroll
           for (int i = 0; i < 8; ++i) s_bias[br * kCols + bv * 8 + i] = bias[i];
           asm volatile("bar.sync 1, 64;" ::: "memory");
-          const uint32_t rows = w.tma_steps < w.steps && (w.steps - 1) % a.bias_tiles == w.ct ? 12 : 4;
+          const uint32_t rows = w.tma_steps < w.steps && (w.steps - 1) % a.bias_tiles == w.ct ? 20 : 4;
           for (uint32_t c = t; c < grad_cols && w.go + c < a.outputs; c += 64) {
             float v = 0.0f;
             for (uint32_t i = 0; i < rows; ++i) v += s_bias[i * kCols + c];
@@ -496,41 +532,52 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSum));
     const uint32_t quarter = warp % 4, group = warp / 4;
     bool alive = true;
-    uint32_t it = 0, drained = 0, ordinal = 0;
-    for (uint32_t tile = pair; tile < a.tiles && alive; tile += pairs, ++ordinal) {
+    uint32_t it = 0, drained = 0;
+    for (uint32_t ordinal = 0; ordinal < rounds && alive; ++ordinal) {
+      const uint32_t tile = tile_in_round(ordinal, pair, pairs);
+      if (tile >= a.tiles) break;
       const TileOf w = tile_of<R>(a, tile, rank);
       const uint32_t chunks = (w.steps + CH - 1) / CH;
       float acc[128];
 #pragma unroll
       for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
       for (uint32_t c = 0; c < chunks; ++c, ++drained) {
-        if (c + 1 == chunks && w.tma_steps < w.steps && group == 0) {
-          // an expert's last rows: eight columns of every eighth row a thread, zeros behind them
+        if (c + 1 == chunks && w.tma_steps < w.steps) {
+          // an expert's last rows: eight columns of every sixteenth row a thread, zeros behind them.  What is read is on its way before the stage is
+          // free; sixteen rows that no product takes are left out.
           const uint32_t last = it + w.steps - 1, at = tiles + last % ST * STAGE + TILE, gr = tid / 16, gv = tid % 16, col = w.go + gv * 8;
-          if (last >= ST && !(alive = warp_wait(smem_at(&s_empty[last % ST]), (last / ST - 1) & 1))) break;
-          if (ordinal && !(alive = warp_wait(smem_at(&s_bias_done), (ordinal - 1) & 1))) break;   // the table is free
-          float bias[8] = {};
-#pragma unroll 2
-          for (uint32_t r = gr; r < R; r += 8) {
-            const uint32_t j = (w.steps - 1) * R + r;
+          const uint32_t j0 = (w.steps - 1) * R + gr;
+          uint4 v[P][R / 16];
 #pragma unroll
-            for (uint32_t p = 0; p < P; ++p) {
-              uint4 v = make_uint4(0, 0, 0, 0);
-              if (j < w.count && col < a.outputs) {
-                const __nv_bfloat16* from = a.dy + (p * a.plane_rows + w.first + j) * a.dy_stride + col;
+          for (uint32_t p = 0; p < P; ++p) {
+            const __nv_bfloat16* from = a.dy + (p * a.plane_rows + w.first + j0) * a.dy_stride + col;
+#pragma unroll
+            for (uint32_t u = 0; u < R / 16; ++u, from += 16 * a.dy_stride) {
+              v[p][u] = make_uint4(0, 0, 0, 0);
+              if (j0 + 16 * u < w.count && col < a.outputs) {
                 if (col + 8 <= a.outputs) {
-                  v = __ldg(reinterpret_cast<const uint4*>(from));
+                  v[p][u] = __ldg(reinterpret_cast<const uint4*>(from));
                 } else {
                   uint32_t e[8];
 #pragma unroll
                   for (uint32_t i = 0; i < 8; ++i) e[i] = col + i < a.outputs ? __ldg(reinterpret_cast<const unsigned short*>(from) + i) : 0u;
-                  v = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+                  v[p][u] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
                 }
               }
-              bias_add(v, bias);
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + p * TILE + tile_at<P>(r, gv)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
             }
           }
+          if (last >= ST && !(alive = warp_wait(smem_at(&s_empty[last % ST]), (last / ST - 1) & 1))) break;
+          if (ordinal && !(alive = warp_wait(smem_at(&s_bias_done), (ordinal - 1) & 1))) break;   // the table is free
+          float bias[8] = {};
+#pragma unroll
+          for (uint32_t p = 0; p < P; ++p)
+#pragma unroll
+            for (uint32_t u = 0; u < R / 16; ++u)
+              if ((w.steps - 1) * R + 16 * u < w.count) {
+                const uint4 q = v[p][u];
+                bias_add(q, bias);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + p * TILE + tile_at<P>(gr + 16 * u, gv)), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
+              }
 #pragma unroll
           for (int i = 0; i < 8; ++i) s_bias[(4 + gr) * kCols + gv * 8 + i] = bias[i];
           writes_to_async_proxy();
@@ -588,19 +635,26 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
   }
 }
 
-// Adds up partial results in their order: of dw over the splits, of db over the splits and the CTAs that shared its steps.
+// Adds up partial results in their order: of dw over the splits, of db over the splits and the CTAs that shared its steps.  Four results a thread
+// at a time, so that their parts are on their way together.
 __global__ void __launch_bounds__(256) k_weight_sum(float* dw, float* db, const float* pw, const float* pb, uint64_t nw, uint64_t nb, uint32_t parts_w,
                                                     uint32_t parts_b, uint32_t add) {
-  const uint64_t total = nw + nb;
-  for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += uint64_t(gridDim.x) * 256) {
-    const bool w = i < nw;
-    const uint64_t k = w ? i : i - nw, n = w ? nw : nb;
-    const float* p = (w ? pw : pb) + k;
-    float* out = (w ? dw : db) + k;
-    const uint32_t parts = w ? parts_w : parts_b;
-    float v = 0.0f;
-    for (uint32_t s = 0; s < parts; ++s) v += p[s * n];
-    *out = add ? *out + v : v;
+  const bool bias = blockIdx.y != 0;
+  float* out = bias ? db : dw;
+  const float* p = bias ? pb : pw;
+  const uint64_t n = bias ? nb : nw, step = uint64_t(gridDim.x) * 256;
+  const uint32_t parts = bias ? parts_b : parts_w;
+  for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += 4 * step) {
+    float v[4], old[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = 0.0f, old[k] = add && i + k * step < n ? out[i + k * step] : 0.0f;
+    for (uint32_t s = 0; s < parts; ++s)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i + k * step < n) v[k] += p[s * n + i + k * step];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i + k * step < n) out[i + k * step] = old[k] + v[k];
   }
 }
 
@@ -608,7 +662,7 @@ __global__ void __launch_bounds__(256) k_weight_sum(float* dw, float* db, const 
 struct WeightPlan {
   uint32_t parts, code_tiles, grad_tiles, n, splits, bias_tiles, experts, step_rows, stride;
   bool direct;                       // the gradient is read as it is
-  uint64_t nw, nb, plane_rows, decoded, planes, bytes;
+  uint64_t nw, nb, plane_rows, decoded, planes, order, bytes;
 };
 
 bool lists_ok(const dgs_row_lists* l) {
@@ -653,7 +707,8 @@ int plan_weight(const dgs_checkpoint* c, const dgs_matrix* dy, const dgs_row_lis
   p->plane_rows = p->direct ? dy->rows : (dy->rows + p->step_rows - 1) / p->step_rows * p->step_rows + p->step_rows;   // a step may begin on the last row
   p->planes = p->direct ? 0 : p->parts * p->plane_rows * p->stride * 2;
   p->decoded = dy->rows ? decoded_rows(dy->rows, lists ? p->experts : 0, p->step_rows) * held_width(c->cols) * 2 : 0;
-  p->bytes = p->decoded + p->planes + (p->splits > 1 ? p->nw * p->splits * 4 : 0) + (parts_b > 1 ? p->nb * parts_b * 4 : 0);
+  p->order = lists && dy->rows ? (uint64_t(p->experts) * 4 + 15) / 16 * 16 : 0;
+  p->bytes = p->decoded + p->planes + p->order + (p->splits > 1 ? p->nw * p->splits * 4 : 0) + (parts_b > 1 ? p->nb * parts_b * 4 : 0);
   return DGS_OK;
 }
 
@@ -753,7 +808,8 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
   a.offsets = lists ? lists->offsets : nullptr;
   a.rows = lists ? lists->rows : nullptr;
   a.decoded = reinterpret_cast<__nv_bfloat16*>(work);
-  float* const part_w = reinterpret_cast<float*>(work + p.decoded + p.planes);
+  a.order = p.order ? reinterpret_cast<uint32_t*>(work + p.decoded + p.planes) : nullptr;
+  float* const part_w = reinterpret_cast<float*>(work + p.decoded + p.planes + p.order);
   float* const part_b = part_w + (p.splits > 1 ? p.nw * p.splits : 0);
   a.dw = p.splits > 1 ? part_w : dw;
   a.db = !db ? nullptr : parts_b > 1 ? part_b : db;
@@ -769,7 +825,7 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
     rc = make_map(a.decoded, rows, a.h.width, a.h.width, p.step_rows, &held);
     if (rc == DGS_OK) rc = make_map(a.dy, p.parts * p.plane_rows, dy->cols, a.dy_stride, p.step_rows, &grad);
     if (rc != DGS_OK) return rc;
-    const uint32_t ctas = ceil_div(rows, kDecodeRows);
+    const uint32_t ctas = ceil_div(rows, kDecodeRows) + (lists ? 1 : 0);
     if (ckpt->format == DGS_FORMAT_E4M3)
       k_weight_decode<true><<<ctas, 256, 0, st>>>(a);
     else
@@ -789,6 +845,6 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
   rc = p.parts == 1 ? launch<1>(a, held, grad, st) : p.parts == 2 ? launch<2>(a, held, grad, st) : launch<3>(a, held, grad, st);
   const uint64_t nw = p.splits > 1 ? p.nw : 0, nb = db && parts_b > 1 ? p.nb : 0;
   if (rc != DGS_OK || nw + nb == 0) return rc;
-  k_weight_sum<<<uint32_t(std::min<uint64_t>((nw + nb + 255) / 256, kSms * 8)), 256, 0, st>>>(dw, db, part_w, part_b, nw, nb, p.splits, parts_b, add);
+  k_weight_sum<<<dim3(uint32_t(std::min<uint64_t>((std::max(nw, nb) + 1023) / 1024, kSms * 8)), nb ? 2 : 1), 256, 0, st>>>(dw, db, part_w, part_b, nw, nb, p.splits, parts_b, add);
   return cudaGetLastError() == cudaSuccess ? DGS_OK : DGS_ECUDA;
 }
