@@ -260,6 +260,27 @@ __device__ __forceinline__ uint32_t largest_half(const Eight<T>& e) {
 __device__ __forceinline__ uint32_t largest_bits(const Eight<__nv_bfloat16>& e) { return largest_half(e) << 16; }
 __device__ __forceinline__ uint32_t largest_bits(const Eight<__half>& e) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)largest_half(e)))); }
 
+// Kernels of one call follow one another with their beginnings overlapped (programmatic launches).  wait_for_last_kernel: what the kernel ahead wrote is
+// there, and all before it; let_next_kernel_begin: the next may be brought onto the SMs.
+__device__ __forceinline__ void wait_for_last_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_kernel_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+struct EarlyLaunch {
+  cudaLaunchAttribute early;
+  cudaLaunchConfig_t cfg;
+  EarlyLaunch(dim3 grid, uint32_t threads, uint32_t smem, cudaStream_t st) {
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+  }
+  EarlyLaunch(const EarlyLaunch&) = delete;
+};
+
 __device__ __forceinline__ void report(int* status, int code) { atomicMin(status, code); }
 
 }  // namespace dgs

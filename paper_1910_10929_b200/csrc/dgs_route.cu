@@ -471,9 +471,6 @@ __global__ void __launch_bounds__(route_warps(PER) * 32, 1) k_route(const T* log
   }
 }
 
-// Starts before the kernel ahead of it has ended; what that one wrote is there after this.
-__device__ __forceinline__ void wait_for_last_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 // One CTA per expert (and one for the empty slots): the counts of its tiles become sums over the tiles before.
 __global__ void __launch_bounds__(256) k_route_sums(const __grid_constant__ RouteArgs a) {
   wait_for_last_kernel();
@@ -727,20 +724,9 @@ extern "C" int dgs_route_experts(const dgs_router* router, const dgs_matrix* log
     });
   });
   if (rc != DGS_OK || !a.counts) return rc;
-  // the next kernels are brought onto the SMs while the one before still runs
-  cudaLaunchAttribute early;
-  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t c = {};
-  c.blockDim = dim3(256);
-  c.stream = st;
-  c.attrs = &early;
-  c.numAttrs = 1;
-  c.gridDim = dim3(a.experts + 1);
-  if (cudaLaunchKernelEx(&c, k_route_sums, a) != cudaSuccess) return DGS_ECUDA;
-  c.gridDim = dim3(a.tiles);
-  c.dynamicSmemBytes = (3 * a.experts + 1) * 4;
-  return cudaLaunchKernelEx(&c, k_route_place, a) == cudaSuccess ? DGS_OK : DGS_ECUDA;
+  const EarlyLaunch sums(dim3(a.experts + 1), 256, 0, st), placing(dim3(a.tiles), 256, (3 * a.experts + 1) * 4, st);
+  if (cudaLaunchKernelEx(&sums.cfg, k_route_sums, a) != cudaSuccess) return DGS_ECUDA;
+  return cudaLaunchKernelEx(&placing.cfg, k_route_place, a) == cudaSuccess ? DGS_OK : DGS_ECUDA;
 }
 
 extern "C" int dgs_route_experts_grad(const dgs_router* router, const dgs_matrix* logits, const uint32_t* expert, const float* dweight,

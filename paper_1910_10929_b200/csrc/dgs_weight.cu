@@ -167,6 +167,7 @@ __device__ __forceinline__ void expert_rows(const WeightArgs& a, uint32_t expert
 constexpr uint32_t kDecodeRows = 16;   // of a CTA
 template <bool FLOAT8>
 __global__ void __launch_bounds__(256) k_weight_decode(const __grid_constant__ WeightArgs a) {
+  let_next_kernel_begin();
   const uint64_t at = uint64_t(blockIdx.x) * kDecodeRows;   // row of the decoded values
   uint64_t first = 0, last = a.dy_rows, begin = 0;
   if (a.offsets && blockIdx.x == gridDim.x - 1) {   // one CTA more: who comes before whom
@@ -277,9 +278,9 @@ template <class T>
 __global__ void __launch_bounds__(256) k_weight_parts(const T* dy, uint64_t rows, uint32_t cols, uint64_t from_stride, __nv_bfloat16* out, uint32_t stride,
                                                       uint64_t plane_rows) {
   constexpr uint32_t P = kParts<T>;
+  let_next_kernel_begin();
   const uint32_t unit = blockIdx.x * 256 + threadIdx.x, col = unit * 8;
-  if (col >= stride) return;
-  for (uint64_t row = blockIdx.y; row < plane_rows; row += gridDim.y) {
+  for (uint64_t row = blockIdx.y; row < plane_rows && col < stride; row += gridDim.y) {
     Eight<T> e;
     const T* p = dy + row * from_stride + col;
     const uint32_t left = row < rows && col < cols ? cols - col : 0;
@@ -319,6 +320,7 @@ __global__ void __launch_bounds__(256) k_weight_parts(const T* dy, uint64_t rows
 #pragma unroll
     for (uint32_t q = 0; q < P; ++q) *reinterpret_cast<uint4*>(out + (q * plane_rows + row) * stride + col) = w[q];
   }
+  wait_for_last_kernel();   // it runs beside the decoding, and whoever waits for this kernel waits for both
 }
 __device__ __forceinline__ void bias_add(const uint4& w, float (&bias)[8]) {   // eight bfloat16 numbers
   const uint32_t v[4] = {w.x, w.y, w.z, w.w};
@@ -419,6 +421,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
   pair_sync();
   tmem_after();
   const uint32_t tmem = s_tmem;
+  wait_for_last_kernel();   // nothing above touches memory outside the SM
 
   // Every role goes through the tiles by itself; it counts steps and chunks over all of them, which is what the barriers' phases go by.
   __syncwarp();
@@ -639,6 +642,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
 // at a time, so that their parts are on their way together.
 __global__ void __launch_bounds__(256) k_weight_sum(float* dw, float* db, const float* pw, const float* pb, uint64_t nw, uint64_t nb, uint32_t parts_w,
                                                     uint32_t parts_b, uint32_t add) {
+  wait_for_last_kernel();
   const bool bias = blockIdx.y != 0;
   float* out = bias ? db : dw;
   const float* p = bias ? pb : pw;
@@ -749,8 +753,8 @@ int make_map(const void* data, uint64_t rows, uint64_t cols, uint64_t stride, ui
 
 template <uint32_t P>
 int launch(const WeightArgs& a, const CUtensorMap& held, const CUtensorMap& grad, cudaStream_t st) {
-  k_weight_grad<P><<<std::min(a.tiles, kSms / 2) * 2, kThreads, Shape<P>::kSmem, st>>>(a, held, grad);
-  return cudaGetLastError() == cudaSuccess ? DGS_OK : DGS_ECUDA;
+  const EarlyLaunch l(dim3(std::min(a.tiles, kSms / 2) * 2), kThreads, Shape<P>::kSmem, st);
+  return cudaLaunchKernelEx(&l.cfg, k_weight_grad<P>, a, held, grad) == cudaSuccess ? DGS_OK : DGS_ECUDA;
 }
 
 }  // namespace
@@ -836,8 +840,9 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
       const dim3 grid(across, uint32_t(std::min<uint64_t>(p.plane_rows, std::max(1u, kSms * 16 / across))));
       rc = with_type(dy->type, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        k_weight_parts<T><<<grid, 256, 0, st>>>(static_cast<const T*>(dy->data), dy->rows, dy->cols, dy->stride, const_cast<__nv_bfloat16*>(a.dy), p.stride, p.plane_rows);
-        return cudaGetLastError() == cudaSuccess ? int(DGS_OK) : int(DGS_ECUDA);
+        const EarlyLaunch l(grid, 256, 0, st);
+        return cudaLaunchKernelEx(&l.cfg, k_weight_parts<T>, static_cast<const T*>(dy->data), dy->rows, dy->cols, dy->stride, const_cast<__nv_bfloat16*>(a.dy), p.stride,
+                                  p.plane_rows) == cudaSuccess ? int(DGS_OK) : int(DGS_ECUDA);
       });
       if (rc != DGS_OK) return rc;
     }
@@ -845,6 +850,8 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
   rc = p.parts == 1 ? launch<1>(a, held, grad, st) : p.parts == 2 ? launch<2>(a, held, grad, st) : launch<3>(a, held, grad, st);
   const uint64_t nw = p.splits > 1 ? p.nw : 0, nb = db && parts_b > 1 ? p.nb : 0;
   if (rc != DGS_OK || nw + nb == 0) return rc;
-  k_weight_sum<<<dim3(uint32_t(std::min<uint64_t>((std::max(nw, nb) + 1023) / 1024, kSms * 8)), nb ? 2 : 1), 256, 0, st>>>(dw, db, part_w, part_b, nw, nb, p.splits, parts_b, add);
-  return cudaGetLastError() == cudaSuccess ? DGS_OK : DGS_ECUDA;
+  const EarlyLaunch l(dim3(uint32_t(std::min<uint64_t>((std::max(nw, nb) + 1023) / 1024, kSms * 8)), nb ? 2 : 1), 256, 0, st);
+  return cudaLaunchKernelEx(&l.cfg, k_weight_sum, dw, db, static_cast<const float*>(part_w), static_cast<const float*>(part_b), nw, nb, p.splits, parts_b, add) == cudaSuccess
+             ? DGS_OK
+             : DGS_ECUDA;
 }
