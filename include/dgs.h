@@ -345,7 +345,7 @@ int dgs_topk_encode_static_status(void* stream, int* device_status);
 enum { DGS_TYPE_F32 = 0, DGS_TYPE_BF16 = 1, DGS_TYPE_FP16 = 2 };
 
 /* A matrix of the caller: element [r][c] is data[r * stride + c].  stride >= cols, or 0 for a matrix that is only read
- * and whose rows are all the same one.  data is aligned to the element.  rows < 2^32. */
+ * and whose rows are all the same one.  data is aligned to the element.  rows < 2^31. */
 typedef struct {
   void* data;      /* DEVICE */
   uint64_t rows;
@@ -367,7 +367,7 @@ enum { DGS_ACT_NONE = 0, DGS_ACT_RELU = 1, DGS_ACT_GELU = 2, DGS_ACT_GELU_TANH =
  * Bytes behind the last column are zero. */
 typedef struct {
   void* data;      /* DEVICE, 16-byte aligned, dgs_checkpoint_bytes long */
-  uint64_t rows;   /* < 2^32 */
+  uint64_t rows;   /* < 2^31 */
   uint32_t cols;   /* 1 .. 2^30 */
   uint32_t format; /* DGS_FORMAT_* */
 } dgs_checkpoint;
@@ -389,7 +389,8 @@ enum { DGS_WEIGHT_IN_OUT = 1u << 0, /* dw is [inputs][outputs]; without it [outp
        DGS_WEIGHT_ADD = 1u << 1     /* dw and db are added to; without it they are set      */ };
 
 /* Which rows belong to which expert.  Row j of dy with offsets[e] <= j < offsets[e + 1] belongs to expert e and to
- * row rows[j] / rows_per of the checkpoint (to row j if rows is NULL).  Offsets ascend. */
+ * row rows[j] / rows_per of the checkpoint (to row j if rows is NULL).  Offsets ascend; where they do not, the gradients are
+ * not specified. */
 typedef struct {
   const uint32_t* offsets; /* DEVICE u32[experts + 1] */
   const uint32_t* rows;    /* DEVICE u32[rows of dy] or NULL */
@@ -403,8 +404,11 @@ typedef struct {
  * or NULL.  inputs = ckpt->cols, outputs = dy->cols.  With lists, one such gradient per expert over the expert's rows,
  * dw [experts][...] and db [experts][outputs]; an expert without rows gets zeros.  Without lists (NULL) dy has the
  * checkpoint's rows.  Products are exact and are summed in f32 (f16 and f32 gradients are taken apart into bfloat16
- * numbers whose sum they are).  workspace: DEVICE, 16-byte aligned, at least what dgs_checkpoint_weight_grad_bytes says for
- * these arguments (which may be 0). */
+ * numbers whose sum they are).  A row of dy that is in no list has no part in anything.  At most DGS_ROUTE_MAX_EXPERTS experts.
+ * workspace: DEVICE, 16-byte aligned, at least what dgs_checkpoint_weight_grad_bytes says for these arguments (data pointers
+ * included: their alignment counts).  It takes the checkpoint's values as bfloat16 numbers (2 bytes a value for each row of dy), dy as
+ * bfloat16 numbers unless it is that with rows on 16 bytes (2 bytes a value, fp16 4, f32 6), and partial results where
+ * rows are split.  Rows times parts of a value below 2^31, else DGS_ELIMIT. */
 int dgs_checkpoint_weight_grad_bytes(const dgs_checkpoint* ckpt, const dgs_matrix* dy, const dgs_row_lists* lists, uint32_t flags,
                                      uint64_t* out_bytes);
 int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_matrix* dy, const dgs_row_lists* lists, float* dw, float* db,

@@ -62,7 +62,7 @@ inline bool aligned(const void* p, uint64_t to) { return reinterpret_cast<uintpt
 constexpr uint64_t kMostElements = 1ull << 40;   // rows * stride: keeps every byte count far inside 64 bits
 // A matrix that a call reads (rows may share one row: stride 0) or writes.
 inline bool matrix_ok(const dgs_matrix* m, bool written) {
-  if (!m || m->type > DGS_TYPE_FP16 || m->cols == 0 || m->rows >= (1ull << 32)) return false;
+  if (!m || m->type > DGS_TYPE_FP16 || m->cols == 0 || m->rows >= (1ull << 31)) return false;
   if (m->stride < m->cols && m->rows > 1 && (written || m->stride != 0)) return false;
   if (m->stride && m->rows > kMostElements / m->stride) return false;
   return m->rows == 0 || (m->data && aligned(m->data, elem_bytes(m->type)));
@@ -97,7 +97,7 @@ inline Held held_of(const dgs_checkpoint* c) {
   return h;
 }
 inline bool checkpoint_ok(const dgs_checkpoint* c) {
-  return c && c->format <= DGS_FORMAT_E4M3 && c->cols && c->cols <= (1u << 30) && c->rows < (1ull << 32) &&
+  return c && c->format <= DGS_FORMAT_E4M3 && c->cols && c->cols <= (1u << 30) && c->rows < (1ull << 31) &&
          c->rows <= kMostElements / c->cols && (c->rows == 0 || (c->data && aligned(c->data, 16)));
 }
 

@@ -8,7 +8,8 @@ namespace dgs {
 namespace {
 
 constexpr uint32_t kTile = 64;           // tokens of a CTA: two words of a bit mask per expert
-// Warps of a CTA: each takes some of the tile's tokens one after the other (8192 tokens of 60 experts: 21 us with 8 warps).
+// Warps of a CTA: each takes some of the tile's tokens one after the other (8192 tokens of 60 experts: 21 us with 8 warps,
+// 10 with 32; 65536 of 256: 113 and 97).  Rows beyond 256 experts need more registers than 32 warps have.
 __host__ __device__ constexpr uint32_t route_warps(int per) { return per <= 8 ? 32 : 8; }
 constexpr uint32_t kAll = 0xffffffffu;
 
@@ -325,7 +326,8 @@ __device__ __forceinline__ void place_tile(const RouteArgs& a, uint32_t tile, co
 
 // One warp per token, a tile of 64 tokens per CTA.  The token's logits stay in registers.  The experts chosen are marked in a bit mask per
 // expert (bit = token of the tile), whose counts are what a later kernel needs to place the tile's slots; a single tile is placed here.
-// Bound by instructions: about 450 a token of 256 experts with groups and a bias, where reading takes the time of 170.
+// Bound by instructions: about 1000 a token of 256 experts with groups and a bias (97 us for 65536 tokens, whose reading takes 10), 530 for 60 experts
+// without; a token's chain of maxima over the warp is hidden by the other warps only.
 template <int PER, class T>
 __global__ void __launch_bounds__(route_warps(PER) * 32, 1) k_route(const T* logits, const __grid_constant__ RouteArgs a) {
   extern __shared__ uint32_t mask[];   // [experts][2]
@@ -540,6 +542,7 @@ __device__ __forceinline__ void write_logits(T* row, const RouteArgs& a, const f
     if (e0 + i < a.experts) row[e0 + i] = Elem<T>::put(z[i]);
 }
 
+// 65536 x 256 in f32: 42 us, half of it writing the rows; bound by the trip from slot to logit to row of each token.
 // A slot a lane, then the dense row.  Everything but a softmax without renormalising leaves a row zero outside the chosen, so only
 // their logits are read; where an expert is listed twice its gradients add up.
 template <int PER, class T>

@@ -3,7 +3,7 @@ activations held in 8 bits and the gradients formed from them, and the router of
 
 Outputs and workspaces are torch tensors of the inputs' device, and work is enqueued on that device's current
 stream, whichever device is current for the caller; as with torch's own operators, a tensor used on another stream than the one it was
-made on has to be ordered and recorded by the caller.  Nothing waits for the GPU.  Arguments that do not fit raise ValueError before any work
+made on has to be ordered and recorded by the caller.  They are not part of torch's differentiation: a backward pass calls them by name.  Nothing waits for the GPU.  Arguments that do not fit raise ValueError before any work
 is enqueued, what the library refuses raises DgsError.
 """
 from __future__ import annotations
@@ -102,7 +102,7 @@ class Checkpoint:
         if self.rows < 0 or self.cols < 1:
             raise ValueError(f"a checkpoint has rows >= 0 and cols >= 1: got {rows} x {cols}")
         size = self.rows * (-(-self.cols // 32) * 32 + -(-self.cols // 128) * 4)
-        if self.rows >= 1 << 32 or self.cols > 1 << 30 or self.rows * self.cols > 1 << 40:
+        if self.rows >= 1 << 31 or self.cols > 1 << 30 or self.rows * self.cols > 1 << 40:
             size = dgs.dgs_checkpoint_bytes(self.rows, self.cols)   # raises what the library says
         if data is None:
             data = torch.empty(size, dtype=torch.uint8, device="cuda" if device is None else device)

@@ -175,8 +175,8 @@ def test_activation_grad_against_the_formula_and_differences(dtype, act, fmt):
 
 
 def test_more_than_one_stride_of_the_grid():
-    """Rows and columns past what the grid covers at once: 148 * 8 CTAs of 256 units of 8."""
-    for rows, cols in ((20_000, 257), (9, 600_000)):
+    """Rows and columns past what the grid covers at once: 148 * 6 CTAs of 256 units of 8."""
+    for rows, cols in ((20_000, 257), (9, 600_000), (3, 1_900_001)):
         x = torch.randn(rows, cols, device=DEV, dtype=torch.bfloat16)
         c = dgs.Checkpoint(rows, cols, device=DEV)
         c.save(x)

@@ -32,8 +32,8 @@ def test_sizes():
     for rows, cols in ((1, 1), (3, 32), (5, 33), (7, 128), (2, 129), (11, 2048)):
         buffer, _ = encode(np.zeros((rows, cols)), "int8")
         assert dgs.dgs_checkpoint_bytes(rows, cols) == len(buffer)
-    assert dgs.dgs_checkpoint_bytes((1 << 32) - 1, 100) == ((1 << 32) - 1) * 132          # far past 32 bits
-    for rows, cols in ((1, 0), (1, (1 << 30) + 1), (1 << 32, 1), (1 << 31, 1 << 10)):
+    assert dgs.dgs_checkpoint_bytes((1 << 31) - 1, 100) == ((1 << 31) - 1) * 132          # far past 32 bits
+    for rows, cols in ((1, 0), (1, (1 << 30) + 1), (1 << 31, 1), ((1 << 31) - 1, 1 << 10)):
         with pytest.raises(dgs.DgsError) as e:
             dgs.dgs_checkpoint_bytes(rows, cols)
         assert e.value.code == dgs.DGS_EINVAL
@@ -42,7 +42,7 @@ def test_sizes():
     assert dgs.lib().dgs_checkpoint_bytes(1, 1, None) == dgs.DGS_EINVAL
 
 
-BAD_MATRICES = [dict(rows=9), dict(cols=63), dict(stride=63), dict(kind=3), dict(data=P + 2), dict(data=0), dict(rows=1 << 32),
+BAD_MATRICES = [dict(rows=9), dict(cols=63), dict(stride=63), dict(kind=3), dict(data=P + 2), dict(data=0), dict(rows=1 << 31),
                 dict(stride=1 << 45)]
 
 
