@@ -204,32 +204,39 @@ __global__ void __launch_bounds__(256) k_weight_decode(const __grid_constant__ W
   // rows behind the expert's last are zero up to the end of its last step
   const uint64_t row0 = at - begin, rows = last - first;
   if (row0 >= (rows + a.step_rows - 1) / a.step_rows * a.step_rows) return;
+  // which row of the checkpoint each of the sixteen is
+  constexpr uint32_t kNone = 0xffffffffu;
+  __shared__ uint32_t s_src[kDecodeRows];
+  if (threadIdx.x < kDecodeRows) {
+    uint32_t src = kNone;
+    if (row0 + threadIdx.x < rows) {
+      src = uint32_t(first + row0) + threadIdx.x;
+      if (a.rows) src = a.rows[src] / a.rows_per;
+      if (src >= a.h.rows) {
+        report(a.status, DGS_EINVAL);
+        src = kNone;
+      }
+    }
+    s_src[threadIdx.x] = src;
+  }
+  __syncthreads();
   const uint32_t units = a.h.width / 8, total = kDecodeRows * units;
+  // i / units as the upper half of a product: exact while i * units < 2^32
+  const uint32_t magic = units > 1 && units < (1u << 14) ? 0xffffffffu / units + 1 : 0;
   for (uint32_t i0 = threadIdx.x; i0 < total; i0 += 4 * 256) {
     uint2 w[4];
     uint32_t scale[4], row[4], unit[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {   // four units on their way together
       const uint32_t i = min(i0 + k * 256, total - 1);
-      row[k] = i / units;
+      row[k] = magic ? __umulhi(i, magic) : i / units;
       unit[k] = i - row[k] * units;
-      uint64_t src = first + row0 + row[k];
-      bool there = row0 + row[k] < rows;
-      if (a.offsets && there) {
-        if (a.rows) {
-          const uint32_t v = a.rows[src];
-          src = a.rows_per == 1 ? v : v / a.rows_per;
-        }
-        if (src >= a.h.rows) {
-          report(a.status, DGS_EINVAL);
-          there = false;
-        }
-      }
+      const uint32_t src = s_src[row[k]];
       w[k] = make_uint2(0, 0);
       scale[k] = 0;
-      if (there) {
-        w[k] = __ldg(reinterpret_cast<const uint2*>(a.h.codes + src * a.h.width + unit[k] * 8));
-        scale[k] = __ldg(a.h.scales + src * a.h.spitch + unit[k] / 4);
+      if (src != kNone) {
+        w[k] = __ldg(reinterpret_cast<const uint2*>(a.h.codes + uint64_t(src) * a.h.width + unit[k] * 8));
+        scale[k] = __ldg(a.h.scales + uint64_t(src) * a.h.spitch + unit[k] / 4);
       }
     }
 #pragma unroll
@@ -662,10 +669,95 @@ __global__ void __launch_bounds__(256) k_weight_sum(float* dw, float* db, const 
   }
 }
 
+// ---- few rows ---------------------------------------------------------------------------------------
+// Where there is little to do, the three kernels that bring operands to the tensor cores cost more than products without them: one launch, a tile of 64 x 64
+// results a CTA, 4 x 4 of them a thread, sixteen rows at a time through shared memory, sums in f32 with rounding.  Bound by the trips to memory and the
+// barriers of each sixteen rows, 1 us.  Here / with tensor cores, us: 37 x 512 x 1000 12.7 / 25.3 in f32, 12.7 / 21.5 in bfloat16; 128 x 1024 x 1024 17.4 /
+// 22.5; 256 x 768 x 680 19.6 / 22.9; 512 x 512 x 512 35.5 / 22.3, 31.8 / 28.8 in f32.
+constexpr uint32_t kSmallRows = 256;
+constexpr uint64_t kSmallProducts = 1ull << 27;
+constexpr uint32_t kSmallTile = 64, kSmallStep = 16;
+
+template <class T, bool FLOAT8>
+__global__ void __launch_bounds__(256) k_weight_small(const __grid_constant__ WeightArgs a, const T* dy) {
+  __shared__ __align__(16) float s_held[kSmallStep][kSmallTile + 4], s_grad[kSmallStep][kSmallTile + 4];
+  const uint32_t t = threadIdx.x, i0 = blockIdx.x * kSmallTile, o0 = blockIdx.y * kSmallTile, expert = blockIdx.z;
+  uint64_t first, last;
+  expert_rows(a, expert, &first, &last, t == 0 && blockIdx.x == 0 && blockIdx.y == 0);
+  const uint32_t count = uint32_t(last - first), row = t / 16, quad = t % 16 * 4;   // four columns of one of the sixteen rows
+  const uint32_t held_col = i0 + quad, grad_col = o0 + quad;
+  float acc[4][4], bias = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = 0.0f;
+  uint32_t code = 0, scale = 0;
+  float grad[4];
+  auto fetch = [&](uint32_t from) {
+    const uint32_t j = from + row;
+    code = scale = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) grad[i] = 0.0f;
+    if (j >= count) return;
+    uint32_t src = uint32_t(first) + j;
+    const T* g = dy + (first + j) * a.dy_stride + grad_col;
+    if (a.rows) src = a.rows[src] / a.rows_per;
+    if (src >= a.h.rows) {
+      report(a.status, DGS_EINVAL);
+    } else if (held_col < a.h.width) {
+      code = *reinterpret_cast<const uint32_t*>(a.h.codes + uint64_t(src) * a.h.width + held_col);
+      scale = a.h.scales[uint64_t(src) * a.h.spitch + held_col / 32];
+    }
+    // a row that names no row of the checkpoint still counts for the bias of its own, as in the other kernel
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (grad_col + i < a.outputs) grad[i] = Elem<T>::get(g[i]);
+  };
+  fetch(0);
+  for (uint32_t from = 0; from < count; from += kSmallStep) {
+    float2 v[4];
+    decode8<FLOAT8>(make_uint2(code, 0), scale_down(scale), v);
+    *reinterpret_cast<float4*>(&s_held[row][quad]) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+    *reinterpret_cast<float4*>(&s_grad[row][quad]) = make_float4(grad[0], grad[1], grad[2], grad[3]);
+    __syncthreads();
+    fetch(from + kSmallStep);
+    const float(*along)[kSmallTile + 4] = a.in_out ? s_grad : s_held;    // the dimension of dw that is contiguous
+    const float(*across)[kSmallTile + 4] = a.in_out ? s_held : s_grad;
+#pragma unroll
+    for (uint32_t k = 0; k < kSmallStep; ++k) {
+      const float4 x = *reinterpret_cast<const float4*>(&along[k][quad]), y = *reinterpret_cast<const float4*>(&across[k][row * 4]);
+      const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(ys[i], xs[j], acc[i][j]);
+    }
+    if (a.db && blockIdx.x == 0 && t < kSmallTile)
+#pragma unroll
+      for (uint32_t k = 0; k < kSmallStep; ++k) bias += s_grad[k][t];
+    __syncthreads();
+  }
+  const uint32_t along_at = (a.in_out ? o0 : i0) + quad, along_end = a.in_out ? a.outputs : a.inputs;
+  const uint32_t across_at = (a.in_out ? i0 : o0) + row * 4, across_end = a.in_out ? a.inputs : a.outputs;
+  float* dw = a.dw + uint64_t(expert) * a.inputs * a.outputs;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (across_at + i < across_end && along_at + j < along_end) {
+        float* p = dw + uint64_t(across_at + i) * along_end + along_at + j;
+        *p = a.add_w ? *p + acc[i][j] : acc[i][j];
+      }
+  if (a.db && blockIdx.x == 0 && t < kSmallTile && o0 + t < a.outputs) {
+    float* p = a.db + uint64_t(expert) * a.outputs + o0 + t;
+    *p = a.add_b ? *p + bias : bias;
+  }
+}
+
 // ---- host side --------------------------------------------------------------------------------
 struct WeightPlan {
   uint32_t parts, code_tiles, grad_tiles, n, splits, bias_tiles, experts, step_rows, stride;
-  bool direct;                       // the gradient is read as it is
+  bool small, direct;                // one kernel without tensor cores; the gradient is read as it is
   uint64_t nw, nb, plane_rows, decoded, planes, order, bytes;
 };
 
@@ -687,6 +779,14 @@ int plan_weight(const dgs_checkpoint* c, const dgs_matrix* dy, const dgs_row_lis
   if (uint64_t(c->cols) * dy->cols > kMostElements / p->experts || dy->rows >= (1u << 31) / p->parts - 1026 * 128 || dy->cols > (1u << 30)) return DGS_ELIMIT;
   p->nw = uint64_t(c->cols) * dy->cols * p->experts;
   p->nb = uint64_t(dy->cols) * p->experts;
+  // both sides are measured at k_weight_small
+  p->small = dy->rows <= kSmallRows && uint64_t(c->cols) * dy->cols <= kSmallProducts / std::max<uint64_t>(dy->rows, 1) &&
+             ceil_div(dy->cols, kSmallTile) <= 65535;
+  if (p->small) {
+    p->splits = p->bias_tiles = 1;
+    p->bytes = 0;
+    return DGS_OK;
+  }
   // The tile's width and the split of a tile's rows among pairs: whatever ends soonest.  74 pairs run at a time; 64 rows take 0.3 us and 0.1 by the
   // width, a tile about 4 us besides, and partial results cost their way through the second cache and another launch.  (8192 x 768 x 2304: 54
   // tiles of 128 columns 57 us, 27 of 256 in two runs of rows each 37.)
@@ -764,7 +864,7 @@ using namespace dgs;
 
 extern "C" int dgs_checkpoint_weight_grad_bytes(const dgs_checkpoint* ckpt, const dgs_matrix* dy, const dgs_row_lists* lists, uint32_t flags,
                                                 uint64_t* out_bytes) {
-  WeightPlan p;
+  WeightPlan p = {};
   if (!out_bytes || (flags & ~(DGS_WEIGHT_IN_OUT | DGS_WEIGHT_ADD))) return DGS_EINVAL;
   const int rc = plan_weight(ckpt, dy, lists, flags, &p);
   if (rc == DGS_OK) *out_bytes = p.bytes;
@@ -773,7 +873,7 @@ extern "C" int dgs_checkpoint_weight_grad_bytes(const dgs_checkpoint* ckpt, cons
 
 extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_matrix* dy, const dgs_row_lists* lists, float* dw, float* db,
                                           uint32_t flags, void* workspace, uint64_t workspace_bytes, void* stream) {
-  WeightPlan p;
+  WeightPlan p = {};
   if (flags & ~(DGS_WEIGHT_IN_OUT | DGS_WEIGHT_ADD)) return DGS_EINVAL;
   int rc = plan_weight(ckpt, dy, lists, flags, &p);
   if (rc != DGS_OK) return rc;
@@ -787,8 +887,7 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
   for (const auto& x : part)
     for (const auto& y : part)
       if (&x != &y && x.out && overlap(x.p, x.n, y.p, y.n)) return DGS_EINVAL;
-  rc = weight_ready();
-  if (rc != DGS_OK) return rc;
+  if (!p.small && (rc = weight_ready()) != DGS_OK) return rc;
   const uint32_t parts_b = p.splits * p.bias_tiles;
   char* const work = static_cast<char*>(workspace);
   WeightArgs a = {};
@@ -823,6 +922,18 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
   a.status = operator_status_word();
   if (!a.status) return DGS_ECUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (p.small) {
+    a.dy_stride = dy->stride;
+    return with_type(dy->type, [&](auto* t) {
+      using T = std::remove_pointer_t<decltype(t)>;
+      const dim3 grid(ceil_div(a.inputs, kSmallTile), ceil_div(a.outputs, kSmallTile), a.experts);
+      if (ckpt->format == DGS_FORMAT_E4M3)
+        k_weight_small<T, true><<<grid, 256, 0, st>>>(a, static_cast<const T*>(dy->data));
+      else
+        k_weight_small<T, false><<<grid, 256, 0, st>>>(a, static_cast<const T*>(dy->data));
+      return cudaGetLastError() == cudaSuccess ? int(DGS_OK) : int(DGS_ECUDA);
+    });
+  }
   CUtensorMap held = {}, grad = {};
   if (dy->rows) {
     const uint64_t rows = p.decoded / (2 * uint64_t(a.h.width));

@@ -93,7 +93,7 @@ def test_weight_grad_refusals():
         assert call(lists=lists) == dgs.DGS_EINVAL
     big, long = held(rows=100_000), matrix(rows=100_000)       # split: needs a workspace
     need = dgs.dgs_checkpoint_weight_grad_bytes(big, long)
-    assert need > 0
+    assert need > 0 and dgs.dgs_checkpoint_weight_grad_bytes(c, dy) == 0      # few rows: none
     assert call(big, long, dw=P << 8, work=P << 12, size=need - 1) == dgs.DGS_ENOMEM
     assert call(big, long, dw=P << 8, work=None, size=need) == dgs.DGS_EINVAL
     assert call(big, long, dw=P << 8, work=(P << 12) + 4, size=need) == dgs.DGS_EINVAL

@@ -1,6 +1,6 @@
 """The operators of a worker's own computation together, as a worker of a model with experts uses them between two pushes: route, hold the
 inputs in 8 bits, apply an activation, form every layer's gradient in its slice of the flat vector, push.  The gradient is compared with the one that
-64-bit differentiation of the same network gives, and what the push makes of it with the CPU checker, bit for bit."""
+64-bit differentiation of the same network gives, and what the push makes of it with the oracle, bit for bit."""
 import numpy as np
 import pytest
 import torch
@@ -106,7 +106,7 @@ def test_a_worker_with_experts_from_tokens_to_packets():
     for e, s in enumerate(spans):
         w2 = dout[s].double().T @ held_a.load()[s].double()
         assert float((got.w2[e] - w2).norm()) <= 600 * 2.0 ** -24 * float(w2.norm()) + 1e-30
-    # the push of that gradient, against the CPU checker
+    # the push of that gradient, against the oracle
     seg = Layers(theta).seg
     off, length = [s[0] for s in seg], [s[1] for s in seg]
     k = [max(1, v // 20) for v in length]
