@@ -334,7 +334,8 @@ int dgs_topk_encode_static_status(void* stream, int* device_status);
  * slices of that vector, and, for models with experts, the router whose selection says which rows belong to which
  * expert.  They need no context.  Common rules:
  *   - Nothing is allocated; outputs and workspaces are the caller's.  Work is enqueued on `stream` (a cudaStream_t of
- *     the current device; NULL = default stream) and the call returns.  All of them may be captured into a graph.
+ *     the current device; NULL = default stream) and the call returns.  All of them may be captured into a graph once a call of
+ *     the kind has been made on the device outside a capture.
  *     Two calls whose work may overlap need workspaces of their own.
  *   - Results are the same bits for the same inputs, on every run.
  *   - Outputs must not overlap inputs unless a call says so; where the ranges do, it returns DGS_EINVAL.

@@ -2,9 +2,10 @@
 activations held in 8 bits and the gradients formed from them, and the router of a model with experts.
 
 Outputs and workspaces are torch tensors of the inputs' device, and work is enqueued on that device's current
-stream, whichever device is current for the caller; as with torch's own operators, a tensor used on another stream than the one it was
-made on has to be ordered and recorded by the caller.  They are not part of torch's differentiation: a backward pass calls them by name.  Nothing waits for the GPU.  Arguments that do not fit raise ValueError before any work
-is enqueued, what the library refuses raises DgsError.
+stream, whichever device is current for the caller; as with torch's own operators, a tensor used on another stream
+than the one it was made on has to be ordered and recorded by the caller.  Nothing waits for the GPU.  They are not
+part of torch's differentiation: a backward pass calls them by name.  Arguments that do not fit raise ValueError
+before any work is enqueued, what the library refuses raises DgsError.
 """
 from __future__ import annotations
 
@@ -207,13 +208,13 @@ def route_experts(logits: torch.Tensor, k: int, *, score: str = "softmax", bias:
     pb = _plain(bias, "bias", torch.float32, experts, device)
     need = dgs.dgs_route_experts_bytes(router, tokens, experts)
     slots = tokens * router.k
-    # one piece of memory for the outputs of four bytes and the workspace, which begins on a multiple of 16
-    whole = torch.empty(-(-(3 * slots + experts + 1) // 4) * 4 + need // 4, dtype=torch.int32, device=device)
-    expert, order, place, offsets, _ = whole.split([slots, slots, slots, experts + 1, whole.numel() - 3 * slots - experts - 1])
+    whole = torch.empty(3 * slots + experts + 1, dtype=torch.int32, device=device)
+    expert, order, place, offsets = whole.split([slots, slots, slots, experts + 1])
     weight = torch.empty(tokens, router.k, dtype=torch.float32, device=device)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     at = whole.data_ptr()
     _enqueue(device, dgs.dgs_route_experts, router, m, pb, at, weight.data_ptr(), at + 12 * slots, at + 4 * slots, at + 8 * slots,
-             at + 4 * (whole.numel() - need // 4) if need else 0, need)
+             work.data_ptr() if need else 0, need)
     return Route(expert.view(tokens, router.k), weight, offsets, order, place.view(tokens, router.k))
 
 

@@ -89,8 +89,9 @@ def test_values_at_the_edges_of_the_format(fmt):
 
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 @pytest.mark.parametrize("cols", [64, 70])
-def test_a_block_with_an_infinity_or_nan_reads_as_nan_and_no_other(fmt, cols):
-    x = torch.randn(4, cols, device=DEV)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_block_with_an_infinity_or_nan_reads_as_nan_and_no_other(dtype, cols, fmt):
+    x = torch.randn(4, cols, device=DEV).to(dtype)
     x[0, 3], x[1, 40], x[2, 31], x[2, 32] = float("inf"), float("nan"), -float("inf"), float("nan")
     want, held = encode(x.double().cpu().numpy(), fmt)
     c = dgs.Checkpoint(4, cols, fmt, device=DEV)
