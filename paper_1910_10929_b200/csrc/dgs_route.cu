@@ -509,6 +509,10 @@ __global__ void __launch_bounds__(256) k_route_place(const __grid_constant__ Rou
 // ---- gradient ---------------------------------------------------------------------------------
 // g_j = scale * dweight_j.  softmax: dz_e = s_e ([e chosen] g_e - sum_j g_j s_j); renormalised dz_l = p_l (g_l - sum g p) on the chosen only (p the
 // weights without scale); sigmoid: dz_l = g_l s_l (1 - s_l); renormalised: p_l (g_l - sum g p)(1 - s_l).
+// CTAs on an SM: as many as are launched, so that all have the same to do (65536 x 256: 36 us, 43 with sixteen that come in turns, 41 with the next
+// tokens' slots and logits read ahead).
+constexpr uint32_t kGradPerSm = 6;
+
 template <int PER, class T>
 __device__ __forceinline__ void write_logits(T* row, const RouteArgs& a, const float (&z)[PER]) {
   const uint32_t e0 = (threadIdx.x & 31) * PER;
@@ -542,11 +546,11 @@ __device__ __forceinline__ void write_logits(T* row, const RouteArgs& a, const f
     if (e0 + i < a.experts) row[e0 + i] = Elem<T>::put(z[i]);
 }
 
-// 65536 x 256 in f32: 42 us, half of it writing the rows; bound by the trip from slot to logit to row of each token.
+// 65536 x 256 in f32: 36 us, half of it writing the rows; bound by the trip from slot to logit to row of each token.
 // A slot a lane, then the dense row.  Everything but a softmax without renormalising leaves a row zero outside the chosen, so only
 // their logits are read; where an expert is listed twice its gradients add up.
 template <int PER, class T>
-__global__ void __launch_bounds__(256) k_route_grad(const T* logits, T* dlogits, uint64_t dstride, const uint32_t* expert, const float* dweight,
+__global__ void __launch_bounds__(256, PER <= 8 ? kGradPerSm : 1) k_route_grad(const T* logits, T* dlogits, uint64_t dstride, const uint32_t* expert, const float* dweight,
                                                     const __grid_constant__ RouteArgs a, int* status) {
   __shared__ float s_row[8][PER * 32 + 1];
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -752,7 +756,7 @@ extern "C" int dgs_route_experts_grad(const dgs_router* router, const dgs_matrix
       constexpr uint32_t width = per.value * sizeof(T) < 16 ? per.value * sizeof(T) : 16;
       a.wide = aligned(logits->data, width) && logits->stride * sizeof(T) % width == 0 && aligned(dlogits->data, width) &&
                dlogits->stride * sizeof(T) % width == 0;
-      const uint32_t ctas = std::min<uint32_t>((a.tokens + 7) / 8, kSms * 16);
+      const uint32_t ctas = std::min<uint32_t>((a.tokens + 7) / 8, kSms * kGradPerSm);
       k_route_grad<per.value, T><<<ctas, 256, 0, static_cast<cudaStream_t>(stream)>>>(
           static_cast<const T*>(logits->data), static_cast<T*>(dlogits->data), dlogits->stride, expert, dweight, a, status);
       return launched();
