@@ -397,7 +397,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
   using S = Shape<P>;
   constexpr uint32_t R = S::kRows, ST = S::kStages, CH = S::kChunk, STAGE = S::kStage, TILE = S::kTile, BLOCK = S::kColBlock;
   extern __shared__ unsigned char raw[];
-  __shared__ __align__(8) uint64_t s_full[ST], s_empty[ST], s_loaded[ST], s_sum_full[2], s_sum_empty[2], s_tail, s_bias_done, s_done;
+  __shared__ __align__(8) uint64_t s_full[ST], s_empty[ST], s_loaded[ST], s_sum_full[2], s_sum_empty[2], s_free[ST], s_tail, s_bias_done, s_done;
   __shared__ uint32_t s_tmem;
   __shared__ float s_bias[20 * kCols];   // rows 0 to 3: sums of the steps that came by TMA, 4 to 19: of the last step
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = cta_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2, rounds = (a.tiles + pairs - 1) / pairs;
@@ -411,6 +411,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
         bar_init(smem_at(&s_full[s]), 2);     // that copies landed, of both CTAs
         bar_init(smem_at(&s_empty[s]), 3);    // products done; the bias' warps
         bar_init(smem_at(&s_loaded[s]), 1);
+        bar_init(smem_at(&s_free[s]), 1);     // the gradients of an expert's last rows may be written
       }
       for (uint32_t i = 0; i < 2; ++i) {
         bar_init(smem_at(&s_sum_full[i]), 1);
@@ -476,6 +477,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           const uint32_t st = it % ST, to = tiles + st * STAGE, bar = smem_at(&s_loaded[st]), grads = s < w.tma_steps ? grad_blocks : 0;
           if (it >= ST && !(alive = bar_wait(smem_at(&s_empty[st]), (it / ST - 1) & 1))) break;
+          if (s >= w.tma_steps) bar_arrive(smem_at(&s_free[st]));
           bar_expect(bar, (code_blocks + P * grads) * BLOCK);
           for (uint32_t c = 0; c < code_blocks; ++c) tma_load(to + c * BLOCK, &held_map, int(w.ci + c * 64), int(w.held_first + uint64_t(s) * R), bar);
 #pragma unroll
@@ -542,7 +544,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSum));
     const uint32_t quarter = warp % 4, group = warp / 4;
     bool alive = true;
-    uint32_t it = 0, drained = 0;
+    uint32_t it = 0, drained = 0, used = 0;   // used: bit s is the phase of s_free[s] to wait for
     for (uint32_t ordinal = 0; ordinal < rounds && alive; ++ordinal) {
       const uint32_t tile = tile_in_round(ordinal, pair, pairs);
       if (tile >= a.tiles) break;
@@ -576,7 +578,10 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
               }
             }
           }
-          if (last >= ST && !(alive = warp_wait(smem_at(&s_empty[last % ST]), (last / ST - 1) & 1))) break;
+          // Not s_empty itself: waits by parity only tell neighbouring phases apart, and the sums may be two phases of s_empty ahead of the bias' warps
+          // here.  The thread of the copies waits for every phase of s_empty, and a stage has no second tail before this one is read.
+          if (!(alive = warp_wait(smem_at(&s_free[last % ST]), used >> last % ST & 1))) break;
+          used ^= 1u << last % ST;
           if (ordinal && !(alive = warp_wait(smem_at(&s_bias_done), (ordinal - 1) & 1))) break;   // the table is free
           float bias[8] = {};
 #pragma unroll

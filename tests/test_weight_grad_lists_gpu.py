@@ -1,0 +1,41 @@
+"""Weight gradients of experts at the lengths that the products' kernel treats apart: last steps that share a copy's rows with the next expert, at
+every place in a run of steps.  Sums of whole numbers are exact in f32 in any order, so results must come out bit for bit."""
+import pytest
+import torch
+
+import paper_1910_10929_b200 as dgs
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def check(lengths, inputs, outputs, dtype, layout, behind=0, seed=0, scattered=False):
+    """dw and db of experts with these numbers of rows, `behind` rows of dy in no list, the checkpoint's rows in order or in any."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    rows, experts = sum(lengths) + behind, len(lengths)
+    x = torch.randint(-7, 8, (rows, inputs), generator=g, device=DEV).float()
+    dy = torch.randint(-8, 9, (rows, outputs), generator=g, device=DEV).to(dtype)
+    c = dgs.Checkpoint(rows, inputs, "e4m3", device=DEV)
+    c.save(x)
+    order = torch.randperm(rows, generator=g, device=DEV).to(torch.int32) if scattered else None
+    offsets = torch.tensor([0] + lengths).cumsum(0).to(torch.int32).to(DEV)
+    shape = (experts, outputs, inputs) if layout == "out_in" else (experts, inputs, outputs)
+    dw, db = torch.full(shape, float("nan"), device=DEV), torch.full((experts, outputs), float("nan"), device=DEV)
+    c.weight_grad(dy, dw, db, layout=layout, offsets=offsets, rows=order)
+    assert dgs.operator_status(DEV) == 0
+    at = 0
+    for e, n in enumerate(lengths):
+        d = dy[at:at + n].double()
+        h = (x[order[at:at + n].long()] if scattered else x[at:at + n]).double()
+        want = d.T @ h if layout == "out_in" else h.T @ d
+        assert torch.equal(dw[e].double(), want) and torch.equal(db[e].double(), d.sum(0)), e
+        at += n
+
+
+@pytest.mark.parametrize("layout", ["out_in", "in_out"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_last_steps_at_every_place_in_a_run(dtype, layout):
+    """Experts of 5 to 45 steps of 64 rows, the last one never whole: it is any of the four or eight steps between two sums, and comes up to eight
+    steps after the sums before.  All bias sums are one CTA's, which keeps its stages longest; more tiles than pairs of CTAs."""
+    check([64 * (5 + e) + 1 + e for e in range(40)], 64, 300, dtype, layout, behind=70)
