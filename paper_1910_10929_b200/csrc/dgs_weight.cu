@@ -506,7 +506,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           const uint32_t st = it % ST;
           if (!(alive = warp_wait(smem_at(&s_loaded[st]), it / ST & 1))) break;
-          if (s >= w.tma_steps && warp == 10 && !(alive = warp_wait(smem_at(&s_tail), tails++ & 1))) break;
+          if (s >= w.tma_steps && warp == 10 && !(alive = warp_wait(smem_at(&s_tail), tails & 1))) break;
           if (warp == 10 && lane == 0) bar_arrive_cluster(in_leader(smem_at(&s_full[st])));
           if (w.bias && s < w.tma_steps && s % a.bias_tiles == w.ct) {
 #pragma unroll 4
@@ -536,7 +536,10 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
           }
           asm volatile("bar.sync 1, 64;" ::: "memory");
         }
-        if (warp == 10 && lane == 0) bar_arrive(smem_at(&s_bias_done));
+        if (w.tma_steps < w.steps) {
+          ++tails;
+          if (warp == 10 && lane == 0) bar_arrive(smem_at(&s_bias_done));
+        }
       }
       if (!alive && lane == 0) report(a.status, DGS_ETIMEOUT);
     }
@@ -544,7 +547,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSum));
     const uint32_t quarter = warp % 4, group = warp / 4;
     bool alive = true;
-    uint32_t it = 0, drained = 0, used = 0;   // used: bit s is the phase of s_free[s] to wait for
+    uint32_t it = 0, drained = 0, tails = 0, used = 0;   // tails: tiles with last rows of that kind so far; used: bit s is the phase of s_free[s] to wait for
     for (uint32_t ordinal = 0; ordinal < rounds && alive; ++ordinal) {
       const uint32_t tile = tile_in_round(ordinal, pair, pairs);
       if (tile >= a.tiles) break;
@@ -582,7 +585,9 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
           // here.  The thread of the copies waits for every phase of s_empty, and a stage has no second tail before this one is read.
           if (!(alive = warp_wait(smem_at(&s_free[last % ST]), used >> last % ST & 1))) break;
           used ^= 1u << last % ST;
-          if (ordinal && !(alive = warp_wait(smem_at(&s_bias_done), (ordinal - 1) & 1))) break;   // the table is free
+          // the table is free: both sides count tiles with such rows alone, so that no phase goes by without this wait
+          if (tails && !(alive = warp_wait(smem_at(&s_bias_done), (tails - 1) & 1))) break;
+          ++tails;
           float bias[8] = {};
 #pragma unroll
           for (uint32_t p = 0; p < P; ++p)

@@ -1,5 +1,5 @@
 """Weight gradients of experts at the lengths that the products' kernel treats apart: last steps that share a copy's rows with the next expert, at
-every place in a run of steps.  Sums of whole numbers are exact in f32 in any order, so results must come out bit for bit."""
+every place in a run of steps, and tiles without rows between others.  Sums of whole numbers are exact in f32 in any order, so results must come out bit for bit."""
 import pytest
 import torch
 
@@ -39,3 +39,18 @@ def test_last_steps_at_every_place_in_a_run(dtype, layout):
     """Experts of 5 to 45 steps of 64 rows, the last one never whole: it is any of the four or eight steps between two sums, and comes up to eight
     steps after the sums before.  All bias sums are one CTA's, which keeps its stages longest; more tiles than pairs of CTAs."""
     check([64 * (5 + e) + 1 + e for e in range(40)], 64, 300, dtype, layout, behind=70)
+
+
+# f32 2048 x 2048 takes two runs of rows a tile and 512 tiles for 74 pairs: those of 1 and 5 rows leave the second run empty between others
+@pytest.mark.parametrize("lengths,inputs,outputs,dtype,layout", [
+    ([30000, 1, 5, 16000], 2048, 2048, torch.float32, "out_in"), ([100, 100, 100, 30000], 2048, 768, torch.float32, "in_out"),
+    ([30000, 1, 5, 16000], 2048, 2048, torch.bfloat16, "out_in"), ([100, 100, 100, 30000], 2048, 768, torch.float16, "in_out")])
+def test_runs_without_rows_between_others(lengths, inputs, outputs, dtype, layout):
+    check(lengths, inputs, outputs, dtype, layout, behind=3)
+
+
+@pytest.mark.parametrize("layout", ["out_in", "in_out"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sixteen_experts_of_unequal_length_on_more_tiles_than_pairs(dtype, layout):
+    lengths = [0, 700, 3, 0, 1500, 64, 128, 1, 0, 2050, 129, 63, 640, 0, 31, 999]
+    check(lengths, 768, 700, dtype, layout, behind=5, scattered=True)
