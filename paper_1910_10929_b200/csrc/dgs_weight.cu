@@ -110,7 +110,7 @@ template <uint32_t P> struct Shape {
   static constexpr uint32_t kStage = kTile * (1 + P), kSmem = 1024 + kStages * kStage;
 };
 // Eight warps keep the sums, four do the rest and leave them their registers.
-constexpr uint32_t kThreads = 384, kRegsLaunch = 168, kRegsSum = 232, kRegsRest = 40;
+constexpr uint32_t kThreads = 384, kRegsLaunch = 168, kRegsSum = 224, kRegsRest = 56;
 static_assert(kRegsSum * 256 + kRegsRest * 128 <= kRegsLaunch * kThreads, "setmaxnreg draws on the launch's registers");
 template <uint32_t P>
 __device__ __forceinline__ uint32_t tile_at(uint32_t row, uint32_t piece) {   // piece: eight columns
@@ -397,7 +397,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
   using S = Shape<P>;
   constexpr uint32_t R = S::kRows, ST = S::kStages, CH = S::kChunk, STAGE = S::kStage, TILE = S::kTile, BLOCK = S::kColBlock;
   extern __shared__ unsigned char raw[];
-  __shared__ __align__(8) uint64_t s_full[ST], s_empty[ST], s_loaded[ST], s_sum_full[2], s_sum_empty[2], s_free[ST], s_tail, s_bias_done, s_done;
+  __shared__ __align__(8) uint64_t s_full[ST], s_empty[ST], s_loaded[ST], s_sum_full[2], s_sum_empty[2], s_free[ST], s_tail, s_bias_both, s_bias_done, s_done;
   __shared__ uint32_t s_tmem;
   __shared__ float s_bias[20 * kCols];   // rows 0 to 3: sums of the steps that came by TMA, 4 to 19: of the last step
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = cta_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2, rounds = (a.tiles + pairs - 1) / pairs;
@@ -418,6 +418,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
         bar_init(smem_at(&s_sum_empty[i]), 16);
       }
       bar_init(smem_at(&s_tail), 8);
+      bar_init(smem_at(&s_bias_both), 2);
       bar_init(smem_at(&s_bias_done), 1);
       bar_init(smem_at(&s_done), 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -496,6 +497,12 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
       const uint32_t t = tid - 320, br = t / 16, bv = t % 16;
       bool alive = true;
       uint32_t it = 0, tails = 0;
+      // Warps 10 and 11 wait for each other, twice a tile, and not for ever: one of them may have given up.
+      const auto both = [&](uint32_t parity) {
+        __syncwarp();
+        if (lane == 0) bar_arrive(smem_at(&s_bias_both));
+        return warp_wait(smem_at(&s_bias_both), parity);
+      };
       for (uint32_t round = 0; round < rounds && alive; ++round) {
         const uint32_t tile = tile_in_round(round, pair, pairs);
         if (tile >= a.tiles) break;   // in the last round only
@@ -523,10 +530,11 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
           __syncwarp();
           if (lane == 0) bar_arrive(smem_at(&s_empty[st]));
         }
-        if (w.bias && alive) {
+        if (!alive) break;
+        if (w.bias) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) s_bias[br * kCols + bv * 8 + i] = bias[i];
-          asm volatile("bar.sync 1, 64;" ::: "memory");
+          if (!(alive = both(0))) break;
           const uint32_t rows = w.tma_steps < w.steps && (w.steps - 1) % a.bias_tiles == w.ct ? 20 : 4;
           for (uint32_t c = t; c < grad_cols && w.go + c < a.outputs; c += 64) {
             float v = 0.0f;
@@ -534,7 +542,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
             float* p = a.db + (uint64_t(w.split * a.bias_tiles + w.ct) * a.experts + w.expert) * a.outputs + w.go + c;
             *p = a.add_b ? *p + v : v;
           }
-          asm volatile("bar.sync 1, 64;" ::: "memory");
+          if (!(alive = both(1))) break;
         }
         if (w.tma_steps < w.steps) {
           ++tails;
