@@ -464,8 +464,8 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
           if (s % CH == CH - 1 || s == w.steps - 1) mma_commit(smem_at(&s_sum_full[chunk++ & 1]));
         }
       }
-      mma_commit(smem_at(&s_done));   // nothing is under way when tensor memory is given back
-      if (!(bar_wait(smem_at(&s_done), 0) && alive)) report(a.status, DGS_ETIMEOUT);
+      mma_commit(smem_at(&s_done));   // waited for in both CTAs, at the end: nothing is under way when tensor memory is given back
+      if (!alive) report(a.status, DGS_ETIMEOUT);
     }
     if (warp == 9 && lane == 0) {
       const uint32_t code_blocks = (code_cols + 63) / 64, grad_blocks = (grad_cols + 63) / 64;
@@ -487,10 +487,12 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
               tma_load(to + (1 + p) * TILE + c * BLOCK, &grad_map, int(w.go + c * 64), int(p * a.plane_rows + w.first + uint64_t(s) * R), bar);
         }
       }
-      if (!alive) {   // copies that nobody waits for any more
-        report(a.status, DGS_ETIMEOUT);
-        for (uint32_t i = it > ST ? it - ST : 0; i < it; ++i) bar_wait(smem_at(&s_loaded[i % ST]), i / ST & 1);
+      // Nothing is under way to this CTA's memory when it leaves: its copies, and the arrivals that the products' commits send to both CTAs.
+      for (uint32_t i = it > ST ? it - ST : 0; i < it; ++i) {
+        const bool landed = bar_wait(smem_at(&s_loaded[i % ST]), i / ST & 1);
+        alive = alive && landed && bar_wait(smem_at(&s_empty[i % ST]), i / ST & 1);
       }
+      if (!alive) report(a.status, DGS_ETIMEOUT);
     }
     if (warp >= 10) {
       // 64 threads: eight columns of every fourth row
@@ -655,6 +657,9 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
   __syncwarp();
   tmem_before();
   __syncthreads();
+  // the commit behind the last products arrives in both CTAs: neither leaves before its own
+  if (warp == 8 && lane == 0 && !bar_wait(smem_at(&s_done), 0)) report(a.status, DGS_ETIMEOUT);
+  __syncwarp();
   pair_sync();
   if (warp == 8) {
     __syncwarp();
