@@ -33,6 +33,13 @@ __device__ __forceinline__ uint32_t in_leader(uint32_t bar) {
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// Likewise, and what threads of this CTA have written is there for a thread that has waited and then called bar_acquire_cluster.
+__device__ __forceinline__ void bar_release_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_acquire_cluster(uint32_t bar, uint32_t parity) {   // of a phase that is complete
+  asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n}\n" ::"r"(bar), "r"(parity) : "memory");
+}
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -448,6 +455,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
           if (s % CH == 0 && chunk >= 2) alive = bar_wait(smem_at(&s_sum_empty[chunk & 1]), (chunk / 2 - 1) & 1);
           alive = alive && bar_wait(smem_at(&s_full[st]), it / ST & 1);
           if (!alive) break;
+          if (s >= w.tma_steps) bar_acquire_cluster(smem_at(&s_full[st]), it / ST & 1);
           tmem_after();
           const uint32_t groups = min(R / 16, (w.count - s * R + 15) / 16);   // of sixteen rows: the last step may have fewer
 #pragma unroll
@@ -515,8 +523,18 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           const uint32_t st = it % ST;
           if (!(alive = warp_wait(smem_at(&s_loaded[st]), it / ST & 1))) break;
-          if (s >= w.tma_steps && warp == 10 && !(alive = warp_wait(smem_at(&s_tail), tails & 1))) break;
-          if (warp == 10 && lane == 0) bar_arrive_cluster(in_leader(smem_at(&s_full[st])));
+          if (warp == 10) {
+            const bool tail = s >= w.tma_steps;
+            if (tail && !(alive = warp_wait(smem_at(&s_tail), tails & 1))) break;
+            if (lane == 0) {
+              // what threads wrote is released to the other CTA, whose thread issues the products; for copies nothing need be (8192 x 768 x 50257: 1187 us
+              // with releases for them too, 853 so)
+              if (tail)
+                bar_release_cluster(in_leader(smem_at(&s_full[st])));
+              else
+                bar_arrive_cluster(in_leader(smem_at(&s_full[st])));
+            }
+          }
           if (w.bias && s < w.tma_steps && s % a.bias_tiles == w.ct) {
 #pragma unroll 4
             for (uint32_t r = br; r < R; r += 4) {
