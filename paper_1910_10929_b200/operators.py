@@ -191,11 +191,19 @@ class Route(NamedTuple):
 
 
 @functools.lru_cache(maxsize=64)
+def _router_of(k: int, score: int, groups: int, groups_kept: int, group_best: int, renormalise: bool, scale: float) -> "dgs.dgs_router":
+    return dgs.dgs_router(k, score, groups, groups_kept, group_best, renormalise, scale)
+
+
 def _router(k, score, groups, groups_kept, group_best, renormalise, scale) -> "dgs.dgs_router":
+    whole = []
     for v, what in ((k, "k"), (groups, "groups"), (groups_kept, "groups_kept"), (group_best, "group_best")):
-        if int(v) != v or not 0 < v < 1 << 31:
+        n = int(v)
+        if n != v or not 0 < n < 1 << 31:
             raise ValueError(f"{what} is a positive whole number: got {v!r}")
-    return dgs.dgs_router(int(k), _pick(_SCORE, score, "score"), int(groups), int(groups_kept), int(group_best), int(bool(renormalise)), float(scale))
+        whole.append(n)
+    # looked up by plain numbers: a tensor given for one may hold another value by the next call (+ 0.0: -0 and 0 are one key)
+    return _router_of(whole[0], _pick(_SCORE, score, "score"), *whole[1:], bool(renormalise), float(scale) + 0.0)
 
 
 def route_experts(logits: torch.Tensor, k: int, *, score: str = "softmax", bias: Optional[torch.Tensor] = None, groups: int = 1,
