@@ -455,7 +455,8 @@ int dgs_route_experts_grad(const dgs_router* router, const dgs_matrix* logits, c
                            const dgs_matrix* dlogits, void* stream);
 
 /* Waits for `stream` and stores in *device_status the lowest status that kernels of the calls above have left on the current device
- * since the last time it was read: 0, DGS_EINVAL (an index or list pointed outside its matrix) or DGS_ETIMEOUT (a bounded wait gave up). */
+ * since the last time it was read: 0, DGS_EINVAL (an index or list pointed outside its matrix) or DGS_ETIMEOUT (a bounded wait gave up).  The word is one
+ * for the device and is read and cleared in one step: a report is returned once, to whichever caller reads it first. */
 int dgs_operator_status(void* stream, int* device_status);
 
 /* Static text for a dgs_error value. */

@@ -2,11 +2,36 @@
 #include "dgs_operators.cuh"
 
 #include <algorithm>
+#include <atomic>
+#include <thread>
 
 namespace dgs {
 namespace {
 
 __device__ int g_operator_status;
+
+// Reading takes the word and clears it in one step, so that a report from another stream's kernel is returned by this reading or by a later one.
+// Readings under way have a place each for what they took.
+constexpr uint32_t kReadings = 64;
+__device__ int g_taken[kReadings];
+std::atomic<uint64_t> g_reading{0};   // bit i: place i is in use
+__global__ void k_status_take(uint32_t place) { g_taken[place] = atomicExch(&g_operator_status, 0); }
+struct Reading {
+  uint32_t place = 0;
+  Reading() {
+    uint64_t used = g_reading.load();
+    for (;;) {
+      if (used == ~0ull) {
+        std::this_thread::yield();
+        used = g_reading.load();
+        continue;
+      }
+      place = uint32_t(__builtin_ctzll(~used));
+      if (g_reading.compare_exchange_weak(used, used | 1ull << place)) return;
+    }
+  }
+  ~Reading() { g_reading.fetch_and(~(1ull << place)); }
+};
 
 // ---- activations and their slopes -------------------------------------------------------------
 // silu is x s(x), gelu_tanh x s(u) with u = 2 sqrt(2/pi) (x + 0.044715 x^3), s(u) = 1 / (1 + e^-u).  Slopes: s (1 + x u' (1 - s)).
@@ -358,9 +383,11 @@ extern "C" int dgs_checkpoint_activation_grad(const dgs_checkpoint* ckpt, int ac
 extern "C" int dgs_operator_status(void* stream, int* device_status) {
   if (!device_status) return DGS_EINVAL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  int word = 0, zero = 0;
-  if (cudaMemcpyFromSymbolAsync(&word, g_operator_status, sizeof(word), 0, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
-      cudaMemcpyToSymbolAsync(g_operator_status, &zero, sizeof(zero), 0, cudaMemcpyHostToDevice, st) != cudaSuccess)
+  const Reading reading;
+  int word = 0;
+  k_status_take<<<1, 1, 0, st>>>(reading.place);
+  if (cudaGetLastError() != cudaSuccess ||
+      cudaMemcpyFromSymbolAsync(&word, g_taken, sizeof(word), reading.place * sizeof(word), cudaMemcpyDeviceToHost, st) != cudaSuccess)
     return DGS_ECUDA;
   if (cudaStreamSynchronize(st) != cudaSuccess) return DGS_ECUDA;
   *device_status = word;
