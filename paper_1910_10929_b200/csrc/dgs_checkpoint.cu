@@ -71,9 +71,10 @@ __device__ __forceinline__ float act_slope(float x) {
   return 1.0f;
 }
 
-// For results of 16 bits, whose own rounding is 2^-9 or 2^-12 of them: the hardware's exponential and reciprocal, off by 2^-20 at most, two
-// numbers at a time where there is an instruction for it.  2^-24 e^-u takes the place of e^-u, so that r = 2^24 s is a normal number wherever x s is.
-// (32768 x 2048, gelu_tanh, with expf and divisions: 42 instructions a value, 104 us; so 22 and 66.)
+// silu and gelu_tanh for results of 16 bits, whose own rounding is 2^-9 or 2^-12 of them: the hardware's exponential and reciprocal, off by 2^-20 at most
+// beside the exponent's own roundings (3 |u| 2^-24), two numbers at a time where there is an instruction for it.  2^-24 e^-u takes the place of e^-u: its
+// reciprocal 2^24 s is not flushed to zero where x s still counts.  (32768 x 2048, gelu_tanh, with expf and divisions: 42 instructions a value, 104 us; so 22
+// and 66.)  gelu keeps erfcf in all types.
 __device__ __forceinline__ float clamp_nan(float x, float most) {   // NaN stays NaN
   asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(most));
   asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(-most));
@@ -97,7 +98,7 @@ __device__ __forceinline__ void values_of(float2 (&v)[4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (FAST && (ACT == DGS_ACT_SILU || ACT == DGS_ACT_GELU_TANH))
-      v[i] = mul2(mul2(v[i], both(0x1p-24f)), Scaled(exponent<ACT>(v[i])).r);
+      v[i] = mul2(v[i], mul2(Scaled(exponent<ACT>(v[i])).r, both(0x1p-24f)));   // s first: x 2^-24 of a small x would lose its digits
     else
       v[i] = make_float2(act_value<ACT>(v[i].x), act_value<ACT>(v[i].y));
   }
