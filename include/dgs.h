@@ -391,7 +391,7 @@ enum { DGS_WEIGHT_IN_OUT = 1u << 0, /* dw is [inputs][outputs]; without it [outp
 
 /* Which rows belong to which expert.  Row j of dy with offsets[e] <= j < offsets[e + 1] belongs to expert e and to
  * row rows[j] / rows_per of the checkpoint (to row j if rows is NULL).  Offsets ascend; where they do not, the gradients are
- * not specified. */
+ * not specified.  A row of dy in a list that names no row of the checkpoint takes no part in dw or db and is reported. */
 typedef struct {
   const uint32_t* offsets; /* DEVICE u32[experts + 1] */
   const uint32_t* rows;    /* DEVICE u32[rows of dy] or NULL */

@@ -142,7 +142,7 @@ struct WeightArgs {
   uint32_t in_out, bias_tiles, step_rows, tiles;
   const uint32_t* offsets;
   const uint32_t* rows;
-  uint32_t* order;          // experts by their number of rows, the longest first
+  uint32_t* order;          // experts by their number of rows, the longest first; then whether a row is left out
   __nv_bfloat16* decoded;   // [rows][h.width]: the checkpoint's values in dy's order, an expert's from expert_at(...) on
   float* dw;          // or the splits' partial results, [splits][experts][inputs * outputs]
   float* db;          // likewise, [splits * bias_tiles][experts][outputs]; NULL: not wanted
@@ -167,6 +167,11 @@ __device__ __forceinline__ void expert_rows(const WeightArgs& a, uint32_t expert
   }
 }
 
+// Whether row j of dy, which is in a list, names no row of the checkpoint: it is left out.
+__device__ __forceinline__ bool left_out(const WeightArgs& a, uint64_t j) {
+  return a.rows ? a.rows[j] >= a.h.rows * a.rows_per : j >= a.h.rows;
+}
+
 // ---- the checkpoint's values as bfloat16 numbers ------------------------------------------------------
 // They are that exactly, so nothing is lost.  Decoding inside the products' kernel, by the warps that keep the sums, cost more than it saved:
 // every tile of 256 outputs decodes again, and eight warps (all that the sums' registers leave room for) took 1.05 us a step of 128 rows where
@@ -175,10 +180,22 @@ constexpr uint32_t kDecodeRows = 16;   // of a CTA
 template <bool FLOAT8>
 __global__ void __launch_bounds__(256) k_weight_decode(const __grid_constant__ WeightArgs a) {
   let_next_kernel_begin();
-  const uint64_t at = uint64_t(blockIdx.x) * kDecodeRows;   // row of the decoded values
+  const uint64_t at = uint64_t(blockIdx.x - (a.offsets ? 1 : 0)) * kDecodeRows;   // row of the decoded values
   uint64_t first = 0, last = a.dy_rows, begin = 0;
-  if (a.offsets && blockIdx.x == gridDim.x - 1) {   // one CTA more: who comes before whom
+  if (a.offsets && blockIdx.x == 0) {   // one CTA more, the first, as it takes long: who comes before whom, and whether all rows are there
     __shared__ uint32_t s_rows[DGS_ROUTE_MAX_EXPERTS];
+    uint64_t from, to, x;
+    expert_rows(a, 0, &from, &x, false);
+    expert_rows(a, a.experts - 1, &x, &to, false);
+    bool out = false;
+    for (uint64_t j = from + threadIdx.x; j < to; j += 8 * 256)
+#pragma unroll
+      for (uint32_t k = 0; k < 8; ++k) out |= j + k * 256 < to && left_out(a, j + k * 256);
+    out = __syncthreads_or(out);
+    if (threadIdx.x == 0) {
+      a.order[a.experts] = out;
+      if (out) report(a.status, DGS_EINVAL);
+    }
     for (uint32_t e = threadIdx.x; e < a.experts; e += 256) {
       expert_rows(a, e, &first, &last, true);
       s_rows[e] = uint32_t(last - first);
@@ -219,10 +236,7 @@ __global__ void __launch_bounds__(256) k_weight_decode(const __grid_constant__ W
     if (row0 + threadIdx.x < rows) {
       src = uint32_t(first + row0) + threadIdx.x;
       if (a.rows) src = a.rows[src] / a.rows_per;
-      if (src >= a.h.rows) {
-        report(a.status, DGS_EINVAL);
-        src = kNone;
-      }
+      if (src >= a.h.rows) src = kNone;
     }
     s_src[threadIdx.x] = src;
   }
@@ -369,7 +383,7 @@ struct TileOf {
 __device__ __forceinline__ uint32_t tile_in_round(uint32_t round, uint32_t pair, uint32_t pairs) {
   return round * pairs + (round & 1 ? pairs - 1 - pair : pair);
 }
-template <uint32_t R>
+template <uint32_t R, bool LISTS>
 __device__ __forceinline__ TileOf tile_of(const WeightArgs& a, uint32_t tile, uint32_t rank) {
   TileOf t;
   t.ct = tile % a.code_tiles;
@@ -378,14 +392,15 @@ __device__ __forceinline__ TileOf tile_of(const WeightArgs& a, uint32_t tile, ui
   tile /= a.grad_tiles;
   t.split = tile % a.splits;
   t.expert = tile / a.splits;
-  if (a.order) t.expert = a.order[t.expert];
+  if (LISTS && a.order) t.expert = a.order[t.expert];
   t.i0 = t.ct * (a.in_out ? a.n : 256);
   t.o0 = gt * (a.in_out ? 256 : a.n);
   t.ci = t.i0 + rank * (a.in_out ? a.n / 2 : kCols);
   t.go = t.o0 + rank * (a.in_out ? kCols : a.n / 2);
   uint64_t first, last;
-  expert_rows(a, t.expert, &first, &last, false);
-  t.held_first = a.offsets ? expert_at(first, t.expert, R) : 0;
+  if constexpr (LISTS) expert_rows(a, t.expert, &first, &last, false);
+  else first = 0, last = a.dy_rows;
+  t.held_first = LISTS ? expert_at(first, t.expert, R) : 0;
   const uint64_t all = (last - first + R - 1) / R, each = (all + a.splits - 1) / a.splits, from = min(first + t.split * each * R, last);
   last = min(from + each * R, last);
   t.held_first += from - first;
@@ -393,12 +408,13 @@ __device__ __forceinline__ TileOf tile_of(const WeightArgs& a, uint32_t tile, ui
   t.count = uint32_t(last - from);
   t.steps = (t.count + (R - 1)) / R;
   // the last step's gradients come by TMA only where nothing but the end of the matrix follows
-  t.tma_steps = t.count % R == 0 || last == a.dy_rows ? t.steps : t.steps - 1;
+  t.tma_steps = !LISTS || t.count % R == 0 || last == a.dy_rows ? t.steps : t.steps - 1;
   t.bias = a.db != nullptr && t.ct < a.bias_tiles;
   return t;
 }
 
-template <uint32_t P>
+// LISTS: with them, and the code for rows that are not brought by copies alone (8192 x 768 x 2304 without lists: 49 us a call, 55 with that code there).
+template <uint32_t P, bool LISTS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUtensorMap held_map, const __grid_constant__ CUtensorMap grad_map) {
   using S = Shape<P>;
@@ -438,6 +454,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
   tmem_after();
   const uint32_t tmem = s_tmem;
   wait_for_last_kernel();   // nothing above touches memory outside the SM
+  const bool skips = LISTS && a.order && a.order[a.experts];   // rows of the gradient become zeros on their way
 
   // Every role goes through the tiles by itself; it counts steps and chunks over all of them, which is what the barriers' phases go by.
   __syncwarp();
@@ -449,13 +466,14 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
       for (uint32_t round = 0; round < rounds && alive; ++round) {
         const uint32_t tile = tile_in_round(round, pair, pairs);
         if (tile >= a.tiles) break;   // in the last round only
-        const TileOf w = tile_of<R>(a, tile, rank);
+        const TileOf w = tile_of<R, LISTS>(a, tile, rank);
+        const uint32_t written = skips ? 0 : w.tma_steps;
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           const uint32_t st = it % ST, code = tiles + st * STAGE, grad = code + TILE, acc = tmem + (chunk & 1) * 256;
           if (s % CH == 0 && chunk >= 2) alive = bar_wait(smem_at(&s_sum_empty[chunk & 1]), (chunk / 2 - 1) & 1);
           alive = alive && bar_wait(smem_at(&s_full[st]), it / ST & 1);
           if (!alive) break;
-          if (s >= w.tma_steps) bar_acquire_cluster(smem_at(&s_full[st]), it / ST & 1);
+          if (s >= written) bar_acquire_cluster(smem_at(&s_full[st]), it / ST & 1);
           tmem_after();
           const uint32_t groups = min(R / 16, (w.count - s * R + 15) / 16);   // of sixteen rows: the last step may have fewer
 #pragma unroll
@@ -482,7 +500,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
       for (uint32_t round = 0; round < rounds && alive; ++round) {
         const uint32_t tile = tile_in_round(round, pair, pairs);
         if (tile >= a.tiles) break;   // in the last round only
-        const TileOf w = tile_of<R>(a, tile, rank);
+        const TileOf w = tile_of<R, LISTS>(a, tile, rank);
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           const uint32_t st = it % ST, to = tiles + st * STAGE, bar = smem_at(&s_loaded[st]), grads = s < w.tma_steps ? grad_blocks : 0;
           if (it >= ST && !(alive = bar_wait(smem_at(&s_empty[st]), (it / ST - 1) & 1))) break;
@@ -506,34 +524,40 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
       // 64 threads: eight columns of every fourth row
       const uint32_t t = tid - 320, br = t / 16, bv = t % 16;
       bool alive = true;
-      uint32_t it = 0, tails = 0;
-      // Warps 10 and 11 wait for each other, twice a tile, and not for ever: one of them may have given up.
-      const auto both = [&](uint32_t parity) {
+      uint32_t it = 0, tails = 0, met = 0;
+      // Warps 10 and 11 wait for each other, and not for ever: one of them may have given up.
+      const auto both = [&] {
         __syncwarp();
         if (lane == 0) bar_arrive(smem_at(&s_bias_both));
-        return warp_wait(smem_at(&s_bias_both), parity);
+        return warp_wait(smem_at(&s_bias_both), met++ & 1);
       };
       for (uint32_t round = 0; round < rounds && alive; ++round) {
         const uint32_t tile = tile_in_round(round, pair, pairs);
         if (tile >= a.tiles) break;   // in the last round only
-        const TileOf w = tile_of<R>(a, tile, rank);
+        const TileOf w = tile_of<R, LISTS>(a, tile, rank);
+        const uint32_t written = skips ? 0 : w.tma_steps;   // from here on threads write to the stages
         float bias[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           const uint32_t st = it % ST;
           if (!(alive = warp_wait(smem_at(&s_loaded[st]), it / ST & 1))) break;
-          if (warp == 10) {
-            const bool tail = s >= w.tma_steps;
-            if (tail && !(alive = warp_wait(smem_at(&s_tail), tails & 1))) break;
-            if (lane == 0) {
-              // what threads wrote is released to the other CTA, whose thread issues the products; for copies nothing need be (8192 x 768 x 50257: 1187 us
-              // with releases for them too, 853 so)
-              if (tail)
-                bar_release_cluster(in_leader(smem_at(&s_full[st])));
-              else
-                bar_arrive_cluster(in_leader(smem_at(&s_full[st])));
+          if (s >= written) {   // rare; what threads wrote is released to the other CTA, whose thread issues the products
+            if (s < w.tma_steps) {
+#pragma unroll 1
+              for (uint32_t r = t; r < R && s * R + r < w.count; r += 64)
+                if (left_out(a, w.first + s * R + r))
+#pragma unroll 1
+                  for (uint32_t i = 0; i < P * 16; ++i)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tiles + st * STAGE + (1 + i / 16) * TILE + tile_at<P>(r, i % 16)), "r"(0) : "memory");
+              writes_to_async_proxy();
+              if (!(alive = both())) break;
+            } else if (warp == 10 && !(alive = warp_wait(smem_at(&s_tail), tails & 1))) {
+              break;
             }
+            if (warp == 10 && lane == 0) bar_release_cluster(in_leader(smem_at(&s_full[st])));
+          } else if (warp == 10 && lane == 0) {   // for copies nothing need be released (8192 x 768 x 50257: 1187 us if it is, 853 so)
+            bar_arrive_cluster(in_leader(smem_at(&s_full[st])));
           }
           if (w.bias && s < w.tma_steps && s % a.bias_tiles == w.ct) {
 #pragma unroll 4
@@ -554,7 +578,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
         if (w.bias) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) s_bias[br * kCols + bv * 8 + i] = bias[i];
-          if (!(alive = both(0))) break;
+          if (!(alive = both())) break;
           const uint32_t rows = w.tma_steps < w.steps && (w.steps - 1) % a.bias_tiles == w.ct ? 20 : 4;
           for (uint32_t c = t; c < grad_cols && w.go + c < a.outputs; c += 64) {
             float v = 0.0f;
@@ -562,7 +586,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
             float* p = a.db + (uint64_t(w.split * a.bias_tiles + w.ct) * a.experts + w.expert) * a.outputs + w.go + c;
             *p = a.add_b ? *p + v : v;
           }
-          if (!(alive = both(1))) break;
+          if (!(alive = both())) break;
         }
         if (w.tma_steps < w.steps) {
           ++tails;
@@ -579,13 +603,13 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
     for (uint32_t ordinal = 0; ordinal < rounds && alive; ++ordinal) {
       const uint32_t tile = tile_in_round(ordinal, pair, pairs);
       if (tile >= a.tiles) break;
-      const TileOf w = tile_of<R>(a, tile, rank);
+      const TileOf w = tile_of<R, LISTS>(a, tile, rank);
       const uint32_t chunks = (w.steps + CH - 1) / CH;
       float acc[128];
 #pragma unroll
       for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
       for (uint32_t c = 0; c < chunks; ++c, ++drained) {
-        if (c + 1 == chunks && w.tma_steps < w.steps) {
+        if (LISTS && c + 1 == chunks && w.tma_steps < w.steps) {
           // an expert's last rows: eight columns of every sixteenth row a thread, zeros behind them.  What is read is on its way before the stage is
           // free; sixteen rows that no product takes are left out.
           const uint32_t last = it + w.steps - 1, at = tiles + last % ST * STAGE + TILE, gr = tid / 16, gv = tid % 16, col = w.go + gv * 8;
@@ -597,7 +621,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
 #pragma unroll
             for (uint32_t u = 0; u < R / 16; ++u, from += 16 * a.dy_stride) {
               v[p][u] = make_uint4(0, 0, 0, 0);
-              if (j0 + 16 * u < w.count && col < a.outputs) {
+              if (j0 + 16 * u < w.count && col < a.outputs && !(skips && left_out(a, w.first + j0 + 16 * u))) {
                 if (col + 8 <= a.outputs) {
                   v[p][u] = __ldg(reinterpret_cast<const uint4*>(from));
                 } else {
@@ -743,13 +767,14 @@ __global__ void __launch_bounds__(256) k_weight_small(const __grid_constant__ We
     uint32_t src = uint32_t(first) + j;
     const T* g = dy + (first + j) * a.dy_stride + grad_col;
     if (a.rows) src = a.rows[src] / a.rows_per;
-    if (src >= a.h.rows) {
+    if (src >= a.h.rows) {   // left out
       report(a.status, DGS_EINVAL);
-    } else if (held_col < a.h.width) {
+      return;
+    }
+    if (held_col < a.h.width) {
       code = *reinterpret_cast<const uint32_t*>(a.h.codes + uint64_t(src) * a.h.width + held_col);
       scale = a.h.scales[uint64_t(src) * a.h.spitch + held_col / 32];
     }
-    // a row that names no row of the checkpoint still counts for the bias of its own, as in the other kernel
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (grad_col + i < a.outputs) grad[i] = Elem<T>::get(g[i]);
@@ -852,7 +877,7 @@ int plan_weight(const dgs_checkpoint* c, const dgs_matrix* dy, const dgs_row_lis
   p->plane_rows = p->direct ? dy->rows : (dy->rows + p->step_rows - 1) / p->step_rows * p->step_rows + p->step_rows;   // a step may begin on the last row
   p->planes = p->direct ? 0 : p->parts * p->plane_rows * p->stride * 2;
   p->decoded = dy->rows ? decoded_rows(dy->rows, lists ? p->experts : 0, p->step_rows) * held_width(c->cols) * 2 : 0;
-  p->order = lists && dy->rows ? (uint64_t(p->experts) * 4 + 15) / 16 * 16 : 0;
+  p->order = lists && dy->rows ? (uint64_t(p->experts + 1) * 4 + 15) / 16 * 16 : 0;
   p->bytes = p->decoded + p->planes + p->order + (p->splits > 1 ? p->nw * p->splits * 4 : 0) + (parts_b > 1 ? p->nb * parts_b * 4 : 0);
   return DGS_OK;
 }
@@ -861,19 +886,21 @@ constexpr int kMaxDevices = 64;
 std::mutex g_weight_mu;
 bool g_weight_ready[kMaxDevices];
 PFN_cuTensorMapEncodeTiled_v12000 g_encode;   // written once, under the mutex
-template <uint32_t P>
+template <uint32_t P, bool LISTS>
 bool weight_setup() {
   cudaFuncAttributes f;
   // the split of the registers counts on what the launch brings
-  return cudaFuncGetAttributes(&f, k_weight_grad<P>) == cudaSuccess && uint32_t(f.numRegs) >= kRegsLaunch &&
-         cudaFuncSetAttribute(k_weight_grad<P>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<P>::kSmem) == cudaSuccess;
+  return cudaFuncGetAttributes(&f, k_weight_grad<P, LISTS>) == cudaSuccess && uint32_t(f.numRegs) >= kRegsLaunch &&
+         cudaFuncSetAttribute(k_weight_grad<P, LISTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<P>::kSmem) == cudaSuccess;
 }
 int weight_ready() {   // once per device
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return DGS_ECUDA;
   std::lock_guard<std::mutex> lock(g_weight_mu);
   if (!g_weight_ready[dev]) {
-    if (!weight_setup<1>() || !weight_setup<2>() || !weight_setup<3>()) return DGS_ECUDA;
+    if (!weight_setup<1, false>() || !weight_setup<2, false>() || !weight_setup<3, false>() || !weight_setup<1, true>() || !weight_setup<2, true>() ||
+        !weight_setup<3, true>())
+      return DGS_ECUDA;
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult found;
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess || !fn) return DGS_ECUDA;
@@ -895,7 +922,7 @@ int make_map(const void* data, uint64_t rows, uint64_t cols, uint64_t stride, ui
 template <uint32_t P>
 int launch(const WeightArgs& a, const CUtensorMap& held, const CUtensorMap& grad, cudaStream_t st) {
   const EarlyLaunch l(dim3(std::min(a.tiles, kSms / 2) * 2), kThreads, Shape<P>::kSmem, st);
-  return cudaLaunchKernelEx(&l.cfg, k_weight_grad<P>, a, held, grad) == cudaSuccess ? DGS_OK : DGS_ECUDA;
+  return cudaLaunchKernelEx(&l.cfg, a.offsets ? k_weight_grad<P, true> : k_weight_grad<P, false>, a, held, grad) == cudaSuccess ? DGS_OK : DGS_ECUDA;
 }
 
 }  // namespace

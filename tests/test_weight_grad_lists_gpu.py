@@ -54,3 +54,42 @@ def test_runs_without_rows_between_others(lengths, inputs, outputs, dtype, layou
 def test_sixteen_experts_of_unequal_length_on_more_tiles_than_pairs(dtype, layout):
     lengths = [0, 700, 3, 0, 1500, 64, 128, 1, 0, 2050, 129, 63, 640, 0, 31, 999]
     check(lengths, 768, 700, dtype, layout, behind=5, scattered=True)
+
+
+@pytest.mark.parametrize("layout", ["out_in", "in_out"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths,inputs,outputs,named", [([20, 0, 30], 70, 40, True), ([20, 0, 30], 70, 40, False), ([700, 90, 1, 300], 40, 72, True),
+                                                          ([700, 90, 1, 300], 40, 72, False), ([20000, 130], 96, 300, True)])
+def test_rows_that_name_no_row_of_the_checkpoint_take_no_part(lengths, inputs, outputs, named, dtype, layout):
+    """Neither in dw nor in db, whatever they hold: NaN, infinities and large numbers of dy stay out.  named: by rows; otherwise dy has more rows than the
+    checkpoint.  In whole steps and in last ones, in one run of rows and in several."""
+    g = torch.Generator(device=DEV).manual_seed(len(lengths))
+    n, experts, k = sum(lengths), len(lengths), 3
+    held = n if named else n - 17
+    x = torch.randint(-7, 8, (held, inputs), generator=g, device=DEV).float()
+    dy = torch.randint(-8, 9, (n + 4, outputs), generator=g, device=DEV).to(dtype)
+    c = dgs.Checkpoint(held, inputs, device=DEV)
+    c.save(x)
+    rows, there = None, torch.arange(n, device=DEV) < held
+    at = torch.arange(n, device=DEV)
+    if named:
+        at = torch.randint(0, held, (n,), generator=g, device=DEV)
+        rows = torch.cat([at * k + 1, torch.tensor([-1, held * k, 0, -5], device=DEV)]).to(torch.int32)   # behind the last list: not looked at
+        out = torch.rand(n, generator=g, device=DEV) < 0.05
+        out[[0, lengths[0] - 1, n - 1]] = True
+        there = ~out
+        bad = torch.tensor([held * k, -1, -(1 << 31)], device=DEV).to(torch.int32)
+        rows[:n] = torch.where(out, bad[at % 3], rows[:n])
+    dy[:n][~there] = torch.tensor([float("nan"), float("inf"), -float("inf"), 60000.0], device=DEV).to(dtype)[torch.arange(int((~there).sum()), device=DEV) % 4][:, None]
+    dy[n:] = float("nan")
+    offsets = torch.tensor([0] + lengths).cumsum(0).to(torch.int32).to(DEV)
+    shape = (experts, outputs, inputs) if layout == "out_in" else (experts, inputs, outputs)
+    dw, db = torch.full(shape, float("nan"), device=DEV), torch.full((experts, outputs), float("nan"), device=DEV)
+    c.weight_grad(dy, dw, db, layout=layout, offsets=offsets, rows=rows, rows_per=k if named else 1)
+    assert dgs.operator_status(DEV) == dgs.DGS_EINVAL and dgs.operator_status(DEV) == 0
+    cut = offsets.tolist()
+    for e in range(experts):
+        part = torch.arange(cut[e], cut[e + 1], device=DEV)
+        part = part[there[part]]
+        d, h = dy[part].double(), x[at[part]].double()
+        assert torch.equal(dw[e].double(), d.T @ h if layout == "out_in" else h.T @ d) and torch.equal(db[e].double(), d.sum(0)), e
