@@ -405,7 +405,7 @@ typedef struct {
  * or NULL.  inputs = ckpt->cols, outputs = dy->cols.  With lists, one such gradient per expert over the expert's rows,
  * dw [experts][...] and db [experts][outputs]; an expert without rows gets zeros.  Without lists (NULL) dy has the
  * checkpoint's rows.  Products are exact and are summed in f32 (f16 and f32 gradients are taken apart into bfloat16
- * numbers whose sum they are).  A row of dy that is in no list has no part in anything.  At most DGS_ROUTE_MAX_EXPERTS experts.
+ * numbers whose sum they are; of an f32 gradient below 2^-110 what lies under 2^-133, the last bit of a bfloat16 number, may be lost).  A row of dy that is in no list has no part in anything.  At most DGS_ROUTE_MAX_EXPERTS experts.
  * workspace: DEVICE, 16-byte aligned, at least what dgs_checkpoint_weight_grad_bytes says for these arguments (data pointers
  * included: their alignment counts).  It takes the checkpoint's values as bfloat16 numbers (2 bytes a value for each row of dy), dy as
  * bfloat16 numbers unless it is that with rows on 16 bytes (2 bytes a value, fp16 4, f32 6), and partial results where

@@ -282,6 +282,7 @@ __device__ __forceinline__ uint32_t upper(float v, float* rest) {
   *rest = finite ? v - __uint_as_float(b) : 0.0f;
   return b;
 }
+// Three of them hold a float's 24 bits, as far as bfloat16's last bit, 2^-133: every float of at least 2^-110.
 template <class T> constexpr uint32_t kParts = std::is_same_v<T, float> ? 3 : std::is_same_v<T, __half> ? 2 : 1;
 
 // 16 bytes from the off-th on of two words.
