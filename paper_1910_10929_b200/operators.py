@@ -52,10 +52,18 @@ def _matrix(t: torch.Tensor, what: str) -> "dgs.dgs_matrix":
     else:
         if not shape:
             raise ValueError(f"{what} needs a last dimension")
-        if len(shape) > 2 and not t.is_contiguous():
-            raise ValueError(f"{what} has more than two dimensions and is not contiguous")
         cols = shape[-1]
         rows, stride, step = t.numel() // cols if cols else 0, cols, t.stride(-1)
+        if rows > 1 and not t.is_contiguous():
+            stride, run = None, 1                        # the rows so far: `run` of them, `stride` apart
+            for n, s in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
+                if n == 1:
+                    continue
+                if stride is None:
+                    stride = s
+                elif s != stride * run:
+                    raise ValueError(f"{what}: the rows of all but the last dimension must lie evenly spaced (shape {tuple(shape)}, strides {t.stride()})")
+                run *= n
     if step != 1 and cols > 1 and rows:
         raise ValueError(f"{what}: neighbours in the last dimension must be neighbours in memory (stride {step})")
     return dgs.dgs_matrix(t.data_ptr(), rows, stride if rows > 1 else cols, cols, kind)

@@ -20,3 +20,21 @@ def test_a_router_is_made_from_the_values_that_arguments_have_now():
             operators._router(bad, "softmax", 1, 1, 1, True, 1.0)
     with pytest.raises(ValueError):
         operators._router(2, "relu", 1, 1, 1, True, 1.0)
+
+
+def test_views_of_more_dimensions_whose_rows_lie_evenly_spaced(monkeypatch):
+    monkeypatch.setattr(operators, "_on_gpu", lambda t, what: None)
+    whole = torch.arange(2 * 3 * 5 * 24, dtype=torch.float32).view(2, 3, 5, 24)
+    even = [whole, whole[..., 3:11], whole[:, :, :, :1], whole[:, :, 2:3, :8], whole[1:, 1:2, ::2, :8], whole[1:, :, :, 4:], whole[:1, :1, :1, 5:9],
+            whole[0, 0, 0], whole[0, 0, 0, :1].expand(4, 3, 1), whole[0, 0, :1, :7].expand(6, 2, 5, 7), whole[:0, :, 1:], whole[:1, 2:, :, :5].transpose(0, 1),
+            whole.view(6, 5, 24)[:, :, 8:16]]
+    for v in even:
+        m = operators._matrix(v, "v")
+        assert m.rows * m.cols == v.numel() and m.cols == v.shape[-1]
+        if v.numel():
+            at = v.storage_offset() + torch.arange(m.rows)[:, None] * m.stride + torch.arange(m.cols)
+            assert torch.equal(whole.reshape(-1)[at], v.reshape(-1, v.shape[-1])) and m.data == v.data_ptr()
+    for v in (whole[:, :, :3, :8], whole[:, :2], whole[:, 1:2, ::2, :8], whole[:, 2:, :, :5].transpose(0, 1), whole.transpose(0, 1), whole.transpose(2, 3), whole[..., ::2], whole[:, :1].expand(2, 4, 5, 24),
+              whole[0, 0, :, :7].expand(6, 5, 7)):
+        with pytest.raises(ValueError):
+            operators._matrix(v, "v")
