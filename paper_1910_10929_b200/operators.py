@@ -4,12 +4,14 @@ activations held in 8 bits and the gradients formed from them, and the router of
 Outputs and workspaces are torch tensors of the inputs' device, and work is enqueued on that device's current
 stream, whichever device is current for the caller; as with torch's own operators, a tensor used on another stream
 than the one it was made on has to be ordered and recorded by the caller.  Nothing waits for the GPU.  They are not
-part of torch's differentiation: a backward pass calls them by name.  Arguments that do not fit raise ValueError
+part of torch's differentiation: a backward pass calls them by name.  Where torch would record a call's result (an activation, a router's
+weights), the call warns that it is cut off.  Arguments that do not fit raise ValueError
 before any work is enqueued, what the library refuses raises DgsError.
 """
 from __future__ import annotations
 
 import functools
+import warnings
 from typing import NamedTuple, Optional
 
 import torch
@@ -85,6 +87,12 @@ def _same_device(device, *tensors) -> None:
             raise ValueError(f"tensors of one call must be on one device: {device} and {t.device}")
 
 
+def _cut_off(t: torch.Tensor, what: str, call: str) -> None:
+    if t.requires_grad and torch.is_grad_enabled():
+        warnings.warn(f"{what} requires a gradient, but what {call} returns is cut off from torch's differentiation: the backward pass calls "
+                      "the gradient by name. Detach the argument, or call under torch.no_grad().", stacklevel=3)
+
+
 def _enqueue(device, call, *args) -> None:
     """call(*args, stream) with the device current and its current stream."""
     index = device.index
@@ -135,6 +143,8 @@ class Checkpoint:
         mx = self._fit(x, "x")
         if activation is None and out is not None:
             raise ValueError("out needs an activation")
+        if activation is not None:
+            _cut_off(x, "x", "Checkpoint.save")
         if activation is not None and out is None:
             out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         my = None
@@ -219,6 +229,7 @@ def route_experts(logits: torch.Tensor, k: int, *, score: str = "softmax", bias:
     """Chooses k experts for every token (dgs_route_experts): by softmax or sigmoid of the logits plus `bias`, in the `groups_kept` best of
     `groups` groups, ties to the lowest index; with the experts' lists of slots."""
     m = _matrix(logits, "logits")
+    _cut_off(logits, "logits", "route_experts")
     router = _router(k, score, groups, groups_kept, group_best, renormalise, scale)
     tokens, experts, device = m.rows, m.cols, logits.device
     pb = _plain(bias, "bias", torch.float32, experts, device)
