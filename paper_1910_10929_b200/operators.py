@@ -209,19 +209,27 @@ class Route(NamedTuple):
 
 
 @functools.lru_cache(maxsize=64)
-def _router_of(k: int, score: int, groups: int, groups_kept: int, group_best: int, renormalise: bool, scale: float) -> "dgs.dgs_router":
-    return dgs.dgs_router(k, score, groups, groups_kept, group_best, renormalise, scale)
+def _router_of(k: int, score: str, groups: int, groups_kept: int, group_best: int, renormalise: bool, scale: float) -> "dgs.dgs_router":
+    for v, what in ((k, "k"), (groups, "groups"), (groups_kept, "groups_kept"), (group_best, "group_best")):
+        if not 0 < v < 1 << 31:
+            raise ValueError(f"{what} is a positive whole number: got {v!r}")
+    return dgs.dgs_router(k, _pick(_SCORE, score, "score"), groups, groups_kept, group_best, renormalise, scale)
+
+
+def _whole(v, what) -> int:
+    n = int(v)
+    if n != v:
+        raise ValueError(f"{what} is a positive whole number: got {v!r}")
+    return n
 
 
 def _router(k, score, groups, groups_kept, group_best, renormalise, scale) -> "dgs.dgs_router":
-    whole = []
-    for v, what in ((k, "k"), (groups, "groups"), (groups_kept, "groups_kept"), (group_best, "group_best")):
-        n = int(v)
-        if n != v or not 0 < n < 1 << 31:
-            raise ValueError(f"{what} is a positive whole number: got {v!r}")
-        whole.append(n)
-    # looked up by plain numbers: a tensor given for one may hold another value by the next call (+ 0.0: -0 and 0 are one key)
-    return _router_of(whole[0], _pick(_SCORE, score, "score"), *whole[1:], bool(renormalise), float(scale) + 0.0)
+    # Looked up by plain numbers: a tensor given for one may hold another value by the next call.  (Made anew each time: 1 us; + 0.0: -0 and 0 are one key.)
+    if not (type(k) is type(groups) is type(groups_kept) is type(group_best) is int and type(score) is str and type(renormalise) is bool and type(scale) is float):
+        k, groups, groups_kept, group_best = _whole(k, "k"), _whole(groups, "groups"), _whole(groups_kept, "groups_kept"), _whole(group_best, "group_best")
+        _pick(_SCORE, score, "score")
+        renormalise, scale = bool(renormalise), float(scale)
+    return _router_of(k, score, groups, groups_kept, group_best, renormalise, scale + 0.0)
 
 
 def route_experts(logits: torch.Tensor, k: int, *, score: str = "softmax", bias: Optional[torch.Tensor] = None, groups: int = 1,
