@@ -117,7 +117,7 @@ template <uint32_t P> struct Shape {
   static constexpr uint32_t kStage = kTile * (1 + P), kSmem = 1024 + kStages * kStage;
 };
 // Eight warps keep the sums, four do the rest and leave them their registers.
-constexpr uint32_t kThreads = 384, kRegsLaunch = 168, kRegsSum = 224, kRegsRest = 56;
+constexpr uint32_t kThreads = 384, kRegsLaunch = 168, kRegsSum = 216, kRegsRest = 72;
 static_assert(kRegsSum * 256 + kRegsRest * 128 <= kRegsLaunch * kThreads, "setmaxnreg draws on the launch's registers");
 template <uint32_t P>
 __device__ __forceinline__ uint32_t tile_at(uint32_t row, uint32_t piece) {   // piece: eight columns
@@ -139,10 +139,10 @@ struct WeightArgs {
   uint64_t dy_rows, dy_stride, plane_rows;
   uint32_t inputs, outputs, code_tiles, grad_tiles, splits, experts, rows_per;
   uint32_t n;           // columns of the operand that the pair shares out: 64 .. 256
-  uint32_t in_out, bias_tiles, step_rows, tiles;
+  uint32_t in_out, bias_tiles, step_rows, tiles, scans;
   const uint32_t* offsets;
   const uint32_t* rows;
-  uint32_t* order;          // experts by their number of rows, the longest first; then whether a row is left out
+  uint32_t* order;          // experts by their number of rows, the longest first; then, for each kScanRows rows of dy, whether one is left out
   __nv_bfloat16* decoded;   // [rows][h.width]: the checkpoint's values in dy's order, an expert's from expert_at(...) on
   float* dw;          // or the splits' partial results, [splits][experts][inputs * outputs]
   float* db;          // likewise, [splits * bias_tiles][experts][outputs]; NULL: not wanted
@@ -176,26 +176,31 @@ __device__ __forceinline__ bool left_out(const WeightArgs& a, uint64_t j) {
 // They are that exactly, so nothing is lost.  Decoding inside the products' kernel, by the warps that keep the sums, cost more than it saved:
 // every tile of 256 outputs decodes again, and eight warps (all that the sums' registers leave room for) took 1.05 us a step of 128 rows where
 // the products take 0.68 (32768 x 2048 x 2048: 257 us, 174 without decoding).
-constexpr uint32_t kDecodeRows = 16;   // of a CTA
+constexpr uint32_t kDecodeRows = 16, kScanRows = 4096;   // of a CTA
 template <bool FLOAT8>
 __global__ void __launch_bounds__(256) k_weight_decode(const __grid_constant__ WeightArgs a) {
   let_next_kernel_begin();
-  const uint64_t at = uint64_t(blockIdx.x - (a.offsets ? 1 : 0)) * kDecodeRows;   // row of the decoded values
+  const uint32_t ahead = a.scans ? a.scans + 1 : 0;                       // CTAs before those that decode
+  const uint64_t at = uint64_t(blockIdx.x - ahead) * kDecodeRows;   // row of the decoded values
   uint64_t first = 0, last = a.dy_rows, begin = 0;
-  if (a.offsets && blockIdx.x == 0) {   // one CTA more, the first, as it takes long: who comes before whom, and whether all rows are there
-    __shared__ uint32_t s_rows[DGS_ROUTE_MAX_EXPERTS];
+  if (blockIdx.x < a.scans) {   // whether all of dy's rows in lists name one of the checkpoint
     uint64_t from, to, x;
     expert_rows(a, 0, &from, &x, false);
     expert_rows(a, a.experts - 1, &x, &to, false);
+    from = max(from, uint64_t(blockIdx.x) * kScanRows), to = min(to, uint64_t(blockIdx.x + 1) * kScanRows);
     bool out = false;
     for (uint64_t j = from + threadIdx.x; j < to; j += 8 * 256)
 #pragma unroll
       for (uint32_t k = 0; k < 8; ++k) out |= j + k * 256 < to && left_out(a, j + k * 256);
     out = __syncthreads_or(out);
     if (threadIdx.x == 0) {
-      a.order[a.experts] = out;
+      a.order[a.experts + blockIdx.x] = out;
       if (out) report(a.status, DGS_EINVAL);
     }
+    return;
+  }
+  if (blockIdx.x < ahead) {     // who comes before whom
+    __shared__ uint32_t s_rows[DGS_ROUTE_MAX_EXPERTS];
     for (uint32_t e = threadIdx.x; e < a.experts; e += 256) {
       expert_rows(a, e, &first, &last, true);
       s_rows[e] = uint32_t(last - first);
@@ -455,7 +460,11 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
   tmem_after();
   const uint32_t tmem = s_tmem;
   wait_for_last_kernel();   // nothing above touches memory outside the SM
-  const bool skips = LISTS && a.order && a.order[a.experts];   // rows of the gradient become zeros on their way
+  bool skips = false;       // rows of the gradient become zeros on their way; the copies' warp need not know
+  if (LISTS && warp != 9) {
+    for (uint32_t i = lane; i < a.scans; i += 32) skips |= a.order[a.experts + i] != 0;
+    skips = __any_sync(0xffffffffu, skips);
+  }
 
   // Every role goes through the tiles by itself; it counts steps and chunks over all of them, which is what the barriers' phases go by.
   __syncwarp();
@@ -615,6 +624,11 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
           // free; sixteen rows that no product takes are left out.
           const uint32_t last = it + w.steps - 1, at = tiles + last % ST * STAGE + TILE, gr = tid / 16, gv = tid % 16, col = w.go + gv * 8;
           const uint32_t j0 = (w.steps - 1) * R + gr;
+          uint32_t out = 0;   // bit u: the thread's u-th row is left out
+          if (skips) {
+#pragma unroll 1
+            for (uint32_t u = 0; u < R / 16 && j0 + 16 * u < w.count; ++u) out |= uint32_t(left_out(a, w.first + j0 + 16 * u)) << u;
+          }
           uint4 v[P][R / 16];
 #pragma unroll
           for (uint32_t p = 0; p < P; ++p) {
@@ -622,7 +636,7 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
 #pragma unroll
             for (uint32_t u = 0; u < R / 16; ++u, from += 16 * a.dy_stride) {
               v[p][u] = make_uint4(0, 0, 0, 0);
-              if (j0 + 16 * u < w.count && col < a.outputs && !(skips && left_out(a, w.first + j0 + 16 * u))) {
+              if (j0 + 16 * u < w.count && col < a.outputs && !(out >> u & 1)) {
                 if (col + 8 <= a.outputs) {
                   v[p][u] = __ldg(reinterpret_cast<const uint4*>(from));
                 } else {
@@ -833,6 +847,7 @@ bool lists_ok(const dgs_row_lists* l) {
 }
 
 uint32_t ceil_div(uint64_t a, uint64_t b) { return uint32_t((a + b - 1) / b); }
+uint32_t scans_of(uint64_t dy_rows) { return ceil_div(dy_rows, kScanRows); }
 
 int plan_weight(const dgs_checkpoint* c, const dgs_matrix* dy, const dgs_row_lists* lists, uint32_t flags, WeightPlan* p) {
   if (!checkpoint_ok(c) || !matrix_ok(dy, false) || !lists_ok(lists) || (lists ? c->rows == 0 && dy->rows : dy->rows != c->rows))
@@ -878,7 +893,7 @@ int plan_weight(const dgs_checkpoint* c, const dgs_matrix* dy, const dgs_row_lis
   p->plane_rows = p->direct ? dy->rows : (dy->rows + p->step_rows - 1) / p->step_rows * p->step_rows + p->step_rows;   // a step may begin on the last row
   p->planes = p->direct ? 0 : p->parts * p->plane_rows * p->stride * 2;
   p->decoded = dy->rows ? decoded_rows(dy->rows, lists ? p->experts : 0, p->step_rows) * held_width(c->cols) * 2 : 0;
-  p->order = lists && dy->rows ? (uint64_t(p->experts + 1) * 4 + 15) / 16 * 16 : 0;
+  p->order = lists && dy->rows ? ((p->experts + uint64_t(scans_of(dy->rows))) * 4 + 15) / 16 * 16 : 0;
   p->bytes = p->decoded + p->planes + p->order + (p->splits > 1 ? p->nw * p->splits * 4 : 0) + (parts_b > 1 ? p->nb * parts_b * 4 : 0);
   return DGS_OK;
 }
@@ -977,6 +992,7 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
   a.in_out = flags & DGS_WEIGHT_IN_OUT ? 1 : 0;
   a.bias_tiles = p.bias_tiles;
   a.step_rows = p.step_rows;
+  a.scans = p.order ? scans_of(dy->rows) : 0;
   a.offsets = lists ? lists->offsets : nullptr;
   a.rows = lists ? lists->rows : nullptr;
   a.decoded = reinterpret_cast<__nv_bfloat16*>(work);
@@ -1009,7 +1025,7 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_checkpoint* ckpt, const dgs_
     rc = make_map(a.decoded, rows, a.h.width, a.h.width, p.step_rows, &held);
     if (rc == DGS_OK) rc = make_map(a.dy, p.parts * p.plane_rows, dy->cols, a.dy_stride, p.step_rows, &grad);
     if (rc != DGS_OK) return rc;
-    const uint32_t ctas = ceil_div(rows, kDecodeRows) + (lists ? 1 : 0);
+    const uint32_t ctas = ceil_div(rows, kDecodeRows) + (a.scans ? a.scans + 1 : 0);
     if (ckpt->format == DGS_FORMAT_E4M3)
       k_weight_decode<true><<<ctas, 256, 0, st>>>(a);
     else

@@ -93,3 +93,26 @@ def test_rows_that_name_no_row_of_the_checkpoint_take_no_part(lengths, inputs, o
         part = part[there[part]]
         d, h = dy[part].double(), x[at[part]].double()
         assert torch.equal(dw[e].double(), d.T @ h if layout == "out_in" else h.T @ d) and torch.equal(db[e].double(), d.sum(0)), e
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_one_row_that_names_no_row_wherever_it_stands(dtype):
+    n, inputs, outputs = 9000, 40, 24
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randint(-7, 8, (n, inputs), generator=g, device=DEV).float()
+    clean = torch.randint(-8, 9, (n, outputs), generator=g, device=DEV).to(dtype)
+    c = dgs.Checkpoint(n, inputs, device=DEV)
+    c.save(x)
+    offsets = torch.tensor([2, 5000, 8997], dtype=torch.int32, device=DEV)
+    for at in (2, 4095, 4096, 4999, 5000, 8191, 8192, 8996, 1, 8997):
+        rows = torch.arange(n, dtype=torch.int32, device=DEV)
+        dy = clean.clone()
+        rows[at], dy[at] = n, float("nan")
+        dw, db = torch.zeros(2, outputs, inputs, device=DEV), torch.zeros(2, outputs, device=DEV)
+        c.weight_grad(dy, dw, db, offsets=offsets, rows=rows)
+        assert dgs.operator_status(DEV) == (dgs.DGS_EINVAL if 2 <= at < 8997 else 0), at    # in no list: not looked at
+        for e, (a, b) in enumerate(((2, 5000), (5000, 8997))):
+            keep = torch.arange(a, b, device=DEV)
+            keep = keep[keep != at]
+            d = clean[keep].double()
+            assert torch.equal(dw[e].double(), d.T @ x[keep].double()) and torch.equal(db[e].double(), d.sum(0)), (at, e)
