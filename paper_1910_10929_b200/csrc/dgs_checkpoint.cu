@@ -180,8 +180,9 @@ __device__ __forceinline__ void each_unit(const Units& g, L&& load, D&& done) {
 constexpr int kPerSm = 4, kLoadPerSm = 6;   // CTAs on an SM
 template <class T> constexpr int kAtOnce = sizeof(T) == 2 ? 4 : 2;
 
-// All three are bound by memory where rows are wide: 32768 x 2048 in bfloat16 with gelu_tanh, of the measured copy bandwidth: save 66 us (0.78; 22
-// instructions a value keep the schedulers at 0.64), load 33 us (0.95), gradient 61 us (0.84).
+// 32768 x 2048 in bfloat16 with gelu_tanh, of the measured copy bandwidth: save 68 us (0.76; 22 instructions a value keep the schedulers at 0.65), load 33
+// us (0.95: memory), gradient 64 us (0.81).  gelu by erfcf is bound by its instructions in every type: a save 165 us, a gradient 170 us a call (in f32 152 and 167; silu in f32 113
+// and 101).  Rows that do not begin on 16 bytes go element by element, bound by their accesses: 32768 x 2047 in bfloat16 a save 184, a load 213, a gradient 190 us a call.
 template <class T, bool FLOAT8, bool VEC, int ACT>
 __global__ void __launch_bounds__(256, kPerSm) k_checkpoint_save(Held h, uint8_t* codes, uint8_t* scales, const T* x, uint64_t xs, T* y, uint64_t ys, Units g) {
   constexpr int N = kAtOnce<T>;

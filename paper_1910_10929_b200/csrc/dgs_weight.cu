@@ -116,7 +116,7 @@ template <uint32_t P> struct Shape {
   static constexpr uint32_t kTile = kCols / 64 * kColBlock;
   static constexpr uint32_t kStage = kTile * (1 + P), kSmem = 1024 + kStages * kStage;
 };
-// Eight warps keep the sums, four do the rest and leave them their registers.
+// Eight warps keep the sums, four do the rest and leave them their registers.  (56 for the four and 224 for the sums: 16 experts of 768 x 2048 145 us a call, 140 so.)
 constexpr uint32_t kThreads = 384, kRegsLaunch = 168, kRegsSum = 216, kRegsRest = 72;
 static_assert(kRegsSum * 256 + kRegsRest * 128 <= kRegsLaunch * kThreads, "setmaxnreg draws on the launch's registers");
 template <uint32_t P>
@@ -376,7 +376,8 @@ __device__ __forceinline__ void bias_add(const uint4& w, float (&bias)[8]) {   /
 // accumulators go to registers of the eight warps and are added up there with rounding (2.1e-7), while the products go on in the other half of
 // tensor memory.  Each step's part of db is summed by one of the CTAs that hold the same gradients.
 // One pair of CTAs per pair of SMs takes tile after tile, so that the copies and products of the next run while a tile is written out (a CTA per
-// tile: 10 us around the steps of each).  Bound by what comes from the second cache: 64 KB a CTA and step of 128 rows, 0.8 us.
+// tile: 10 us around the steps of each).  Bound by what comes from the second cache: 64 KB a CTA and step of 128 rows, 0.8 us.  (8192 x 768 x 50257: 488 us,
+// 0.78 of the measured rate of a product that runs alone, 0.92 of one that runs for seconds.)
 struct TileOf {
   uint64_t first, held_first;   // the tile's rows of the gradient, and of the decoded values
   uint32_t i0, o0, ci, go;      // first input and output of the tile, and of what the CTA brings
@@ -752,8 +753,10 @@ __global__ void __launch_bounds__(256) k_weight_sum(float* dw, float* db, const 
 // ---- few rows ---------------------------------------------------------------------------------------
 // Where there is little to do, the three kernels that bring operands to the tensor cores cost more than products without them: one launch, a tile of 64 x 64
 // results a CTA, 4 x 4 of them a thread, sixteen rows at a time through shared memory, sums in f32 with rounding.  Bound by the trips to memory and the
-// barriers of each sixteen rows, 1 us.  Here / with tensor cores, us: 37 x 512 x 1000 12.7 / 25.3 in f32, 12.7 / 21.5 in bfloat16; 128 x 1024 x 1024 17.4 /
-// 22.5; 256 x 768 x 680 19.6 / 22.9; 512 x 512 x 512 35.5 / 22.3, 31.8 / 28.8 in f32.
+// barriers of each sixteen rows, 1 us.  The rule goes by all rows and by one expert's results: a call's results are written either way.  Here / with tensor
+// cores, us a call alone: 37 x 512 x 1000 15 / 25 in bfloat16, 17 / 29 in f32; 64 x 1024 x 1024 20 / 27; 128 x 1024 x 1024 26 / 27; 256 x 768 x 680 29 / 25,
+// 27 / 30 in f32; 512 x 512 x 512 43 / 27, 40 / 32.  With lists: 200 rows, 8 experts of 300 x 300 22 / 31; 64, 32 of 2048 x 1024 101 / 109; 256 slots, 16 of
+// 768 x 2048 71 / 62; 16, 128 of 1024 x 1024 132 / 177; 256, 64 of 2048 x 2048 410 / 440.
 constexpr uint32_t kSmallRows = 256;
 constexpr uint64_t kSmallProducts = 1ull << 27;
 constexpr uint32_t kSmallTile = 64, kSmallStep = 16;
@@ -870,8 +873,9 @@ int plan_weight(const dgs_checkpoint* c, const dgs_matrix* dy, const dgs_row_lis
     return DGS_OK;
   }
   // The tile's width and the split of a tile's rows among pairs: whatever ends soonest.  74 pairs run at a time; 64 rows take 0.3 us and 0.1 by the
-  // width, a tile about 4 us besides, and partial results cost their way through the second cache and another launch.  (8192 x 768 x 2304: 54
-  // tiles of 128 columns 57 us, 27 of 256 in two runs of rows each 37.)
+  // width, a tile about 4 us besides, and partial results cost their way through the second cache and another launch.  (8192 x 768 x 2304, us
+  // a call: 54 tiles of 128 columns 64, 27 of 256 65, 27 of 256 in two runs of rows each 48.2, 36 of 192 in two runs, which this takes, 47.5.)  Steps are those of
+  // the mean expert: where one has most of the rows, few pairs do its tiles (16384 rows, 8 experts of 768 x 2048: 73 us if even, 104 if one has half, 135 if it has all).
   const uint32_t steps = std::max(1u, ceil_div(dy->rows / p->experts, 64));
   double best = 1e300;
   for (uint32_t n = 256; n >= 64; n -= 64) {
