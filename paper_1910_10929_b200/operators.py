@@ -66,6 +66,8 @@ def _matrix(t: torch.Tensor, what: str) -> "dgs.dgs_matrix":
                 elif s != stride * run:
                     raise ValueError(f"{what}: the rows of all but the last dimension must lie evenly spaced (shape {tuple(shape)}, strides {t.stride()})")
                 run *= n
+    if cols >= 1 << 32:                                  # it would wrap around in the library's 32 bits
+        raise ValueError(f"{what} has {cols} columns: 2^32 - 1 at most")
     if step != 1 and cols > 1 and rows:
         raise ValueError(f"{what}: neighbours in the last dimension must be neighbours in memory (stride {step})")
     return dgs.dgs_matrix(t.data_ptr(), rows, stride if rows > 1 else cols, cols, kind)
@@ -116,8 +118,8 @@ class Checkpoint:
     def __init__(self, rows: int, cols: int, format: str = "int8", device=None, data: Optional[torch.Tensor] = None):
         self.rows, self.cols, self.format = int(rows), int(cols), format
         code = _pick(_FORMAT, format, "format")
-        if self.rows < 0 or self.cols < 1:
-            raise ValueError(f"a checkpoint has rows >= 0 and cols >= 1: got {rows} x {cols}")
+        if self.rows < 0 or not 1 <= self.cols < 1 << 32:
+            raise ValueError(f"a checkpoint has rows >= 0 and cols >= 1 below 2^32: got {rows} x {cols}")
         size = self.rows * (-(-self.cols // 32) * 32 + -(-self.cols // 128) * 4)
         if self.rows >= 1 << 31 or self.cols > 1 << 30 or self.rows * self.cols > 1 << 40:
             size = dgs.dgs_checkpoint_bytes(self.rows, self.cols)   # raises what the library says
@@ -184,8 +186,8 @@ class Checkpoint:
         experts, lists = 1, None
         if offsets is not None:
             experts = offsets.numel() - 1
-            if experts < 1 or rows_per < 1:
-                raise ValueError("offsets holds experts + 1 numbers, and rows_per is at least 1")
+            if experts < 1 or not 1 <= rows_per < 1 << 32:
+                raise ValueError("offsets holds experts + 1 numbers, and rows_per is at least 1 and below 2^32")
             lists = dgs.dgs_row_lists(_plain(offsets, "offsets", torch.int32, experts + 1, self.device),
                                       _plain(rows, "rows", torch.int32, m.rows, self.device), experts, rows_per)
         elif rows is not None or rows_per != 1:

@@ -38,3 +38,18 @@ def test_views_of_more_dimensions_whose_rows_lie_evenly_spaced(monkeypatch):
               whole[0, 0, :, :7].expand(6, 5, 7)):
         with pytest.raises(ValueError):
             operators._matrix(v, "v")
+
+
+def test_sizes_past_32_bits_are_refused_and_not_wrapped_around(monkeypatch):
+    monkeypatch.setattr(operators, "_on_gpu", lambda t, what: None)
+    for shape in (((1 << 32) + 8,), (2, (1 << 32) + 8), (1 << 32,)):
+        with pytest.raises(ValueError, match="columns"):
+            operators._matrix(torch.empty(shape, dtype=torch.bfloat16, device="meta"), "x")
+    m = operators._matrix(torch.empty((1 << 32) - 1, dtype=torch.bfloat16, device="meta"), "x")
+    assert (m.rows, m.cols) == (1, (1 << 32) - 1)
+    with pytest.raises(ValueError):
+        operators.Checkpoint(1, (1 << 32) + 8, data=torch.empty(36, dtype=torch.uint8))
+    c = operators.Checkpoint(4, 8, data=torch.empty(4 * 36, dtype=torch.uint8))
+    for rows_per in (0, 1 << 32, (1 << 32) + 1):
+        with pytest.raises(ValueError, match="rows_per"):
+            c.weight_grad(torch.zeros(4, 8), torch.zeros(64), offsets=torch.zeros(2, dtype=torch.int32), rows=torch.zeros(4, dtype=torch.int32), rows_per=rows_per)
