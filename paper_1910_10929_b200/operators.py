@@ -33,7 +33,8 @@ def _pick(table, key, what):
         raise ValueError(f"{what} is one of {sorted(map(str, table))}: got {key!r}") from None
 
 
-_device_now, _stream_now = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream   # what torch.cuda's own calls end in
+# What torch.cuda's own calls end in.  A torch without CUDA has neither: the package is imported all the same, and every call here refuses its tensors.
+_device_now, _stream_now = getattr(torch._C, "_cuda_getDevice", None), getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _on_gpu(t, what):

@@ -1,4 +1,8 @@
 """What the torch-backed calls of a worker's own operators make of their arguments: no GPU needed."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -53,3 +57,15 @@ def test_sizes_past_32_bits_are_refused_and_not_wrapped_around(monkeypatch):
     for rows_per in (0, 1 << 32, (1 << 32) + 1):
         with pytest.raises(ValueError, match="rows_per"):
             c.weight_grad(torch.zeros(4, 8), torch.zeros(64), offsets=torch.zeros(2, dtype=torch.int32), rows=torch.zeros(4, dtype=torch.int32), rows_per=rows_per)
+
+
+def test_the_package_is_imported_where_torch_has_no_cuda():
+    code = ("import torch\n"
+            "for name in ('_cuda_getDevice', '_cuda_getCurrentRawStream'):\n"
+            "    if hasattr(torch._C, name): delattr(torch._C, name)\n"
+            "import paper_1910_10929_b200 as dgs\n"
+            "try: dgs.route_experts(torch.zeros(4, 8), 2)\n"
+            "except ValueError as e: assert 'CUDA' in str(e)\n"
+            "else: raise SystemExit(2)\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=root)
