@@ -466,6 +466,10 @@ k_weight_grad(const __grid_constant__ WeightArgs a, const __grid_constant__ CUte
     for (uint32_t i = lane; i < a.scans; i += 32) skips |= a.order[a.experts + i] != 0;
     skips = __any_sync(0xffffffffu, skips);
   }
+  if (LISTS && a.scans == 0 && blockIdx.x == 0 && warp == 9) {   // dy without rows: nothing was decoded, and nothing looked at the lists
+    uint64_t first, last;
+    for (uint32_t e = lane; e < a.experts; e += 32) expert_rows(a, e, &first, &last, true);
+  }
 
   // Every role goes through the tiles by itself; it counts steps and chunks over all of them, which is what the barriers' phases go by.
   __syncwarp();

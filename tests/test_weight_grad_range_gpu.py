@@ -127,3 +127,16 @@ def test_captured_with_other_lists_and_gradients_at_each_replay(listed, dtype, o
         torch.cuda.synchronize()
         assert torch.equal(got, want) and bool(torch.isfinite(got).all())
     assert dgs.operator_status(DEV) == 0
+
+
+@pytest.mark.parametrize("inputs,outputs", [(40, 24), (4100, 33000)])    # by the kernel for few rows, and by the other
+def test_lists_that_point_outside_a_gradient_without_rows_are_reported(inputs, outputs):
+    c = dgs.Checkpoint(7, inputs, device=DEV)
+    c.save(torch.ones(7, inputs, device=DEV))
+    dy = torch.zeros(0, outputs, device=DEV)
+    dw, db = torch.full((2 * outputs * inputs,), float("nan"), device=DEV), torch.full((2 * outputs,), float("nan"), device=DEV)
+    for offsets, status in (([0, 0, 0], 0), ([0, 0, 5], dgs.DGS_EINVAL), ([3, 3, 3], dgs.DGS_EINVAL)):
+        dw.fill_(float("nan"))
+        c.weight_grad(dy, dw, db, offsets=torch.tensor(offsets, dtype=torch.int32, device=DEV))
+        assert dgs.operator_status(DEV) == status
+        assert not bool(dw.any()) and not bool(db.any())
