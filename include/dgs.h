@@ -454,6 +454,21 @@ int dgs_route_experts(const dgs_router* router, const dgs_matrix* logits, const 
 int dgs_route_experts_grad(const dgs_router* router, const dgs_matrix* logits, const uint32_t* expert, const float* dweight,
                            const dgs_matrix* dlogits, void* stream);
 
+/* Tokens' rows in the order of the experts' lists, and back.  order and place are those of dgs_route_experts (DEVICE u32[tokens * k] each), k at most
+ * DGS_ROUTE_MAX_K, tokens * k < 2^31; matrices of tokens * k rows hold slot t * k + j's row at place[t][j].  The matrices of a call have one type and the
+ * same columns (2^30 at most).  An empty slot (DGS_NO_EXPERT) takes no part, nor does the row that nobody wrote behind the last list, whatever it holds; a place that
+ * points outside is treated as empty and reported.  Two slots at one place are not specified.
+ *
+ * gather:   y[place[t][j]] = x[t]; rows of y whose entry in order is DGS_NO_EXPERT, which stand behind the last list, are zero. */
+int dgs_experts_gather(const dgs_matrix* x, const uint32_t* order, const uint32_t* place, uint32_t k, const dgs_matrix* y, void* stream);
+/* combine:  out[t] = sum over j of weight[t][j] * y[place[t][j]], in f32 in the slots' order, rounded once.  weight: DEVICE f32[tokens][k]; NULL: every weight is
+ * 1, which is the gradient of gather (y its rows' gradients, out the tokens'). */
+int dgs_experts_combine(const dgs_matrix* y, const float* weight, const uint32_t* place, uint32_t k, const dgs_matrix* out, void* stream);
+/* The gradient of combine:  dy[place[t][j]] = weight[t][j] * dout[t], rows behind the last list zero, and dweight[t][j] = the sum over columns of
+ * dout[t] * y[place[t][j]] in f32, 0 for an empty slot (DEVICE f32[tokens][k], what dgs_route_experts_grad takes). */
+int dgs_experts_combine_grad(const dgs_matrix* dout, const dgs_matrix* y, const float* weight, const uint32_t* order, const uint32_t* place, uint32_t k,
+                             const dgs_matrix* dy, float* dweight, void* stream);
+
 /* Waits for `stream` and stores in *device_status the lowest status that kernels of the calls above have left on the current device
  * since the last time it was read: 0, DGS_EINVAL (an index or list pointed outside its matrix) or DGS_ETIMEOUT (a bounded wait gave up).  The word is one
  * for the device and is read and cleared in one step: a report is returned once, to whichever caller reads it first. */

@@ -35,7 +35,7 @@ EXPORTS = (
     "dgs_topk_encode_static_status", "dgs_hardware_queues",
     "dgs_checkpoint_bytes", "dgs_checkpoint_save", "dgs_checkpoint_load", "dgs_checkpoint_activation_grad",
     "dgs_checkpoint_weight_grad_bytes", "dgs_checkpoint_weight_grad", "dgs_route_experts_bytes", "dgs_route_experts",
-    "dgs_route_experts_grad", "dgs_operator_status",
+    "dgs_route_experts_grad", "dgs_operator_status", "dgs_experts_gather", "dgs_experts_combine", "dgs_experts_combine_grad",
 )
 DGS_TYPE_F32, DGS_TYPE_BF16, DGS_TYPE_FP16 = 0, 1, 2
 DGS_FORMAT_INT8, DGS_FORMAT_E4M3 = 0, 1
@@ -141,6 +141,9 @@ def lib() -> C.CDLL:
         L.dgs_route_experts_bytes.argtypes = [router, u64, u32, C.POINTER(u64)]
         L.dgs_route_experts.argtypes = [router, mat, vp, vp, vp, vp, vp, vp, vp, u64, vp]
         L.dgs_route_experts_grad.argtypes = [router, mat, vp, vp, mat, vp]
+        L.dgs_experts_gather.argtypes = [mat, vp, vp, u32, mat, vp]
+        L.dgs_experts_combine.argtypes = [mat, vp, vp, u32, mat, vp]
+        L.dgs_experts_combine_grad.argtypes = [mat, mat, vp, vp, vp, u32, mat, vp, vp]
         L.dgs_operator_status.argtypes = [vp, C.POINTER(i32)]
         L.dgs_error_string.argtypes = [i32]
         L.dgs_error_string.restype = C.c_char_p
@@ -346,6 +349,20 @@ def dgs_route_experts_grad(router: dgs_router, logits: dgs_matrix, expert_ptr: i
            "dgs_route_experts_grad")
 
 
+def dgs_experts_gather(x: dgs_matrix, order_ptr: int, place_ptr: int, k: int, y: dgs_matrix, stream: int = 0) -> None:
+    _check(lib().dgs_experts_gather(x, order_ptr or None, place_ptr or None, k, y, stream or None), "dgs_experts_gather")
+
+
+def dgs_experts_combine(y: dgs_matrix, weight_ptr: int, place_ptr: int, k: int, out: dgs_matrix, stream: int = 0) -> None:
+    _check(lib().dgs_experts_combine(y, weight_ptr or None, place_ptr or None, k, out, stream or None), "dgs_experts_combine")
+
+
+def dgs_experts_combine_grad(dout: dgs_matrix, y: dgs_matrix, weight_ptr: int, order_ptr: int, place_ptr: int, k: int, dy: dgs_matrix,
+                             dweight_ptr: int, stream: int = 0) -> None:
+    _check(lib().dgs_experts_combine_grad(dout, y, weight_ptr or None, order_ptr or None, place_ptr or None, k, dy, dweight_ptr or None,
+                                          stream or None), "dgs_experts_combine_grad")
+
+
 def dgs_operator_status(stream: int = 0) -> int:
     """Waits for `stream`; the lowest status that the operators' kernels have left on the current device since the last call."""
     out = C.c_int(0)
@@ -365,7 +382,9 @@ def dgs_free(ctx: int) -> None:
 
 
 from .context import Context  # noqa: E402  (torch-backed convenience holder of arena + handle)
-from .operators import Checkpoint, Route, operator_status, route_experts, route_experts_grad  # noqa: E402  (likewise, for a worker's own operators)
+from .operators import (Checkpoint, Route, combine_experts, combine_experts_grad, gather_experts, gather_experts_grad,  # noqa: E402  (likewise, for a worker's own operators)
+                        operator_status, route_experts, route_experts_grad)
 
-__all__ = [n for n in dir() if n.startswith(("dgs_", "DGS_"))] + ["Checkpoint", "Context", "DgsError", "Route", "lib", "make_config",
-                                                                   "operator_status", "route_experts", "route_experts_grad"]
+__all__ = [n for n in dir() if n.startswith(("dgs_", "DGS_"))] + [
+    "Checkpoint", "Context", "DgsError", "Route", "combine_experts", "combine_experts_grad", "gather_experts", "gather_experts_grad", "lib",
+    "make_config", "operator_status", "route_experts", "route_experts_grad"]

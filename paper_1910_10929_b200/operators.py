@@ -1,5 +1,5 @@
 """Torch-backed calls of a worker's own operators (include/dgs.h, "what a worker computes before its push"):
-activations held in 8 bits and the gradients formed from them, and the router of a model with experts.
+activations held in 8 bits and the gradients formed from them, the router of a model with experts, and rows taken to its lists and back.
 
 Outputs and workspaces are torch tensors of the inputs' device, and work is enqueued on that device's current
 stream, whichever device is current for the caller; as with torch's own operators, a tensor used on another stream
@@ -272,3 +272,86 @@ def route_experts_grad(logits: torch.Tensor, expert: torch.Tensor, dweight: torc
     _same_device(logits.device, out)
     _enqueue(logits.device, dgs.dgs_route_experts_grad, router, m, pe, pw, mo)
     return out
+
+
+def _slots(place: torch.Tensor) -> int:
+    """k of a [tokens, k] place."""
+    if not isinstance(place, torch.Tensor) or place.dim() < 1 or not 1 <= place.shape[-1] <= dgs.DGS_ROUTE_MAX_K:
+        raise ValueError(f"place is [tokens, k], k from 1 to {dgs.DGS_ROUTE_MAX_K}")
+    return place.shape[-1]
+
+
+def _fit(m: "dgs.dgs_matrix", what: str, rows: int, cols: int, kind: int) -> None:
+    if m.rows != rows or m.cols != cols or m.type != kind:
+        raise ValueError(f"{what} must be {rows} x {cols} and of the other matrices' type: got {m.rows} x {m.cols}")
+
+
+def _rows_like(out: Optional[torch.Tensor], what: str, shape, m: "dgs.dgs_matrix", rows: int, like: torch.Tensor):
+    """(out, its matrix): `rows` rows of m's columns and type, a new tensor if there is none."""
+    if out is None:
+        out = torch.empty(shape, dtype=like.dtype, device=like.device)
+    mo = _matrix(out, what)
+    _fit(mo, what, rows, m.cols, m.type)
+    _same_device(like.device, out)
+    return out, mo
+
+
+def gather_experts(x: torch.Tensor, order: torch.Tensor, place: torch.Tensor, *, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The tokens' rows in the order of the experts' lists (order and place of a Route): row i is that of token order[i] // k, and
+    zero where order[i] is -1.  Returns [tokens * k, cols]."""
+    m = _matrix(x, "x")
+    _cut_off(x, "x", "gather_experts")
+    k = _slots(place)
+    slots = m.rows * k
+    po = _plain(order, "order", torch.int32, slots, x.device)
+    pp = _plain(place, "place", torch.int32, slots, x.device)
+    out, mo = _rows_like(out, "out", (slots, m.cols), m, slots, x)
+    _enqueue(x.device, dgs.dgs_experts_gather, m, po, pp, k, mo)
+    return out
+
+
+def _combine(y, weight, place, out, what):
+    m = _matrix(y, what)
+    k = _slots(place)
+    if m.rows % k:
+        raise ValueError(f"{what} has a row for each of the tokens' {k} slots: got {m.rows} rows")
+    tokens = m.rows // k
+    pw = _plain(weight, "weight", torch.float32, m.rows, y.device)
+    pp = _plain(place, "place", torch.int32, m.rows, y.device)
+    out, mo = _rows_like(out, "out", (tokens, m.cols), m, tokens, y)
+    _enqueue(y.device, dgs.dgs_experts_combine, m, pw, pp, k, mo)
+    return out
+
+
+def gather_experts_grad(dy: torch.Tensor, place: torch.Tensor, *, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of gather_experts: the gradients of a token's rows added up.  Returns [tokens, cols]."""
+    return _combine(dy, None, place, out, "dy")
+
+
+def combine_experts(y: torch.Tensor, weight: torch.Tensor, place: torch.Tensor, *, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Each token's rows of y [tokens * k, cols] (in the order of the experts' lists), weighted (float32 [tokens, k]) and added up in float32.
+    Empty slots take no part.  Returns [tokens, cols]."""
+    _on_gpu(weight, "weight")
+    if isinstance(y, torch.Tensor):
+        _cut_off(y, "y", "combine_experts")
+    _cut_off(weight, "weight", "combine_experts")
+    return _combine(y, weight, place, out, "y")
+
+
+def combine_experts_grad(dout: torch.Tensor, y: torch.Tensor, weight: torch.Tensor, order: torch.Tensor, place: torch.Tensor, *,
+                         out: Optional[torch.Tensor] = None):
+    """The gradient of combine_experts: (dy [tokens * k, cols] in the order of the experts' lists, zero behind the last one, and
+    dweight float32 [tokens, k])."""
+    m = _matrix(dout, "dout")
+    my = _matrix(y, "y")
+    k, device = _slots(place), dout.device
+    slots = m.rows * k
+    _fit(my, "y", slots, m.cols, m.type)
+    _same_device(device, y)
+    pw = _plain(weight, "weight", torch.float32, slots, device)
+    po = _plain(order, "order", torch.int32, slots, device)
+    pp = _plain(place, "place", torch.int32, slots, device)
+    out, mo = _rows_like(out, "out", (slots, m.cols), m, slots, dout)
+    dweight = torch.empty(place.shape, dtype=torch.float32, device=device)
+    _enqueue(device, dgs.dgs_experts_combine_grad, m, my, pw, po, pp, k, mo, dweight.data_ptr())
+    return out, dweight
