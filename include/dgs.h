@@ -469,6 +469,35 @@ int dgs_experts_combine(const dgs_matrix* y, const float* weight, const uint32_t
 int dgs_experts_combine_grad(const dgs_matrix* dout, const dgs_matrix* y, const float* weight, const uint32_t* order, const uint32_t* place, uint32_t k,
                              const dgs_matrix* dy, float* dweight, void* stream);
 
+enum { DGS_TARGET_I64 = 1u << 0, /* targets are i64, 8-byte aligned; without it i32 */
+       DGS_LOSS_ADD = 1u << 1    /* dw is added to; without it it is set            */ };
+
+/* Softmax cross entropy of hidden states against the rows of a vocabulary, as the head of a language model or classifier has it, without
+ * keeping the logits z = hidden weight^T:
+ *     lse[r] = log(sum over words v of exp z[r][v]),     loss[r] = lse[r] - z[r][target[r]]
+ * hidden: rows x width, weight: words x width (one row a word, one at least), of one type.  target: DEVICE i32 or i64 [rows]; a row whose target is below 0 is
+ * ignored: its loss is 0 (its lse is that of whatever the row holds).  A target past the last word is treated so and reported.  loss, lse: DEVICE f32[rows]; lse is
+ * what the gradient takes.  Products of 16-bit types are exact, f32 values are taken as 22 bits under a power of two for each row; sums are in f32.  A row whose
+ * logits hold a NaN or +inf has NaN for both.
+ * workspace: DEVICE, 256-byte aligned, at least what dgs_vocabulary_loss_bytes says for these arguments (data pointers included: their alignment counts).  It takes
+ * 8 bytes for each row and 128 words, and copies of f32 matrices (4 bytes a value) and of those whose rows do not begin on 16 bytes (2 bytes).
+ * width at most 2^24, rows and words 2^30, rows or words times width 2^38, else DGS_ELIMIT. */
+int dgs_vocabulary_loss_bytes(const dgs_matrix* hidden, const dgs_matrix* weight, uint64_t* out_bytes);
+int dgs_vocabulary_loss(const dgs_matrix* hidden, const dgs_matrix* weight, const void* target, uint32_t flags, float* loss, float* lse, void* workspace,
+                        uint64_t workspace_bytes, void* stream);
+
+/* Its gradient.  With s[r][v] = dloss[r] * (exp(z[r][v] - lse[r]) - [v is target[r]]), 0 in ignored rows whatever they hold:
+ *     dhidden[r][c] = sum over v of s[r][v] * weight[v][c],     dw[v][c] = sum over r of s[r][v] * hidden[r][c]
+ * lse: DEVICE f32[rows], as dgs_vocabulary_loss writes it.  dloss: DEVICE f32[rows] with dloss_stride 1, or one value for all rows with 0; finite.  dhidden: rows x
+ * width, of the hidden states' type.  dw: DEVICE f32, words * width elements (4-byte aligned: the layer's slice of the flat gradient), or NULL: not wanted.
+ * s is formed a piece of the vocabulary at a time and kept in 22 bits under one power of two for the call (for dhidden in bfloat16 in 11); hidden and weight meet it
+ * as 11 bits (f32: 22) under a power of two for each column, which holds bfloat16 values exactly down to 2^-29 of their column's largest.
+ * workspace: likewise, dgs_vocabulary_loss_grad_bytes: up to 256 MB (or 1 KB a row, if more) of s, 2 bytes a value of both matrices (f32 4), 4 bytes a value of
+ * dhidden, partial results where contractions are split, and the copies that the loss needs. */
+int dgs_vocabulary_loss_grad_bytes(const dgs_matrix* hidden, const dgs_matrix* weight, uint64_t* out_bytes);
+int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matrix* weight, const void* target, const float* lse, const float* dloss, uint32_t dloss_stride,
+                             const dgs_matrix* dhidden, float* dw, uint32_t flags, void* workspace, uint64_t workspace_bytes, void* stream);
+
 /* Waits for `stream` and stores in *device_status the lowest status that kernels of the calls above have left on the current device
  * since the last time it was read: 0, DGS_EINVAL (an index or list pointed outside its matrix) or DGS_ETIMEOUT (a bounded wait gave up).  The word is one
  * for the device and is read and cleared in one step: a report is returned once, to whichever caller reads it first. */

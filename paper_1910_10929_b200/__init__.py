@@ -36,12 +36,14 @@ EXPORTS = (
     "dgs_checkpoint_bytes", "dgs_checkpoint_save", "dgs_checkpoint_load", "dgs_checkpoint_activation_grad",
     "dgs_checkpoint_weight_grad_bytes", "dgs_checkpoint_weight_grad", "dgs_route_experts_bytes", "dgs_route_experts",
     "dgs_route_experts_grad", "dgs_operator_status", "dgs_experts_gather", "dgs_experts_combine", "dgs_experts_combine_grad",
+    "dgs_vocabulary_loss_bytes", "dgs_vocabulary_loss", "dgs_vocabulary_loss_grad_bytes", "dgs_vocabulary_loss_grad",
 )
 DGS_TYPE_F32, DGS_TYPE_BF16, DGS_TYPE_FP16 = 0, 1, 2
 DGS_FORMAT_INT8, DGS_FORMAT_E4M3 = 0, 1
 DGS_ACT_NONE, DGS_ACT_RELU, DGS_ACT_GELU, DGS_ACT_GELU_TANH, DGS_ACT_SILU = 0, 1, 2, 3, 4
 DGS_WEIGHT_IN_OUT, DGS_WEIGHT_ADD = 1, 2
 DGS_SCORE_SOFTMAX, DGS_SCORE_SIGMOID = 0, 1
+DGS_TARGET_I64, DGS_LOSS_ADD = 1, 2
 DGS_ROUTE_MAX_EXPERTS, DGS_ROUTE_MAX_K = 1024, 32
 DGS_NO_EXPERT = 0xFFFFFFFF
 DGS_ELIMIT = -6
@@ -144,6 +146,10 @@ def lib() -> C.CDLL:
         L.dgs_experts_gather.argtypes = [mat, vp, vp, u32, mat, vp]
         L.dgs_experts_combine.argtypes = [mat, vp, vp, u32, mat, vp]
         L.dgs_experts_combine_grad.argtypes = [mat, mat, vp, vp, vp, u32, mat, vp, vp]
+        L.dgs_vocabulary_loss_bytes.argtypes = [mat, mat, C.POINTER(u64)]
+        L.dgs_vocabulary_loss.argtypes = [mat, mat, vp, u32, vp, vp, vp, u64, vp]
+        L.dgs_vocabulary_loss_grad_bytes.argtypes = [mat, mat, C.POINTER(u64)]
+        L.dgs_vocabulary_loss_grad.argtypes = [mat, mat, vp, vp, vp, u32, mat, vp, u32, vp, u64, vp]
         L.dgs_operator_status.argtypes = [vp, C.POINTER(i32)]
         L.dgs_error_string.argtypes = [i32]
         L.dgs_error_string.restype = C.c_char_p
@@ -363,6 +369,30 @@ def dgs_experts_combine_grad(dout: dgs_matrix, y: dgs_matrix, weight_ptr: int, o
                                           stream or None), "dgs_experts_combine_grad")
 
 
+def dgs_vocabulary_loss_bytes(hidden: dgs_matrix, weight: dgs_matrix) -> int:
+    out = C.c_uint64(0)
+    _check(lib().dgs_vocabulary_loss_bytes(hidden, weight, C.byref(out)), "dgs_vocabulary_loss_bytes")
+    return int(out.value)
+
+
+def dgs_vocabulary_loss(hidden: dgs_matrix, weight: dgs_matrix, target_ptr: int, flags: int, loss_ptr: int, lse_ptr: int, workspace_ptr: int = 0,
+                        workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().dgs_vocabulary_loss(hidden, weight, target_ptr or None, flags, loss_ptr or None, lse_ptr or None, workspace_ptr or None,
+                                     workspace_bytes, stream or None), "dgs_vocabulary_loss")
+
+
+def dgs_vocabulary_loss_grad_bytes(hidden: dgs_matrix, weight: dgs_matrix) -> int:
+    out = C.c_uint64(0)
+    _check(lib().dgs_vocabulary_loss_grad_bytes(hidden, weight, C.byref(out)), "dgs_vocabulary_loss_grad_bytes")
+    return int(out.value)
+
+
+def dgs_vocabulary_loss_grad(hidden: dgs_matrix, weight: dgs_matrix, target_ptr: int, lse_ptr: int, dloss_ptr: int, dloss_stride: int,
+                             dhidden: dgs_matrix, dw_ptr: int, flags: int, workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().dgs_vocabulary_loss_grad(hidden, weight, target_ptr or None, lse_ptr or None, dloss_ptr or None, dloss_stride, dhidden,
+                                          dw_ptr or None, flags, workspace_ptr or None, workspace_bytes, stream or None), "dgs_vocabulary_loss_grad")
+
+
 def dgs_operator_status(stream: int = 0) -> int:
     """Waits for `stream`; the lowest status that the operators' kernels have left on the current device since the last call."""
     out = C.c_int(0)
@@ -382,9 +412,9 @@ def dgs_free(ctx: int) -> None:
 
 
 from .context import Context  # noqa: E402  (torch-backed convenience holder of arena + handle)
-from .operators import (Checkpoint, Route, combine_experts, combine_experts_grad, gather_experts, gather_experts_grad,  # noqa: E402  (likewise, for a worker's own operators)
-                        operator_status, route_experts, route_experts_grad)
+from .operators import (Checkpoint, Route, VocabularyLoss, combine_experts, combine_experts_grad, gather_experts, gather_experts_grad,  # noqa: E402  (likewise, for a worker's own operators)
+                        operator_status, route_experts, route_experts_grad, vocabulary_loss, vocabulary_loss_grad)
 
 __all__ = [n for n in dir() if n.startswith(("dgs_", "DGS_"))] + [
-    "Checkpoint", "Context", "DgsError", "Route", "combine_experts", "combine_experts_grad", "gather_experts", "gather_experts_grad", "lib",
-    "make_config", "operator_status", "route_experts", "route_experts_grad"]
+    "Checkpoint", "Context", "DgsError", "Route", "VocabularyLoss", "combine_experts", "combine_experts_grad", "gather_experts", "gather_experts_grad", "lib",
+    "make_config", "operator_status", "route_experts", "route_experts_grad", "vocabulary_loss", "vocabulary_loss_grad"]

@@ -6,10 +6,6 @@
 namespace dgs {
 namespace {
 
-// A warp takes 256 columns of a token's rows, eight a lane, so that a row in 16 bits is read 512 bytes at a time wherever a list puts it.  Rows that
-// begin on 16 bytes: eight neighbours a lane; others: every 32nd column, so that a warp's elements are neighbours still.
-constexpr uint32_t kSpan = 256;
-
 struct Rows {
   const uint32_t* order;
   const uint32_t* place;
@@ -17,56 +13,6 @@ struct Rows {
   uint64_t slots, in_stride, mid_stride, out_stride;
   int* status;
 };
-
-template <class T, bool VEC>
-__device__ __forceinline__ void load8(const T* row, uint32_t col0, uint32_t lane, uint32_t cols, Eight<T>& e) {
-  if constexpr (VEC) {
-    const uint32_t c = col0 + lane * 8;
-    if (c + 8 <= cols) {
-#pragma unroll
-      for (uint32_t i = 0; i < sizeof(T) / 2; ++i) {
-        const uint4 w = __ldcs(reinterpret_cast<const uint4*>(row + c) + i);
-        e.w[4 * i] = w.x, e.w[4 * i + 1] = w.y, e.w[4 * i + 2] = w.z, e.w[4 * i + 3] = w.w;
-      }
-      return;
-    }
-    T t[8];
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) t[i] = c + i < cols ? row[c + i] : Elem<T>::put(0.0f);
-    memcpy(e.w, t, sizeof(t));
-  } else {
-    T t[8];
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-      const uint32_t c = col0 + i * 32 + lane;
-      t[i] = c < cols ? row[c] : Elem<T>::put(0.0f);
-    }
-    memcpy(e.w, t, sizeof(t));
-  }
-}
-template <class T, bool VEC>
-__device__ __forceinline__ void store8(T* row, uint32_t col0, uint32_t lane, uint32_t cols, const Eight<T>& e) {
-  T t[8];
-  memcpy(t, e.w, sizeof(t));
-  if constexpr (VEC) {
-    const uint32_t c = col0 + lane * 8;
-    if (c + 8 <= cols) {
-#pragma unroll
-      for (uint32_t i = 0; i < sizeof(T) / 2; ++i)
-        __stcs(reinterpret_cast<uint4*>(row + c) + i, make_uint4(e.w[4 * i], e.w[4 * i + 1], e.w[4 * i + 2], e.w[4 * i + 3]));
-      return;
-    }
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i)
-      if (c + i < cols) row[c + i] = t[i];
-  } else {
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-      const uint32_t c = col0 + i * 32 + lane;
-      if (c < cols) row[c] = t[i];
-    }
-  }
-}
 
 // Lane j: where the token's j-th slot stands, DGS_NO_EXPERT for an empty one, for one past the last and (reported) for one that points outside.
 __device__ __forceinline__ uint32_t lane_place(const Rows& a, uint32_t token, uint32_t lane) {
@@ -202,8 +148,6 @@ __global__ void __launch_bounds__(256) k_experts_combine_grad(const __grid_const
   }
 }
 
-bool wide(const dgs_matrix* m) { return aligned(m->data, 16) && m->stride * elem_bytes(m->type) % 16 == 0; }
-
 bool slots_ok(const uint32_t* order, const uint32_t* place, uint32_t k, uint64_t tokens) {
   return k && k <= DGS_ROUTE_MAX_K && tokens < (1ull << 31) / k && aligned(order, 4) && aligned(place, 4) && (tokens == 0 || place);
 }
@@ -224,23 +168,6 @@ Rows rows_of(const uint32_t* order, const uint32_t* place, uint32_t k, const dgs
 }
 uint32_t ctas(uint64_t units) { return uint32_t(std::min<uint64_t>((units + 7) / 8, 1u << 22)); }
 
-struct Span {
-  const void* p;
-  uint64_t n;
-  bool out;
-};
-template <size_t N>
-bool apart(const Span (&part)[N]) {
-  for (const Span& x : part)
-    for (const Span& y : part)
-      if (&x != &y && x.out && overlap(x.p, x.n, y.p, y.n)) return false;
-  return true;
-}
-
-template <class F>
-int with_wide(uint32_t type, bool vec, F&& f) {
-  return with_type(type, [&](auto* t) { return vec ? f(t, std::true_type{}) : f(t, std::false_type{}); });
-}
 int launched() { return cudaGetLastError() == cudaSuccess ? DGS_OK : DGS_ECUDA; }
 
 }  // namespace
@@ -258,7 +185,7 @@ extern "C" int dgs_experts_gather(const dgs_matrix* x, const uint32_t* order, co
   if (!a.status) return DGS_ECUDA;
   a.in_stride = x->stride;
   a.out_stride = y->stride;
-  return with_wide(x->type, wide(x) && wide(y), [&](auto* t, auto vec) {
+  return with_wide(x->type, on_16_bytes(x) && on_16_bytes(y), [&](auto* t, auto vec) {
     using T = std::remove_pointer_t<decltype(t)>;
     k_experts_gather<T, vec.value><<<ctas(uint64_t(a.tokens) * a.chunks), 256, 0, static_cast<cudaStream_t>(stream)>>>(a, static_cast<const T*>(x->data), static_cast<T*>(y->data));
     return launched();
@@ -275,7 +202,7 @@ extern "C" int dgs_experts_combine(const dgs_matrix* y, const float* weight, con
   if (!a.status) return DGS_ECUDA;
   a.in_stride = y->stride;
   a.out_stride = out->stride;
-  return with_wide(y->type, wide(y) && wide(out), [&](auto* t, auto vec) {
+  return with_wide(y->type, on_16_bytes(y) && on_16_bytes(out), [&](auto* t, auto vec) {
     using T = std::remove_pointer_t<decltype(t)>;
     k_experts_combine<T, vec.value><<<ctas(uint64_t(a.tokens) * a.chunks), 256, 0, static_cast<cudaStream_t>(stream)>>>(a, weight, static_cast<const T*>(y->data), static_cast<T*>(out->data));
     return launched();
@@ -301,7 +228,7 @@ extern "C" int dgs_experts_combine_grad(const dgs_matrix* dout, const dgs_matrix
   a.warps = 1;
   while (a.warps < 8 && a.warps < a.chunks && uint64_t(a.tokens) * a.warps < kSms * 32) a.warps *= 2;
   const uint32_t grid = uint32_t(std::min<uint64_t>((uint64_t(a.tokens) * a.warps + 7) / 8, 1u << 22));
-  return with_wide(y->type, wide(dout) && wide(y) && wide(dy), [&](auto* t, auto vec) {
+  return with_wide(y->type, on_16_bytes(dout) && on_16_bytes(y) && on_16_bytes(dy), [&](auto* t, auto vec) {
     using T = std::remove_pointer_t<decltype(t)>;
     k_experts_combine_grad<T, vec.value><<<grid, 256, 0, static_cast<cudaStream_t>(stream)>>>(a, weight, static_cast<const T*>(dout->data), static_cast<const T*>(y->data),
                                                                                               static_cast<T*>(dy->data), dweight);

@@ -71,6 +71,27 @@ inline bool same_matrix(const dgs_matrix* a, const dgs_matrix* b) {
   return a->data == b->data && a->stride == b->stride && a->type == b->type;
 }
 
+// Whether every row begins on 16 bytes.
+inline bool on_16_bytes(const dgs_matrix* m) { return aligned(m->data, 16) && m->stride * elem_bytes(m->type) % 16 == 0; }
+// Whether no output of a call overlaps another of its ranges.
+struct Span {
+  const void* p;
+  uint64_t n;
+  bool out;
+};
+template <size_t N>
+bool apart(const Span (&part)[N]) {
+  for (const Span& x : part)
+    for (const Span& y : part)
+      if (&x != &y && x.out && overlap(x.p, x.n, y.p, y.n)) return false;
+  return true;
+}
+// Calls f with a null pointer of the element type and whether rows begin on 16 bytes.
+template <class F>
+int with_wide(uint32_t type, bool vec, F&& f) {
+  return with_type(type, [&](auto* t) { return vec ? f(t, std::true_type{}) : f(t, std::false_type{}); });
+}
+
 // ---- the 8-bit format -----------------------------------------------------------------------
 // A checkpoint of [rows, cols]: codes [rows][width], then scale bytes [rows][spitch]; width = cols up to a multiple of 32, spitch
 // = 4 bytes for each 128 columns begun.  A scale byte is e + 127: the block's values are code * 2^e, e the smallest
@@ -241,6 +262,58 @@ __device__ __forceinline__ void of_floats(const float2 (&v)[4], Eight<__half>& e
   for (int i = 0; i < 4; ++i) {
     const __half2 b = __float22half2_rn(v[i]);
     memcpy(&e.w[i], &b, 4);
+  }
+}
+// A warp takes 256 columns of a row, eight a lane, so that a row in 16 bits is read 512 bytes at a time wherever it lies.  Rows that
+// begin on 16 bytes: eight neighbours a lane; others: every 32nd column, so that a warp's elements are neighbours still.
+constexpr uint32_t kSpan = 256;
+template <class T, bool VEC>
+__device__ __forceinline__ void load8(const T* row, uint32_t col0, uint32_t lane, uint32_t cols, Eight<T>& e) {
+  if constexpr (VEC) {
+    const uint32_t c = col0 + lane * 8;
+    if (c + 8 <= cols) {
+#pragma unroll
+      for (uint32_t i = 0; i < sizeof(T) / 2; ++i) {
+        const uint4 w = __ldcs(reinterpret_cast<const uint4*>(row + c) + i);
+        e.w[4 * i] = w.x, e.w[4 * i + 1] = w.y, e.w[4 * i + 2] = w.z, e.w[4 * i + 3] = w.w;
+      }
+      return;
+    }
+    T t[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) t[i] = c + i < cols ? row[c + i] : Elem<T>::put(0.0f);
+    memcpy(e.w, t, sizeof(t));
+  } else {
+    T t[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      const uint32_t c = col0 + i * 32 + lane;
+      t[i] = c < cols ? row[c] : Elem<T>::put(0.0f);
+    }
+    memcpy(e.w, t, sizeof(t));
+  }
+}
+template <class T, bool VEC>
+__device__ __forceinline__ void store8(T* row, uint32_t col0, uint32_t lane, uint32_t cols, const Eight<T>& e) {
+  T t[8];
+  memcpy(t, e.w, sizeof(t));
+  if constexpr (VEC) {
+    const uint32_t c = col0 + lane * 8;
+    if (c + 8 <= cols) {
+#pragma unroll
+      for (uint32_t i = 0; i < sizeof(T) / 2; ++i)
+        __stcs(reinterpret_cast<uint4*>(row + c) + i, make_uint4(e.w[4 * i], e.w[4 * i + 1], e.w[4 * i + 2], e.w[4 * i + 3]));
+      return;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i)
+      if (c + i < cols) row[c + i] = t[i];
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      const uint32_t c = col0 + i * 32 + lane;
+      if (c < cols) row[c] = t[i];
+    }
   }
 }
 // The bits of the largest magnitude as a float; infinities and NaN are larger than all others.

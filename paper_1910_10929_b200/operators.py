@@ -1,5 +1,5 @@
 """Torch-backed calls of a worker's own operators (include/dgs.h, "what a worker computes before its push"):
-activations held in 8 bits and the gradients formed from them, the router of a model with experts, and rows taken to its lists and back.
+activations held in 8 bits and the gradients formed from them, the router of a model with experts, rows taken to its lists and back, and the loss over a vocabulary.
 
 Outputs and workspaces are torch tensors of the inputs' device, and work is enqueued on that device's current
 stream, whichever device is current for the caller; as with torch's own operators, a tensor used on another stream
@@ -355,3 +355,60 @@ def combine_experts_grad(dout: torch.Tensor, y: torch.Tensor, weight: torch.Tens
     dweight = torch.empty(place.shape, dtype=torch.float32, device=device)
     _enqueue(device, dgs.dgs_experts_combine_grad, m, my, pw, po, pp, k, mo, dweight.data_ptr())
     return out, dweight
+
+
+class VocabularyLoss(NamedTuple):
+    """What vocabulary_loss returns, float32 of the targets' shape."""
+    loss: torch.Tensor   # 0 in ignored rows
+    lse: torch.Tensor    # log of the sum of exponentials of a row's logits: what the gradient takes
+
+
+def _head(hidden, weight, target):
+    """(hidden's and weight's matrix, the targets' address, flags) of a head's call."""
+    mh, mw = _matrix(hidden, "hidden"), _matrix(weight, "weight")
+    if mw.cols != mh.cols or mw.type != mh.type:
+        raise ValueError(f"weight has a row of {mh.cols} values for each word, of hidden's type: got {mw.rows} x {mw.cols} in {weight.dtype}")
+    if not isinstance(target, torch.Tensor) or target.dtype not in (torch.int64, torch.int32):
+        raise ValueError("target must be an int64 or int32 tensor")
+    pt = _plain(target, "target", target.dtype, mh.rows, hidden.device)
+    _same_device(hidden.device, weight)
+    return mh, mw, pt, dgs.DGS_TARGET_I64 if target.dtype == torch.int64 else 0
+
+
+def vocabulary_loss(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor) -> VocabularyLoss:
+    """Softmax cross entropy of hidden states [..., width] against a vocabulary [words, width] of their type, a loss for each row, without keeping the
+    logits.  target: int64 or int32, a word for each row; below 0: the row is ignored (loss 0)."""
+    mh, mw, pt, flags = _head(hidden, weight, target)
+    _cut_off(hidden, "hidden", "vocabulary_loss")
+    _cut_off(weight, "weight", "vocabulary_loss")
+    device = hidden.device
+    need = dgs.dgs_vocabulary_loss_bytes(mh, mw)
+    loss, lse = torch.empty(target.shape, dtype=torch.float32, device=device), torch.empty(target.shape, dtype=torch.float32, device=device)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _enqueue(device, dgs.dgs_vocabulary_loss, mh, mw, pt, flags, loss.data_ptr(), lse.data_ptr(), work.data_ptr() if need else 0, need)
+    return VocabularyLoss(loss, lse)
+
+
+def vocabulary_loss_grad(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                         dw: Optional[torch.Tensor] = None, *, add: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of vocabulary_loss: returns that of the hidden states, of their type, and writes (with `add`, adds) the vocabulary's to dw, a
+    contiguous float32 tensor of words * width elements such as the layer's slice of the flat gradient.  dloss: float32, one for each row or one for all."""
+    mh, mw, pt, flags = _head(hidden, weight, target)
+    device = hidden.device
+    if add:
+        flags |= dgs.DGS_LOSS_ADD
+    one = isinstance(dloss, torch.Tensor) and dloss.numel() == 1
+    pl = _plain(lse, "lse", torch.float32, mh.rows, device)
+    pg = _plain(dloss, "dloss", torch.float32, 1 if one else mh.rows, device)
+    pw = _plain(dw, "dw", torch.float32, mw.rows * mw.cols, device)
+    if (mh.rows and not pl) or not isinstance(dloss, torch.Tensor):
+        raise ValueError("lse and dloss are tensors")
+    if out is None:
+        out = torch.empty(hidden.shape, dtype=hidden.dtype, device=device)
+    mo = _matrix(out, "out")
+    _fit(mo, "out", mh.rows, mh.cols, mh.type)
+    _same_device(device, out)
+    need = dgs.dgs_vocabulary_loss_grad_bytes(mh, mw)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _enqueue(device, dgs.dgs_vocabulary_loss_grad, mh, mw, pt, pl, pg, 0 if one else 1, mo, pw, flags, work.data_ptr() if need else 0, need)
+    return out
