@@ -480,7 +480,7 @@ enum { DGS_TARGET_I64 = 1u << 0, /* targets are i64, 8-byte aligned; without it 
  * what the gradient takes.  Products of 16-bit types are exact, f32 values are taken as 22 bits under a power of two for each row; sums are in f32.  A row whose
  * logits hold a NaN or +inf has NaN for both.
  * workspace: DEVICE, 256-byte aligned, at least what dgs_vocabulary_loss_bytes says for these arguments (data pointers included: their alignment counts).  It takes
- * 8 bytes for each row and 128 words, and copies of f32 matrices (4 bytes a value) and of those whose rows do not begin on 16 bytes (2 bytes).
+ * 8 bytes for each row and 64 words, and copies of f32 matrices (4 bytes a value) and of those whose rows do not begin on 16 bytes (2 bytes).
  * width at most 2^24, rows and words 2^30, rows or words times width 2^38, else DGS_ELIMIT. */
 int dgs_vocabulary_loss_bytes(const dgs_matrix* hidden, const dgs_matrix* weight, uint64_t* out_bytes);
 int dgs_vocabulary_loss(const dgs_matrix* hidden, const dgs_matrix* weight, const void* target, uint32_t flags, float* loss, float* lse, void* workspace,

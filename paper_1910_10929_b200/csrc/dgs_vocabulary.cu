@@ -3,7 +3,7 @@
 // With hidden states h [N][D], a vocabulary W [V][D] and z = h W^T:
 //     loss[r] = lse[r] - z[r][target[r]],  lse[r] = log(sum over v of exp z[r][v]),
 //     s[r][v] = dloss[r] (exp(z[r][v] - lse[r]) - [v = target[r]]),  dh = s W,  dW = s^T h.
-// The loss keeps a maximum and a sum for each row and 128 words of a tile of logits, which stay in registers.  The gradient goes through the vocabulary in
+// The loss keeps a maximum and a sum for each row and 64 words of a tile of logits, which stay in registers.  The gradient goes through the vocabulary in
 // pieces: the logits of a piece are formed again, s of the piece goes to the workspace, and its products with W and h are formed from there.
 //
 // Numbers: s is kept as the sum of two fp16 numbers (22 bits) under one power of two for the call, since dW goes to a flat gradient in f32; products of fp16 need
@@ -29,33 +29,35 @@ __device__ __forceinline__ void bulk_load(uint32_t to, const void* from, uint32_
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar)
                : "memory");
 }
-__device__ __forceinline__ void bulk_store(void* to, uint32_t from, uint32_t bytes) {
-  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n cp.async.bulk.commit_group;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
+// 32 bytes that are nobody else's: a whole sector.
+__device__ __forceinline__ void store_sector(void* to, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
 }
-__device__ __forceinline__ void bulk_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void bulk_stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// *to += v, without waiting for what is there.  The only thread that adds to it in this kernel, so the sum's order is that of the kernels.
+__device__ __forceinline__ void add_behind(float* to, float v) { asm volatile("red.global.add.f32 [%0], %1;" ::"l"(to), "f"(v) : "memory"); }
 
-// What the kernel forms: maxima and sums of logits; s of a piece; dW of a piece from s and h; dh's part of a piece from s and W.
-enum : int { kLoss, kSlope, kWords, kHidden };
-template <int MODE> constexpr bool kFromPiece = MODE == kWords || MODE == kHidden;
+// What the kernel forms: maxima and sums of logits; s of a piece; the products of a piece's s with h (dW) and with W (dh's part).
+enum : int { kLoss, kSlope, kGrads };
 
-// A pair of CTAs forms tiles of 256 x n, 128 rows and n columns of it in each CTA's tensor memory.  A step contracts kRows values of the operands' PA and PB
-// parts; a CTA brings 128 rows (or columns) of the first operand and n / 2 of the second, 256 bytes a value contracted.
+// A pair of CTAs forms tiles of 256 x 256, 128 rows and 256 columns of it in each CTA's tensor memory.  A step contracts kRows values of the operands' PA and PB
+// parts; a CTA brings 128 rows (or columns) of either operand, 256 bytes a value contracted.
 //   contracted dimension contiguous (h and W for the logits, s for dh): blocks of 64 values contracted, 128 rows of 128 bytes each
 //   contracted dimension outermost (h and s for dW, W for dh): blocks of 64 columns, kRows rows of 128 bytes each
 // Either way the 16-byte pieces of a row are exchanged by its number (128-byte swizzle).  s lies in the workspace in blocks of 128 rows and 64 columns that are in
 // that order already, so both uses copy it as it is.
-template <uint32_t PA, uint32_t PB> struct Step {
-  static constexpr uint32_t kRows = PA * PB == 1 ? 128 : 64, kTile = kRows * 256, kStage = (PA + PB) * kTile, kStages = 192 * 1024 / kStage;
-};
-// Steps between two sums in registers.  Logits: each step, since an exponential takes a logit's error as it is (a logit of 15 summed over 768 values in one go is off by
-// 7e-6, a step at a time by 1.5e-6).  Sums of s: 512 rows, 256 where each is three products.
-template <int MODE, uint32_t PA, uint32_t PB> constexpr uint32_t kChunkSteps = !kFromPiece<MODE> ? 1 : PA == 2 ? 4 : 512 / Step<PA, PB>::kRows;
+// kChunk: steps between two sums in registers, at most: 512 values, or 256 where each is three products.  Logits of few steps take half of them: an exponential takes a
+// logit's error as it is (a logit of 15 summed over 768 values in one go is off by 7e-6), and two chunks a tile let the products of the next tile run to their
+// end while one is finished.
 constexpr uint32_t kBlockBytes = 128 * 128;                       // 128 rows and 64 columns of s
-constexpr uint32_t kStageBytes = 32 * 1024;                       // s on its way out: 4 KB a warp
-constexpr uint32_t kSmem = 1024 + 192 * 1024 + kStageBytes;
-constexpr uint32_t kHeadThreads = 384, kHeadRegs = 168, kHeadRegsSum = 216, kHeadRegsRest = 72;
-static_assert(kHeadRegsSum * 256 + kHeadRegsRest * 128 <= kHeadRegs * kHeadThreads, "setmaxnreg draws on the launch's registers");
+template <int MODE, uint32_t PA, uint32_t PB> struct Step {
+  static constexpr uint32_t kRows = MODE != kGrads && PA == 1 ? 128 : 64, kTile = kRows * 256, kStage = (PA + PB) * kTile;
+  static constexpr uint32_t kStages = 192 * 1024 / kStage, kChunk = 512 / kRows / PA, kSmem = 1024 + kStages * kStage;
+};
+// Sixteen warps keep the sums, 64 columns of 32 rows each; four do the rest and leave them their registers.  (With eight warps of 128 columns, two a scheduler, the
+// trips to tensor memory and through the exponentials showed: 5632 words of 8192 x 768 took 105 us.)
+constexpr uint32_t kSumWarps = 16, kHeadThreads = kSumWarps * 32 + 128, kHeadRegs = 96, kHeadRegsSum = 104, kHeadRegsRest = 64;
+static_assert(kHeadRegsSum * kSumWarps * 32 + kHeadRegsRest * 128 <= kHeadRegs * kHeadThreads, "setmaxnreg draws on the launch's registers");
 constexpr uint32_t kHeadTmem = 512;                               // two accumulators of 256 columns
 
 // k: which sixteen of the values contracted.
@@ -66,6 +68,15 @@ template <uint32_t R>
 __device__ __forceinline__ uint64_t desc_outer(uint32_t tile, uint32_t k) {
   return uint64_t(((tile + k * 2048) >> 4) & 0x3fff) | uint64_t(R * 128 >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
 }
+__device__ __forceinline__ void tmem_load16(uint32_t at, float (&v)[16]) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+        "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(at));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
 
 // The power of two that takes a largest magnitude (its bits) to [2^14, 2^15), kept where it is a normal number, and its reciprocal.  Infinities and NaN: 1.
 __device__ __forceinline__ float up_of(uint32_t largest) {
@@ -75,11 +86,16 @@ __device__ __forceinline__ float up_of(uint32_t largest) {
 }
 __device__ __forceinline__ float down_of(uint32_t largest) { return __uint_as_float((254u << 23) - __float_as_uint(up_of(largest))); }
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNone = -__builtin_huge_valf();
 
+// One of the two products of a piece's s.
+struct Product {
+  uint32_t m_tiles, n_tiles, splits, tiles, steps, parts;   // steps over the whole contraction; parts of s that it takes
+  float* out;
+};
 struct Head {
   uint32_t rows, width, words;      // N, D, V
-  uint32_t m_tiles, n_tiles, n, splits, tiles;
-  uint32_t steps;                   // over the whole contraction
+  uint32_t m_tiles, n_tiles, tiles, steps, chunk;   // logits
   uint32_t first_word, piece_cols;  // of the piece (a multiple of 256 in the workspace)
   uint32_t row_blocks;              // of s
   uint32_t idesc;
@@ -88,10 +104,11 @@ struct Head {
   const float *lse, *dloss;
   const uint32_t *most_h, *most_w, *most_g;     // bits of the largest magnitudes: of each column of h and of W, of dloss
   const float *row_h, *row_w;       // f32: what the rows of the logits' operands are multiplied with
-  float2* partial;                  // [n_tiles * 2][rows]: maximum, sum
+  float2* partial;                  // [n_tiles * 4][rows]: maximum, sum
   float* at_target;                 // [rows]
   unsigned char* s;                 // [2][row_blocks][piece_cols / 64] blocks
-  float* out;                       // dw, or partial results [splits][...]
+  Product dw, dh;                   // out: dw or partial results [splits][piece_cols][width]; [splits][rows][width]
+  uint32_t share_few, share_more;   // tiles of dh for a pair of CTAs with one more tile of dw, and for others
   uint32_t add, first_piece;
   int* status;
 };
@@ -108,54 +125,69 @@ __device__ __forceinline__ int target_of(const Head& a, uint32_t row, bool tell)
 
 struct HeadTile {
   uint32_t m0, n0, split, from, steps;
+  bool hidden;
 };
-// Tiles go down the rows first, 32 tiles of them at a time: the pairs work on few words together, and on rows that the second cache holds.
+// A pair's i-th tile; false behind its last.  Logits go down the rows first, 32 tiles of them at a time: the pairs work on few words together, and on rows that the
+// second cache holds.  Of the two products with s, dW's tiles are dealt out first, then dh's, more to the pairs that got fewer of the others: one launch of
+// both keeps 74 pairs busy where 66 tiles of dW and 96 of dh would not (155 us for 199).
 template <int MODE>
-__device__ __forceinline__ HeadTile head_tile(const Head& a, uint32_t tile) {
-  HeadTile t;
-  t.split = 0;
-  if constexpr (kFromPiece<MODE>) {
-    t.m0 = tile % a.m_tiles * 256;
-    tile /= a.m_tiles;
-    t.n0 = tile % a.n_tiles * a.n;
-    t.split = tile / a.n_tiles;
-  } else {
+__device__ __forceinline__ bool head_tile(const Head& a, uint32_t pair, uint32_t pairs, uint32_t i, HeadTile* t) {
+  t->hidden = false;
+  t->split = t->from = 0;
+  if constexpr (MODE != kGrads) {
+    const uint32_t tile = i * pairs + pair;
+    if (tile >= a.tiles) return false;
     const uint32_t group = tile / (32 * a.n_tiles), rows = min(32u, a.m_tiles - group * 32), in = tile - group * 32 * a.n_tiles;
-    t.m0 = (group * 32 + in % rows) * 256;
-    t.n0 = in / rows * a.n;
+    t->m0 = (group * 32 + in % rows) * 256;
+    t->n0 = in / rows * 256;
+    t->steps = a.steps;
+    return true;
+  } else {
+    const uint32_t some = a.dw.tiles % pairs, first = a.dw.tiles / pairs + (pair < some ? 1 : 0);
+    uint32_t tile = i * pairs + pair;
+    if (i >= first) {
+      const uint32_t j = i - first, share = pair < some ? a.share_few : a.share_more;
+      tile = (pair < some ? pair * share : some * a.share_few + (pair - some) * share) + j;
+      if (j >= share || tile >= a.dh.tiles) return false;
+      t->hidden = true;
+    }
+    const Product& p = t->hidden ? a.dh : a.dw;
+    t->m0 = tile % p.m_tiles * 256;
+    tile /= p.m_tiles;
+    t->n0 = tile % p.n_tiles * 256;
+    t->split = tile / p.n_tiles;
+    const uint32_t each = (p.steps + p.splits - 1) / p.splits;
+    t->from = min(t->split * each, p.steps);
+    t->steps = min(each, p.steps - t->from);
+    return true;
   }
-  const uint32_t each = (a.steps + a.splits - 1) / a.splits;
-  t.from = min(t.split * each, a.steps);
-  t.steps = min(each, a.steps - t.from);
-  return t;
 }
 
-// Warps: 0 to 7 keep the sums, 8 issues products, 9 copies, 10 passes on that copies have landed.  Accumulators go to registers every kChunk steps, since
-// the tensor cores add with bits cut off, and are added up there with rounding.  One pair of CTAs per pair of SMs takes tile after tile, so that the
-// products of the next run while one is finished.
-template <int MODE, uint32_t PA, uint32_t PB>
+// Warps: 0 to 15 keep the sums, 16 issues products, 17 and 19 copies (one operand each), 18 passes on that copies have landed.  Accumulators go to registers every
+// kChunk steps, since the tensor cores add with bits cut off, and are added up there with rounding.  One pair of CTAs per pair of SMs takes tile after tile,
+// so that the products of the next run while one is finished.
+template <int MODE, uint32_t PA, uint32_t PB, uint32_t PH>   // PH: parts of s that dh takes
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
 k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
-  using S = Step<PA, PB>;
-  constexpr uint32_t R = S::kRows, ST = S::kStages, CH = kChunkSteps<MODE, PA, PB>, TILE = S::kTile;
-  constexpr bool kOuterA = kFromPiece<MODE>, kOuterB = MODE == kWords;
+  using S = Step<MODE, PA, PB>;
+  constexpr uint32_t R = S::kRows, ST = S::kStages, TILE = S::kTile;
   extern __shared__ unsigned char raw[];
   __shared__ __align__(8) uint64_t s_full[ST], s_empty[ST], s_loaded[ST], s_sum_full[2], s_sum_empty[2], s_done;
   __shared__ uint32_t s_tmem;
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = cta_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
-  const uint32_t stages = (smem_at(raw) + 1023u) & ~1023u, half = a.n / 2;
+  const uint32_t stages = (smem_at(raw) + 1023u) & ~1023u, CH = MODE == kGrads ? S::kChunk : a.chunk;
 
-  if (warp == 8) {
+  if (warp == kSumWarps) {
     tmem_alloc(&s_tmem, kHeadTmem);
     if (lane == 0) {
       for (uint32_t s = 0; s < ST; ++s) {
         bar_init(smem_at(&s_full[s]), 2);    // that copies landed, of both CTAs
         bar_init(smem_at(&s_empty[s]), 1);
-        bar_init(smem_at(&s_loaded[s]), 1);
+        bar_init(smem_at(&s_loaded[s]), 2);  // of both operands
       }
       for (uint32_t i = 0; i < 2; ++i) {
         bar_init(smem_at(&s_sum_full[i]), 1);
-        bar_init(smem_at(&s_sum_empty[i]), 16);
+        bar_init(smem_at(&s_sum_empty[i]), 2 * kSumWarps);
       }
       bar_init(smem_at(&s_done), 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -170,71 +202,93 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
   const uint32_t tmem = s_tmem;
   wait_for_last_kernel();   // nothing above touches memory outside the SM
   __syncwarp();
-  if (warp >= 8) {
+  if (warp >= kSumWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHeadRegsRest));
-    if (warp == 8 && lane == 0 && rank == 0) {
+    HeadTile w;
+    if (warp == kSumWarps && lane == 0 && rank == 0) {
       bool alive = true;
-      uint32_t it = 0, chunk = 0;
-      const uint32_t idesc = a.idesc | uint32_t(kOuterA) << 15 | uint32_t(kOuterB) << 16 | idesc_cols(a.n);
-      for (uint32_t tile = pair; tile < a.tiles && alive; tile += pairs) {
-        const HeadTile w = head_tile<MODE>(a, tile);
+      uint32_t it = 0, chunk = 0, in = 0;   // in: steps of the chunk
+      const auto products = [&](auto outer_a, auto outer_b, auto parts_b, uint32_t acc, uint32_t at, uint32_t bt, bool first) {
+        constexpr bool kOuterA = decltype(outer_a)::value, kOuterB = decltype(outer_b)::value;
+        const uint32_t idesc = a.idesc | uint32_t(kOuterA) << 15 | uint32_t(kOuterB) << 16 | idesc_cols(256);
+#pragma unroll
+        for (uint32_t k = 0; k < R / 16; ++k) {
+#pragma unroll
+          for (uint32_t i = 0; i < PA; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < decltype(parts_b)::value; ++j)
+              if (i + j < 2) {
+                const uint64_t ad = kOuterA ? desc_outer<R>(at + i * TILE, k) : desc_inner(at + i * TILE, k);
+                const uint64_t bd = kOuterB ? desc_outer<R>(bt + j * TILE, k) : desc_inner(bt + j * TILE, k);
+                mma(acc, ad, bd, idesc, !first || k || i || j);
+              }
+        }
+      };
+      using Yes = std::true_type;
+      using No = std::false_type;
+      for (uint32_t i = 0; alive && head_tile<MODE>(a, pair, pairs, i, &w); ++i) {
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           const uint32_t st = it % ST, at = stages + st * S::kStage, bt = at + PA * TILE, acc = tmem + (chunk & 1) * 256;
-          if (s % CH == 0 && chunk >= 2) alive = bar_wait(smem_at(&s_sum_empty[chunk & 1]), (chunk / 2 - 1) & 1);
+          const bool begins = in == 0;
+          if (begins && chunk >= 2) alive = bar_wait(smem_at(&s_sum_empty[chunk & 1]), (chunk / 2 - 1) & 1);
           alive = alive && bar_wait(smem_at(&s_full[st]), it / ST & 1);
           if (!alive) break;
           tmem_after();
-#pragma unroll
-          for (uint32_t k = 0; k < R / 16; ++k) {
-#pragma unroll
-            for (uint32_t i = 0; i < PA; ++i)
-#pragma unroll
-              for (uint32_t j = 0; j < PB; ++j)
-                if (i + j < 2) {
-                  const uint64_t ad = kOuterA ? desc_outer<R>(at + i * TILE, k) : desc_inner(at + i * TILE, k);
-                  const uint64_t bd = kOuterB ? desc_outer<R>(bt + j * TILE, k) : desc_inner(bt + j * TILE, k);
-                  mma(acc, ad, bd, idesc, s % CH || k || i || j);
-                }
+          if constexpr (MODE == kGrads) {
+            if (w.hidden) products(Yes{}, No{}, std::integral_constant<uint32_t, PH>{}, acc, at, bt, begins);
+            else products(Yes{}, Yes{}, std::integral_constant<uint32_t, PB>{}, acc, at, bt, begins);
+          } else {
+            products(No{}, No{}, std::integral_constant<uint32_t, PB>{}, acc, at, bt, begins);
           }
           mma_commit(smem_at(&s_empty[st]));
-          if (s % CH == CH - 1 || s == w.steps - 1) mma_commit(smem_at(&s_sum_full[chunk++ & 1]));
+          if (++in == CH || s == w.steps - 1) {
+            mma_commit(smem_at(&s_sum_full[chunk++ & 1]));
+            in = 0;
+          }
         }
       }
       mma_commit(smem_at(&s_done));   // waited for in both CTAs, at the end: nothing is under way when tensor memory is given back
       if (!alive) report(a.status, DGS_ETIMEOUT);
     }
-    if (warp == 9 && lane == 0) {
+    if ((warp == kSumWarps + 1 || warp == kSumWarps + 3) && lane == 0) {
+      const bool second = warp == kSumWarps + 3;   // of the two operands
       bool alive = true;
       uint32_t it = 0;
       const uint32_t col_blocks = a.piece_cols / 64;
       const uint64_t plane = uint64_t(a.row_blocks) * col_blocks * kBlockBytes;
-      for (uint32_t tile = pair; tile < a.tiles && alive; tile += pairs) {
-        const HeadTile w = head_tile<MODE>(a, tile);
-        const uint32_t m = w.m0 + rank * 128, n = w.n0 + rank * half;
+      for (uint32_t i = 0; alive && head_tile<MODE>(a, pair, pairs, i, &w); ++i) {
+        const uint32_t m = w.m0 + rank * 128, n = w.n0 + rank * 128;
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           const uint32_t st = it % ST, at = stages + st * S::kStage, bt = at + PA * TILE, bar = smem_at(&s_loaded[st]), k0 = (w.from + s) * R;
           if (it >= ST && !(alive = bar_wait(smem_at(&s_empty[st]), (it / ST - 1) & 1))) break;
-          bar_expect(bar, PA * TILE + PB * (kFromPiece<MODE> ? R * half * 2 : TILE));
+          if (!second) {
+            bar_expect(bar, PA * TILE);
 #pragma unroll
-          for (uint32_t i = 0; i < PA; ++i) {
-            if constexpr (kOuterA) {
-              for (uint32_t b = 0; b < 2; ++b) tma_load3(at + i * TILE + b * R * 128, &map_a, int(m + b * 64), int((MODE == kHidden ? a.first_word : 0) + k0), int(i), bar);
-            } else {
-              for (uint32_t b = 0; b < R / 64; ++b) tma_load3(at + i * TILE + b * kBlockBytes, &map_a, int(k0 + b * 64), int(m), int(i), bar);
+            for (uint32_t p = 0; p < PA; ++p) {
+              if constexpr (MODE == kGrads) {
+                for (uint32_t b = 0; b < 2; ++b)
+                  tma_load3(at + p * TILE + b * R * 128, w.hidden ? &map_b : &map_a, int(m + b * 64), int(k0 + (w.hidden ? a.first_word : 0)), int(p), bar);
+              } else {
+                for (uint32_t b = 0; b < R / 64; ++b) tma_load3(at + p * TILE + b * kBlockBytes, &map_a, int(k0 + b * 64), int(m), int(p), bar);
+              }
             }
-          }
+          } else if constexpr (MODE == kGrads) {
+            bar_expect(bar, (w.hidden ? PH : PB) * TILE);
 #pragma unroll
-          for (uint32_t j = 0; j < PB; ++j) {
-            const unsigned char* from = a.s + j * plane;
-            if constexpr (MODE == kWords) {   // rows k0 on of n / 2 columns
-              for (uint32_t b = 0; b < half / 64; ++b)
-                bulk_load(bt + j * TILE + b * R * 128, from + (uint64_t(k0 / 128) * col_blocks + n / 64 + b) * kBlockBytes + k0 % 128 * 128, R * 128, bar);
-            } else if constexpr (MODE == kHidden) {   // columns k0 on of n / 2 rows
-              for (uint32_t b = 0; b < R / 64; ++b)
-                bulk_load(bt + j * TILE + b * kBlockBytes, from + (uint64_t(n / 128) * col_blocks + k0 / 64 + b) * kBlockBytes + n % 128 * 128, half * 128, bar);
-            } else {
-              for (uint32_t b = 0; b < R / 64; ++b) tma_load3(bt + j * TILE + b * kBlockBytes, &map_b, int(k0 + b * 64), int(a.first_word + n), int(j), bar);
+            for (uint32_t p = 0; p < PB; ++p) {
+              const unsigned char* from = a.s + p * plane;
+              if (!w.hidden) {   // rows k0 on of 128 columns
+                for (uint32_t b = 0; b < 2; ++b)
+                  bulk_load(bt + p * TILE + b * R * 128, from + (uint64_t(k0 / 128) * col_blocks + n / 64 + b) * kBlockBytes + k0 % 128 * 128, R * 128, bar);
+              } else if (p < PH) {   // columns k0 on of 128 rows
+                bulk_load(bt + p * TILE, from + (uint64_t(n / 128) * col_blocks + k0 / 64) * kBlockBytes, kBlockBytes, bar);
+              }
             }
+          } else {
+            bar_expect(bar, PB * TILE);
+#pragma unroll
+            for (uint32_t p = 0; p < PB; ++p)
+              for (uint32_t b = 0; b < R / 64; ++b) tma_load3(bt + p * TILE + b * kBlockBytes, &map_b, int(k0 + b * 64), int(a.first_word + n), int(p), bar);
           }
         }
       }
@@ -245,12 +299,11 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
       }
       if (!alive) report(a.status, DGS_ETIMEOUT);
     }
-    if (warp == 10 && lane == 0) {
+    if (warp == kSumWarps + 2 && lane == 0) {
       bool alive = true;
       uint32_t it = 0;
-      for (uint32_t tile = pair; tile < a.tiles && alive; tile += pairs) {
-        const uint32_t steps = head_tile<MODE>(a, tile).steps;
-        for (uint32_t s = 0; s < steps; ++s, ++it) {
+      for (uint32_t i = 0; alive && head_tile<MODE>(a, pair, pairs, i, &w); ++i) {
+        for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           if (!(alive = bar_wait(smem_at(&s_loaded[it % ST]), it / ST & 1))) break;
           bar_arrive_cluster(in_leader(smem_at(&s_full[it % ST])));
         }
@@ -260,40 +313,34 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kHeadRegsSum));
     const uint32_t quarter = warp % 4, group = warp / 4, mine = rank * 128 + quarter * 32 + lane;
-    const uint32_t cols = kFromPiece<MODE> ? half : 128;   // of the tile that a thread has
     bool alive = true;
     uint32_t drained = 0;
-    for (uint32_t tile = pair; tile < a.tiles && alive; tile += pairs) {
-      const HeadTile w = head_tile<MODE>(a, tile);
-      const uint32_t chunks = (w.steps + CH - 1) / CH, row = w.m0 + mine;
-      const uint32_t col0 = w.n0 + group * cols;
+    HeadTile w;
+    const float up_g = MODE == kSlope ? up_of(*a.most_g) : 0.0f;
+    for (uint32_t ordinal = 0; alive && head_tile<MODE>(a, pair, pairs, ordinal, &w); ++ordinal) {
+      const uint32_t chunks = (w.steps + CH - 1) / CH, row = w.m0 + mine, col0 = w.n0 + group * 64;
       // what the end of the tile needs comes while its products are formed
       int target = -1;
-      float lse = 0.0f, g = 0.0f, by = 1.0f;
-      if constexpr (!kFromPiece<MODE>) {
+      float lse = 0.0f, by = 1.0f;   // by: dloss; f32 logits: what the row is multiplied with
+      if constexpr (MODE != kGrads) {
         if (row < a.rows) {
           target = target_of(a, row, false);
-          if constexpr (PA == 2) by = a.row_h[row];
-          if (MODE == kSlope && target >= 0) lse = a.lse[row], g = a.dloss[uint64_t(row) * a.dloss_step] * up_of(*a.most_g);
+          if (MODE == kSlope && target >= 0) lse = a.lse[row], by = a.dloss[uint64_t(row) * a.dloss_step];
         }
-      } else if (row < a.width) {
-        by = down_of(MODE == kWords ? a.most_h[row] : a.most_w[row]);
       }
-      float acc[128];
+      float acc[64];
 #pragma unroll
-      for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
+      for (int i = 0; i < 64; ++i) acc[i] = 0.0f;
       for (uint32_t c = 0; c < chunks; ++c, ++drained) {
         const uint32_t buf = drained & 1;
         if (!(alive = warp_wait(smem_at(&s_sum_full[buf]), drained / 2 & 1))) break;
         tmem_after();
 #pragma unroll
         for (uint32_t q = 0; q < 4; ++q) {
-          if (!kFromPiece<MODE> || q * 32 < cols) {
-            float v[32];
-            tmem_load32(tmem + (quarter * 32 << 16) + buf * 256 + group * cols + q * 32, v);
+          float v[16];
+          tmem_load16(tmem + (quarter * 32 << 16) + buf * 256 + group * 64 + q * 16, v);
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) add_to(acc[q * 32 + i], acc[q * 32 + i + 1], v[i], v[i + 1]);
-          }
+          for (int i = 0; i < 16; i += 2) add_to(acc[q * 16 + i], acc[q * 16 + i + 1], v[i], v[i + 1]);
         }
         tmem_before();
         __syncwarp();
@@ -301,125 +348,108 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
       }
       if (!alive) break;
 
-      if constexpr (!kFromPiece<MODE>) {
+      if constexpr (MODE != kGrads) {
         if (MODE == kLoss && w.m0 + rank * 128 + quarter * 32 >= a.rows) continue;   // no row of the warp's
         const uint32_t word0 = a.first_word + col0;
         if constexpr (PA == 2) {
+          const float row_by = row < a.rows ? a.row_h[row] : 0.0f;
 #pragma unroll
-          for (int i = 0; i < 128; ++i) acc[i] = acc[i] * by * (word0 + i < a.words ? a.row_w[word0 + i] : 0.0f);
+          for (uint32_t i = 0; i < 64; ++i) {
+            acc[i] = acc[i] * row_by * (word0 + i < a.words ? a.row_w[word0 + i] : 0.0f);
+            if (i % 8 == 7) asm volatile("" ::: "memory");   // not all of them on their way at once
+          }
         }
-        if (word0 + 128 > a.words) {
+        if (word0 + 64 > a.words) {
 #pragma unroll
-          for (uint32_t i = 0; i < 128; ++i)
-            if (word0 + i >= a.words) acc[i] = __uint_as_float(0xff800000u);
+          for (uint32_t i = 0; i < 64; ++i)
+            if (word0 + i >= a.words) acc[i] = kNone;
         }
         const uint32_t at = uint32_t(target) - word0;   // the target's column, if it is one of the thread's
-        const bool has = __any_sync(0xffffffffu, target >= 0 && at < 128);
+        const bool has = __any_sync(0xffffffffu, target >= 0 && at < 64);
         if constexpr (MODE == kLoss) {
           if (has) {
             float z = 0.0f;
 #pragma unroll
-            for (uint32_t i = 0; i < 128; ++i) z = at == i ? acc[i] : z;
-            if (target >= 0 && at < 128) a.at_target[row] = z;
+            for (uint32_t i = 0; i < 64; ++i) z = at == i ? acc[i] : z;
+            if (target >= 0 && at < 64) a.at_target[row] = z;
           }
           float most = acc[0];
 #pragma unroll
-          for (int i = 1; i < 128; ++i) most = fmaxf(most, acc[i]);
-          const float from = most == __uint_as_float(0xff800000u) ? 0.0f : most;
+          for (int i = 1; i < 64; ++i) most = fmaxf(most, acc[i]);
+          const float from = most == kNone ? 0.0f : most;
           float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
-          for (int i = 0; i < 128; i += 2) {
+          for (int i = 0; i < 64; i += 2) {
             const float2 d = mul2(add2(make_float2(acc[i], acc[i + 1]), both(-from)), both(kLog2e));
             sum = add2(sum, make_float2(hardware_exp2(d.x), hardware_exp2(d.y)));
           }
-          if (row < a.rows) a.partial[uint64_t(col0 / 128) * a.rows + row] = make_float2(most, sum.x + sum.y);
+          if (row < a.rows) a.partial[uint64_t(col0 / 64) * a.rows + row] = make_float2(most, sum.x + sum.y);
         } else {
           if (target < 0) {   // whatever the row's logits are
 #pragma unroll
-            for (int i = 0; i < 128; ++i) acc[i] = __uint_as_float(0xff800000u);
+            for (int i = 0; i < 64; ++i) acc[i] = kNone;
           }
-#pragma unroll
-          for (int i = 0; i < 128; i += 2) {
-            const float2 d = mul2(add2(make_float2(acc[i], acc[i + 1]), both(-lse)), both(kLog2e));
-            const float2 v = mul2(make_float2(hardware_exp2(d.x), hardware_exp2(d.y)), both(g));
-            acc[i] = v.x, acc[i + 1] = v.y;
-          }
-          if (has) {
-            const float minus = target >= 0 ? g : 0.0f;
-#pragma unroll
-            for (uint32_t i = 0; i < 128; ++i)
-              if (at == i) acc[i] -= minus;
-          }
-          // two fp16 numbers each, a pair's first parts in the place of its first number
-          uint32_t* const bits = reinterpret_cast<uint32_t*>(acc);
-#pragma unroll
-          for (int i = 0; i < 128; i += 2) {
-            const __half2 hi = __floats2half2_rn(acc[i], acc[i + 1]);
-            const float2 f = __half22float2(hi);
-            const __half2 lo = __floats2half2_rn(acc[i] - f.x, acc[i + 1] - f.y);
-            memcpy(&bits[i], &hi, 4);
-            memcpy(&bits[i + 1], &lo, 4);
-          }
-          // a warp's 32 rows of a block lie together: one copy of 4 KB
-          const uint32_t stage = stages + 192 * 1024 + warp * 4096, col_blocks = a.piece_cols / 64;
+          const float g = target < 0 ? 0.0f : by * up_g;
+          // Sixteen columns at a time: 32 bytes of a block's row for each of s's parts, its two pieces exchanged by the lowest bit of the row's number.  (By way of
+          // shared memory and copies of 4 KB, the fences and the waits for the buffer took 3000 cycles of a tile's 13,000.)
+          const uint32_t col_blocks = a.piece_cols / 64, turn = lane & 7;
+          unsigned char* const to = a.s + (uint64_t(w.m0 / 128 + rank) * col_blocks + col0 / 64) * kBlockBytes + (quarter * 32 + lane) * 128;
           const uint64_t plane = uint64_t(a.row_blocks) * col_blocks * kBlockBytes;
-          unsigned char* const to = a.s + (uint64_t(w.m0 / 128 + rank) * col_blocks + col0 / 64) * kBlockBytes + quarter * 4096;
 #pragma unroll
-          for (uint32_t b = 0; b < 2; ++b)
+          for (uint32_t q = 0; q < 4; ++q) {
+            uint32_t part[2][8];
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {
+              const uint32_t c = q * 16 + i * 2;
+              const float2 d = mul2(add2(make_float2(acc[c], acc[c + 1]), both(-lse)), both(kLog2e));
+              float2 v = mul2(make_float2(hardware_exp2(d.x), hardware_exp2(d.y)), both(g));
+              if (has) {   // g is 0 in a row without a target
+                if (at == c) v.x -= g;
+                if (at == c + 1) v.y -= g;
+              }
+              const __half2 hi = __floats2half2_rn(v.x, v.y);
+              const float2 f = __half22float2(hi);
+              const __half2 lo = __floats2half2_rn(v.x - f.x, v.y - f.y);
+              memcpy(&part[0][i], &hi, 4);
+              memcpy(&part[1][i], &lo, 4);
+            }
 #pragma unroll
             for (uint32_t p = 0; p < 2; ++p) {
-              if (p < a.parts) {
-                if (lane == 0) bulk_stores_read();
-                __syncwarp();
+              uint32_t o[8];
 #pragma unroll
-                for (uint32_t q = 0; q < 8; ++q)
-                  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 128 + ((q ^ (lane & 7)) << 4)), "r"(bits[b * 64 + q * 8 + p]),
-                               "r"(bits[b * 64 + q * 8 + 2 + p]), "r"(bits[b * 64 + q * 8 + 4 + p]), "r"(bits[b * 64 + q * 8 + 6 + p])
-                               : "memory");
-                writes_to_async_proxy();
-                __syncwarp();
-                if (lane == 0) bulk_store(to + p * plane + b * kBlockBytes, stage, 4096);
-              }
+              for (uint32_t i = 0; i < 8; ++i) o[i] = turn & 1 ? part[p][i ^ 4] : part[p][i];
+              if (p < a.parts) store_sector(to + p * plane + ((q * 2 ^ (turn & 6)) << 4), o);
             }
+          }
         }
       } else if (row < a.width) {
         // lanes are neighbours in dW's and dh's rows
-        const uint32_t last = MODE == kWords ? min(a.piece_cols, a.words - a.first_word) : a.rows;   // of the columns of the tile
-        const bool direct = MODE == kWords && a.splits == 1;
-        float* p = a.out + (uint64_t(w.split) * (MODE == kWords ? a.piece_cols : a.rows) + (direct ? a.first_word : 0) + col0) * a.width + row;
-        const float by2 = direct ? down_of(*a.most_g) : 1.0f, by1 = direct ? by : 1.0f;
-        const bool add = MODE == kWords ? direct && a.add : !a.first_piece;
+        const bool direct = !w.hidden && a.dw.splits == 1, add = w.hidden ? !a.first_piece : direct && a.add;
+        const uint32_t end = w.hidden ? a.rows : min(a.piece_cols, a.words - a.first_word), last = col0 < end ? min(64u, end - col0) : 0;   // columns of the thread's
+        float* p = (w.hidden ? a.dh.out : a.dw.out) + (uint64_t(w.split) * (w.hidden ? a.rows : a.piece_cols) + (direct ? a.first_word : 0) + col0) * a.width + row;
+        if (direct) {
+          const float by1 = down_of(a.most_h[row]), by2 = down_of(*a.most_g);
 #pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-          if (q * 32 >= cols) break;
-          if (direct) {
-#pragma unroll
-            for (uint32_t i = 0; i < 32; ++i) acc[q * 32 + i] = acc[q * 32 + i] * by1 * by2;
-          }
-          if (add) {
-            float old[32];
-#pragma unroll
-            for (uint32_t i = 0; i < 32; ++i) old[i] = col0 + q * 32 + i < last ? p[uint64_t(q * 32 + i) * a.width] : 0.0f;
-#pragma unroll
-            for (uint32_t i = 0; i < 32; ++i) acc[q * 32 + i] += old[i];
-          }
-#pragma unroll
-          for (uint32_t i = 0; i < 32; ++i)
-            if (col0 + q * 32 + i < last) p[uint64_t(q * 32 + i) * a.width] = acc[q * 32 + i];
+          for (int i = 0; i < 64; ++i) acc[i] = acc[i] * by1 * by2;
         }
+#pragma unroll
+        for (uint32_t i = 0; i < 64; ++i)
+          if (i < last) {
+            if (add) add_behind(p + uint64_t(i) * a.width, acc[i]);
+            else p[uint64_t(i) * a.width] = acc[i];
+          }
       }
     }
-    if (MODE == kSlope && lane == 0) bulk_stores_done();
     if (!alive && lane == 0) report(a.status, DGS_ETIMEOUT);
   }
   __syncwarp();
   tmem_before();
   __syncthreads();
   // the commit behind the last products arrives in both CTAs: neither leaves before its own
-  if (warp == 8 && lane == 0 && !bar_wait(smem_at(&s_done), 0)) report(a.status, DGS_ETIMEOUT);
+  if (warp == kSumWarps && lane == 0 && !bar_wait(smem_at(&s_done), 0)) report(a.status, DGS_ETIMEOUT);
   __syncwarp();
   pair_sync();
-  if (warp == 8) {
+  if (warp == kSumWarps) {
     __syncwarp();
     tmem_after();
     tmem_free(tmem, kHeadTmem);
@@ -487,27 +517,33 @@ __device__ __forceinline__ void halves(const float2 (&v)[4], Eight<__half>& hi, 
   of_floats(rest, lo);
 }
 // A matrix as P fp16 numbers a value under a power of two for each column: [P][rows][stride].  Ignored rows are zero, whatever they hold.
+constexpr uint32_t kPlaneRows = 64;   // of a CTA
 template <class T, bool VEC, uint32_t P>
-__device__ __forceinline__ void by_columns(const Head& a, const Source& m, bool targets, uint64_t unit, const uint32_t* most, __half* out, uint32_t stride) {
-  const uint32_t lane = threadIdx.x % 32, r = uint32_t(unit / m.spans), col0 = uint32_t(unit - uint64_t(r) * m.spans) * kSpan;
-  if (r >= m.rows) return;
-  Eight<__half> part[2] = {};
-  if (!targets || target_of(a, r, false) >= 0) {
+__device__ __forceinline__ void by_columns(const Head& a, const Source& m, bool targets, uint32_t block, const uint32_t* most, __half* out, uint32_t stride) {
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, col0 = block % m.spans * kSpan, row0 = block / m.spans * kPlaneRows;
+  float2 up[4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t c = col0 + (VEC ? lane * 8 + i : i * 32 + lane);
+    const float v = c < m.cols ? up_of(most[c]) : 1.0f;
+    if (i % 2) up[i / 2].y = v;
+    else up[i / 2].x = v;
+  }
+#pragma unroll 4
+  for (uint32_t r = row0 + warp; r < min(row0 + kPlaneRows, m.rows); r += 8) {
+    Eight<__half> part[2] = {};
     Eight<T> e;
     load8<T, VEC>(static_cast<const T*>(m.data) + r * m.stride, col0, lane, m.cols, e);
-    float2 v[4];
-    floats_of(e, v);
+    if (!targets || target_of(a, r, false) >= 0) {
+      float2 v[4];
+      floats_of(e, v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t c = col0 + (VEC ? lane * 8 + i : i * 32 + lane);
-      const float up = c < m.cols ? up_of(most[c]) : 1.0f;
-      if (i % 2) v[i / 2].y *= up;
-      else v[i / 2].x *= up;
+      for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], up[i]);
+      halves(v, part[0], part[1]);
     }
-    halves(v, part[0], part[1]);
-  }
 #pragma unroll
-  for (uint32_t p = 0; p < P; ++p) store8<__half, VEC>(out + (uint64_t(p) * m.rows + r) * stride, col0, lane, m.cols, part[p]);
+    for (uint32_t p = 0; p < P; ++p) store8<__half, VEC>(out + (uint64_t(p) * m.rows + r) * stride, col0, lane, m.cols, part[p]);
+  }
 }
 template <class T, bool VEC>
 __global__ void __launch_bounds__(256) k_head_columns(const __grid_constant__ Head a, const __grid_constant__ Source h, const __grid_constant__ Source w, uint32_t blocks_h,
@@ -516,9 +552,9 @@ __global__ void __launch_bounds__(256) k_head_columns(const __grid_constant__ He
   let_next_kernel_begin();
   wait_for_last_kernel();
   if (blockIdx.x < blocks_h)
-    by_columns<T, VEC, P>(a, h, true, uint64_t(blockIdx.x) * 8 + threadIdx.x / 32, a.most_h, out_h, stride);
+    by_columns<T, VEC, P>(a, h, true, blockIdx.x, a.most_h, out_h, stride);
   else
-    by_columns<T, VEC, P>(a, w, false, uint64_t(blockIdx.x - blocks_h) * 8 + threadIdx.x / 32, a.most_w, out_w, stride);
+    by_columns<T, VEC, P>(a, w, false, blockIdx.x - blocks_h, a.most_w, out_w, stride);
 }
 
 // The logits' operands where TMA copies cannot take them from the caller's memory: 16-bit matrices moved onto 16 bytes, f32 ones as two fp16 numbers a value under a
@@ -566,55 +602,92 @@ __global__ void __launch_bounds__(256) k_head_rows(const __grid_constant__ Sourc
 }
 
 // ---- behind the products --------------------------------------------------------------------------
-// A row's parts joined in their order: 32 rows a CTA, each eighth part a warp.
+// A row's parts joined in their order: 32 rows a CTA, each eighth part a warp, eight parts on their way together.
 __global__ void __launch_bounds__(256) k_head_loss(const __grid_constant__ Head a, float* loss, float* lse) {
   __shared__ float2 s_part[8][32];
-  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, row = blockIdx.x * 32 + lane, parts = a.n_tiles * 2;
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, row = blockIdx.x * 32 + lane, parts = a.n_tiles * 4;
   wait_for_last_kernel();
-  const auto join = [](float2 x, float2 y) {
-    const float most = fmaxf(x.x, y.x), from = most == __uint_as_float(0xff800000u) ? 0.0f : most;
-    return make_float2(most, x.y * exp2f((x.x - from) * kLog2e) + y.y * exp2f((y.x - from) * kLog2e));
+  float2 v = make_float2(kNone, 0.0f);
+  const auto join = [&](const float2 (&x)[8]) {
+    float most = v.x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = fmaxf(most, x[i].x);
+    const float from = most == kNone ? 0.0f : most;
+    float sum = v.y * exp2f((v.x - from) * kLog2e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += x[i].y * exp2f((x[i].x - from) * kLog2e);
+    v = make_float2(most, sum);
   };
-  float2 v = make_float2(__uint_as_float(0xff800000u), 0.0f);
   if (row < a.rows) {
-#pragma unroll 8
-    for (uint32_t p = warp; p < parts; p += 8) v = join(v, a.partial[uint64_t(p) * a.rows + row]);
+    for (uint32_t p = warp; p < parts; p += 64) {
+      float2 x[8];
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i) x[i] = p + i * 8 < parts ? a.partial[uint64_t(p + i * 8) * a.rows + row] : make_float2(kNone, 0.0f);
+      join(x);
+    }
   }
   s_part[warp][lane] = v;
   __syncthreads();
   if (warp || row >= a.rows) return;
-  for (uint32_t p = 1; p < 8; ++p) v = join(v, s_part[p][lane]);
+  v = make_float2(kNone, 0.0f);
+  float2 x[8];
+#pragma unroll
+  for (uint32_t i = 0; i < 8; ++i) x[i] = s_part[i][lane];
+  join(x);
   const float rest = logf(v.y);
   const int target = target_of(a, row, true);
   lse[row] = v.x + rest;
   loss[row] = target < 0 ? 0.0f : v.x - a.at_target[row] + rest;   // not lse less the logit: a loss next to 0 keeps its digits where the target is the largest
 }
 
-// Partial results of dW's piece added up in their order.
-__global__ void __launch_bounds__(256) k_head_words(const __grid_constant__ Head a, const float* parts, float* dw) {
+// Partial results of dW's piece added up in their order, a warp for 256 columns of a word.
+__global__ void __launch_bounds__(256) k_head_words(const __grid_constant__ Head a, const float* parts, float* dw, uint32_t spans) {
   let_next_kernel_begin();
   wait_for_last_kernel();
-  const uint64_t all = uint64_t(min(a.piece_cols, a.words - a.first_word)) * a.width, each = uint64_t(a.piece_cols) * a.width;
+  const uint32_t lane = threadIdx.x % 32, words = min(a.piece_cols, a.words - a.first_word);
+  const uint64_t each = uint64_t(a.piece_cols) * a.width, units = uint64_t(words) * spans;
   const float by2 = down_of(*a.most_g);
-  for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += uint64_t(gridDim.x) * 256) {
-    float v = 0.0f;
-    for (uint32_t s = 0; s < a.splits; ++s) v += parts[s * each + i];
-    v = v * down_of(a.most_h[i % a.width]) * by2;
-    float* p = dw + uint64_t(a.first_word) * a.width + i;
-    *p = a.add ? *p + v : v;
+  for (uint64_t u = uint64_t(blockIdx.x) * 8 + threadIdx.x / 32; u < units; u += uint64_t(gridDim.x) * 8) {
+    const uint32_t word = units >> 32 ? uint32_t(u / spans) : uint32_t(u) / spans, col0 = uint32_t(u - uint64_t(word) * spans) * kSpan;
+    float v[8] = {};
+    for (uint32_t s = 0; s < a.dw.splits; ++s)
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i) {
+        const uint32_t c = col0 + i * 32 + lane;
+        if (c < a.width) v[i] += parts[s * each + uint64_t(word) * a.width + c];
+      }
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      const uint32_t c = col0 + i * 32 + lane;
+      if (c < a.width) {
+        float* p = dw + (uint64_t(a.first_word) + word) * a.width + c;
+        const float x = v[i] * down_of(a.most_h[c]) * by2;
+        *p = a.add ? *p + x : x;
+      }
+    }
   }
 }
-// dh from its partial results.
+// dh from its partial results, likewise.
 template <class T>
-__global__ void __launch_bounds__(256) k_head_hidden(const __grid_constant__ Head a, const float* parts, T* dh, uint64_t stride) {
+__global__ void __launch_bounds__(256) k_head_hidden(const __grid_constant__ Head a, const float* parts, T* dh, uint64_t stride, uint32_t spans) {
   wait_for_last_kernel();
-  const uint64_t all = uint64_t(a.rows) * a.width;
+  const uint32_t lane = threadIdx.x % 32;
+  const uint64_t each = uint64_t(a.rows) * a.width, units = uint64_t(a.rows) * spans;
   const float by2 = down_of(*a.most_g);
-  for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += uint64_t(gridDim.x) * 256) {
-    float v = 0.0f;
-    for (uint32_t s = 0; s < a.splits; ++s) v += parts[s * all + i];
-    const uint64_t r = i / a.width, c = i - r * a.width;
-    dh[r * stride + c] = Elem<T>::put(v * down_of(a.most_w[c]) * by2);
+  for (uint64_t u = uint64_t(blockIdx.x) * 8 + threadIdx.x / 32; u < units; u += uint64_t(gridDim.x) * 8) {
+    const uint32_t row = units >> 32 ? uint32_t(u / spans) : uint32_t(u) / spans, col0 = uint32_t(u - uint64_t(row) * spans) * kSpan;
+    float v[8] = {};
+    for (uint32_t s = 0; s < a.dh.splits; ++s)
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i) {
+        const uint32_t c = col0 + i * 32 + lane;
+        if (c < a.width) v[i] += parts[s * each + uint64_t(row) * a.width + c];
+      }
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      const uint32_t c = col0 + i * 32 + lane;
+      if (c < a.width) dh[row * stride + c] = Elem<T>::put(v[i] * down_of(a.most_w[c]) * by2);
+    }
   }
 }
 
@@ -627,79 +700,130 @@ bool in_place(const dgs_matrix* m) {
   return m->type != DGS_TYPE_F32 && on_16_bytes(m) && m->stride >= m->cols && m->rows <= kMostElements / 4 / m->stride;
 }
 
-struct Products {
-  uint32_t splits;
+// How both products of a piece's s are split among 74 pairs of CTAs: runs of their steps, and tiles of dh for the pairs with more and with fewer tiles of dW.
+struct Shares {
+  uint32_t words, hidden, few, more;   // runs of steps; tiles
   double us;
 };
-// How a contraction of `steps` steps over `tiles` tiles is split among 74 pairs of CTAs: whatever ends soonest, with step_us a step, 4 us a tile, and partial results of
-// `results` values written and read again.
-Products split_steps(uint64_t tiles, uint32_t steps, double step_us, uint64_t results) {
-  Products best = {1, 1e300};
-  for (uint32_t s = 1; s <= 32 && s <= steps; ++s) {
-    const double us = double((tiles * s + kSms / 2 - 1) / (kSms / 2)) * (ceil_div(steps, s) * step_us + 4.0) + (s > 1 ? 3.0 + double(results) * 4e-6 * (s + 1) / 2.5 : 0.0);
-    if (us < best.us) best = {s, us};
+struct Work {
+  uint32_t tiles, steps;
+  double step_us;
+  uint64_t results;
+};
+constexpr double kTileUs = 3.0;   // of a tile's beginning and end
+double run_us(const Work& w, uint32_t splits) { return ceil_div(w.steps, splits) * w.step_us + kTileUs; }
+Shares share_out(const Work& words, uint32_t sw, const Work& hidden, uint32_t sh) {
+  const uint64_t pairs = std::min<uint64_t>(kSms / 2, uint64_t(words.tiles) * sw + uint64_t(hidden.tiles) * sh);
+  const uint64_t tw = uint64_t(words.tiles) * sw, th = uint64_t(hidden.tiles) * sh, some = tw % pairs, q = tw / pairs;
+  const double cw = run_us(words, sw), ch = run_us(hidden, sh);
+  Shares best = {sw, sh, 0, 0, 1e300};
+  for (uint64_t few = 0; few <= ceil_div(th, pairs); ++few) {   // for the `some` pairs with q + 1 tiles of dW
+    const uint64_t left = th - std::min(th, few * some), more = ceil_div(left, pairs - some);
+    const double us = std::max(some ? (q + 1) * cw + few * ch : 0.0, q * cw + more * ch);
+    if (us < best.us) best.us = us, best.few = uint32_t(few), best.more = uint32_t(more);
+    if (some == 0) break;
   }
-  best.splits = ceil_div(steps, ceil_div(steps, best.splits));   // none without steps
+  // partial results are written and read again
+  if (sw > 1) best.us += 3.0 + double(words.results) * 4e-6 * (sw + 1) / 2.5;
+  best.us += double(hidden.results) * 4e-6 * sh / 2.5;
+  return best;
+}
+Shares share_out(const Work& words, const Work& hidden) {
+  constexpr uint32_t kRuns[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+  Shares best = {1, 1, 0, 0, 1e300};
+  for (const uint32_t sw : kRuns) {
+    if (sw > 1 && (sw > words.steps || uint64_t(words.tiles) * (sw - 1) > kSms)) break;
+    for (const uint32_t sh : kRuns) {
+      if (sh > 1 && (sh > hidden.steps || uint64_t(hidden.tiles) * (sh - 1) > kSms)) break;
+      const Shares s = share_out(words, sw, hidden, sh);
+      if (s.us < best.us) best = s;
+    }
+  }
   return best;
 }
 
 constexpr uint64_t kPieceBytes = 256ull << 20;   // of s, where one tile of words does not take more
 
 struct HeadPlan {
-  uint32_t parts, stride, piece_tiles, pieces, word_splits, hidden_splits, row_blocks;
+  uint32_t parts, stride, piece_tiles, pieces, row_blocks;
   bool copy_h, copy_w;
-  uint64_t inner_h, inner_w, scales, most, outer_h, outer_w, s, words, hidden, partial, at_target, bytes;
+  Work words, hidden;   // of a whole piece
+  Shares shares;
+  uint64_t inner_h, inner_w, scales, most, outer_h, outer_w, s, part_w, part_h, partial, at_target, bytes;
 };
 
 bool head_ok(const dgs_matrix* h, const dgs_matrix* w) { return matrix_ok(h, false) && matrix_ok(w, false) && h->type == w->type && h->cols == w->cols && w->rows; }
 
-int plan_head(const dgs_matrix* h, const dgs_matrix* w, bool grad, HeadPlan* p) {
-  *p = {};
+// Steps of 64 values: a product 0.40 us; dh of bfloat16 takes one, of fp16 two, dW two, f32 three.
+constexpr double kProductUs = 0.40;
+Work words_of(uint64_t n, uint32_t d, uint32_t tiles, uint32_t type) {
+  return {tiles * ceil_div(d, 256), ceil_div(n, 64), kProductUs * (type == DGS_TYPE_F32 ? 3 : 2), uint64_t(tiles) * 256 * d};
+}
+Work hidden_of(uint64_t n, uint32_t d, uint32_t tiles, uint32_t type) {
+  return {ceil_div(n, 256) * ceil_div(d, 256), tiles * 4, kProductUs * (type == DGS_TYPE_F32 ? 3 : type == DGS_TYPE_FP16 ? 2 : 1), n * d};
+}
+
+int plan_head(const dgs_matrix* h, const dgs_matrix* w, bool grad, HeadPlan* out) {
   if (!head_ok(h, w)) return DGS_EINVAL;
   const uint64_t n = h->rows, v = w->rows;
   const uint32_t d = h->cols;
+  // The last plan of this thread: a call asks twice, and a training loop again and again.
+  struct Key {
+    uint64_t n, v, d, type, copies, grad;
+  };
+  thread_local Key last = {};
+  thread_local HeadPlan plan;
+  HeadPlan* const p = &plan;
+  const Key key = {n, v, d, h->type, uint64_t(!in_place(h)) | uint64_t(!in_place(w)) << 1, grad};
+  if (last.d && memcmp(&key, &last, sizeof(key)) == 0) {
+    *out = plan;
+    return DGS_OK;
+  }
+  last.d = 0;
+  *p = {};
   p->parts = h->type == DGS_TYPE_F32 ? 2 : 1;
   p->stride = uint32_t(up_to(d, 8));
   // rows are 31-bit coordinates of TMA copies and may be passed by a tile; strides of a plane are 40 bits
   if (d > (1u << 24) || n > (1u << 30) || v > (1u << 30) || std::max(n, v) * p->stride > kMostElements / 4 ||
       uint64_t(ceil_div(n, 256)) * ceil_div(v, 256) > 0x3fffffffu)
     return DGS_ELIMIT;
-  if (n == 0) return DGS_OK;
-  p->copy_h = !in_place(h);
-  p->copy_w = !in_place(w);
-  p->inner_h = p->copy_h ? up_to(p->parts * n * p->stride * 2, 256) : 0;
-  p->inner_w = p->copy_w ? up_to(p->parts * v * p->stride * 2, 256) : 0;
-  p->scales = p->parts == 2 ? up_to((n + v) * 4, 256) : 0;
-  if (!grad) {
-    p->partial = up_to(uint64_t(ceil_div(v, 256)) * 2 * n * 8, 256);
+  if (n) {
+    p->copy_h = !in_place(h);
+    p->copy_w = !in_place(w);
+    p->inner_h = p->copy_h ? up_to(p->parts * n * p->stride * 2, 256) : 0;
+    p->inner_w = p->copy_w ? up_to(p->parts * v * p->stride * 2, 256) : 0;
+    p->scales = p->parts == 2 ? up_to((n + v) * 4, 256) : 0;
+    p->bytes = p->inner_h + p->inner_w + p->scales;
+  }
+  if (n && !grad) {
+    p->partial = up_to(uint64_t(ceil_div(v, 256)) * 4 * n * 8, 256);
     p->at_target = up_to(n * 4, 256);
-    p->bytes = p->inner_h + p->inner_w + p->scales + p->partial + p->at_target;
-    return DGS_OK;
+    p->bytes += p->partial + p->at_target;
+  } else if (n) {
+    // Pieces: as many as give the shortest time for the three products of them all.
+    const uint32_t m_tiles = ceil_div(n, 256), v_tiles = ceil_div(v, 256);
+    const uint32_t most = uint32_t(std::max<uint64_t>(1, kPieceBytes / (uint64_t(m_tiles) * 256 * 256 * 4))), least = ceil_div(v_tiles, most);
+    double best = 1e300;
+    for (uint32_t pieces = least; pieces < least + 12 && pieces <= v_tiles; ++pieces) {
+      const uint32_t t = ceil_div(v_tiles, pieces), count = ceil_div(v_tiles, t);
+      if (t == p->piece_tiles) continue;
+      const Work words = words_of(n, d, t, h->type), hidden = hidden_of(n, d, t, h->type);
+      const Shares shares = share_out(words, hidden);
+      const double us = count * (ceil_div(uint64_t(m_tiles) * t, kSms / 2) * (ceil_div(d, 64) * kProductUs * (p->parts == 2 ? 3 : 1) + 1.0) + shares.us + 4.0);
+      if (us < best) best = us, p->pieces = count, p->piece_tiles = t, p->words = words, p->hidden = hidden, p->shares = shares;
+    }
+    if (uint64_t(p->words.tiles) * p->shares.words > 0x3fffffffu || uint64_t(p->hidden.tiles) * p->shares.hidden > 0x3fffffffu) return DGS_ELIMIT;
+    p->row_blocks = m_tiles * 2;
+    p->most = up_to((2 * uint64_t(d) + 1) * 4, 256);
+    p->outer_h = up_to(p->parts * n * p->stride * 2, 256);
+    p->outer_w = up_to(p->parts * v * p->stride * 2, 256);
+    p->s = 2ull * p->row_blocks * p->piece_tiles * 4 * kBlockBytes;
+    p->part_w = p->shares.words > 1 ? up_to(p->shares.words * p->words.results * 4, 256) : 0;
+    p->part_h = up_to(p->shares.hidden * p->hidden.results * 4, 256);
+    p->bytes += p->most + p->outer_h + p->outer_w + p->s + p->part_w + p->part_h;
   }
-  // Pieces: as many as give the shortest time for the three products of them all.
-  const uint32_t m_tiles = ceil_div(n, 256), d_tiles = ceil_div(d, 256), v_tiles = ceil_div(v, 256), products = p->parts == 2 ? 3 : 1;
-  const uint32_t most = uint32_t(std::max<uint64_t>(1, kPieceBytes / (uint64_t(m_tiles) * 256 * 256 * 4))), least = ceil_div(v_tiles, most);
-  const double half_us = 0.40;   // 64 rows of a product
-  double best = 1e300;
-  for (uint32_t pieces = least; pieces < least + 12 && pieces <= v_tiles; ++pieces) {
-    const uint32_t t = ceil_div(v_tiles, pieces), count = ceil_div(v_tiles, t);
-    const Products words = split_steps(uint64_t(t) * d_tiles, ceil_div(n, 64), half_us * (products + 1) * (p->parts == 2 ? 0.75 : 1), uint64_t(t) * 256 * d);
-    const Products hidden = split_steps(uint64_t(m_tiles) * d_tiles, t * 4, half_us * products, n * d);
-    const double us = count * (ceil_div(uint64_t(m_tiles) * t, kSms / 2) * (ceil_div(d, 64) * half_us * products + 1.0) + words.us + hidden.us + 6.0);
-    if (us < best) best = us, p->pieces = count, p->piece_tiles = t;
-  }
-  const Products words = split_steps(uint64_t(p->piece_tiles) * d_tiles, ceil_div(n, 64), half_us * (products + 1) * (p->parts == 2 ? 0.75 : 1), uint64_t(p->piece_tiles) * 256 * d);
-  const Products hidden = split_steps(uint64_t(m_tiles) * d_tiles, p->piece_tiles * 4, half_us * products, n * d);
-  p->word_splits = words.splits;
-  p->hidden_splits = hidden.splits;
-  p->row_blocks = m_tiles * 2;
-  p->most = up_to((2 * uint64_t(d) + 1) * 4, 256);
-  p->outer_h = up_to(p->parts * n * p->stride * 2, 256);
-  p->outer_w = up_to(p->parts * v * p->stride * 2, 256);
-  p->s = 2ull * p->row_blocks * p->piece_tiles * 4 * kBlockBytes;
-  p->words = p->word_splits > 1 ? up_to(uint64_t(p->word_splits) * p->piece_tiles * 256 * d * 4, 256) : 0;
-  p->hidden = up_to(uint64_t(p->hidden_splits) * n * d * 4, 256);
-  p->bytes = p->inner_h + p->inner_w + p->scales + p->most + p->outer_h + p->outer_w + p->s + p->words + p->hidden;
+  last = key;
+  *out = plan;
   return DGS_OK;
 }
 
@@ -707,20 +831,20 @@ constexpr int kMaxDevices = 64;
 std::mutex g_head_mu;
 bool g_head_ready[kMaxDevices];
 PFN_cuTensorMapEncodeTiled_v12000 g_head_encode;   // written once, under the mutex
-template <int MODE, uint32_t PA, uint32_t PB>
+template <int MODE, uint32_t PA, uint32_t PB, uint32_t PH>
 bool head_setup() {
   cudaFuncAttributes f;
   // the split of the registers counts on what the launch brings
-  return cudaFuncGetAttributes(&f, k_head<MODE, PA, PB>) == cudaSuccess && uint32_t(f.numRegs) >= kHeadRegs &&
-         cudaFuncSetAttribute(k_head<MODE, PA, PB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) == cudaSuccess;
+  return cudaFuncGetAttributes(&f, k_head<MODE, PA, PB, PH>) == cudaSuccess && uint32_t(f.numRegs) >= kHeadRegs &&
+         cudaFuncSetAttribute(k_head<MODE, PA, PB, PH>, cudaFuncAttributeMaxDynamicSharedMemorySize, Step<MODE, PA, PB>::kSmem) == cudaSuccess;
 }
 int head_ready() {   // once per device
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return DGS_ECUDA;
   std::lock_guard<std::mutex> lock(g_head_mu);
   if (!g_head_ready[dev]) {
-    if (!head_setup<kLoss, 1, 1>() || !head_setup<kLoss, 2, 2>() || !head_setup<kSlope, 1, 1>() || !head_setup<kSlope, 2, 2>() || !head_setup<kWords, 1, 2>() ||
-        !head_setup<kWords, 2, 2>() || !head_setup<kHidden, 1, 1>() || !head_setup<kHidden, 1, 2>() || !head_setup<kHidden, 2, 2>())
+    if (!head_setup<kLoss, 1, 1, 0>() || !head_setup<kLoss, 2, 2, 0>() || !head_setup<kSlope, 1, 1, 0>() || !head_setup<kSlope, 2, 2, 0>() ||
+        !head_setup<kGrads, 1, 2, 1>() || !head_setup<kGrads, 1, 2, 2>() || !head_setup<kGrads, 2, 2, 2>())
       return DGS_ECUDA;
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult found;
@@ -740,11 +864,11 @@ int head_map(const void* data, uint64_t rows, uint64_t cols, uint64_t stride, ui
              : DGS_ECUDA;
 }
 
-template <int MODE, uint32_t PA, uint32_t PB>
-int head_launch(const Head& a, const CUtensorMap& x, const CUtensorMap& y, bool early, cudaStream_t st) {
-  EarlyLaunch l(dim3(std::min(a.tiles, kSms / 2) * 2), kHeadThreads, kSmem, st);
+template <int MODE, uint32_t PA, uint32_t PB, uint32_t PH>
+int head_launch(const Head& a, uint32_t tiles, const CUtensorMap& x, const CUtensorMap& y, bool early, cudaStream_t st) {
+  EarlyLaunch l(dim3(std::min(tiles, kSms / 2) * 2), kHeadThreads, Step<MODE, PA, PB>::kSmem, st);
   if (!early) l.cfg.numAttrs = 0;
-  return cudaLaunchKernelEx(&l.cfg, k_head<MODE, PA, PB>, a, x, y) == cudaSuccess ? DGS_OK : DGS_ECUDA;
+  return cudaLaunchKernelEx(&l.cfg, k_head<MODE, PA, PB, PH>, a, x, y) == cudaSuccess ? DGS_OK : DGS_ECUDA;
 }
 
 Source source_of(const dgs_matrix* m) { return {m->data, m->stride, uint32_t(m->rows), m->cols, (m->cols + kSpan - 1) / kSpan}; }
@@ -782,13 +906,19 @@ Head head_of(const dgs_matrix* h, const dgs_matrix* w, const void* target, uint3
   a.width = h->cols;
   a.words = uint32_t(w->rows);
   a.m_tiles = ceil_div(h->rows, 256);
-  a.n = 256;
-  a.splits = 1;
   a.idesc = kIdescF32 | (h->type == DGS_TYPE_BF16 ? kIdescBf16 : 0);
   a.target = target;
   a.wide_targets = flags & DGS_TARGET_I64 ? 1 : 0;
   a.status = operator_status_word();
   return a;
+}
+
+void logit_steps(uint32_t parts, Head* a) {
+  using One = Step<kLoss, 1, 1>;
+  using Two = Step<kLoss, 2, 2>;
+  static_assert(One::kRows == Step<kSlope, 1, 1>::kRows && Two::kRows == Step<kSlope, 2, 2>::kRows, "");
+  a->steps = ceil_div(a->width, parts == 2 ? Two::kRows : One::kRows);
+  a->chunk = std::min(ceil_div(a->steps, 2), parts == 2 ? Two::kChunk : One::kChunk);
 }
 
 }  // namespace
@@ -830,8 +960,8 @@ extern "C" int dgs_vocabulary_loss(const dgs_matrix* hidden, const dgs_matrix* w
   a.tiles = a.m_tiles * a.n_tiles;
   a.partial = reinterpret_cast<float2*>(work + p.inner_h + p.inner_w + p.scales);
   a.at_target = reinterpret_cast<float*>(work + p.inner_h + p.inner_w + p.scales + p.partial);
-  a.steps = ceil_div(a.width, p.parts == 2 ? Step<2, 2>::kRows : Step<1, 1>::kRows);
-  rc = p.parts == 2 ? head_launch<kLoss, 2, 2>(a, map_h, map_w, launched, st) : head_launch<kLoss, 1, 1>(a, map_h, map_w, launched, st);
+  logit_steps(p.parts, &a);
+  rc = p.parts == 2 ? head_launch<kLoss, 2, 2, 0>(a, a.tiles, map_h, map_w, launched, st) : head_launch<kLoss, 1, 1, 0>(a, a.tiles, map_h, map_w, launched, st);
   if (rc != DGS_OK) return rc;
   const EarlyLaunch l(dim3(ceil_div(n, 32)), 256, 0, st);
   return cudaLaunchKernelEx(&l.cfg, k_head_loss, a, loss, lse) == cudaSuccess ? DGS_OK : DGS_ECUDA;
@@ -877,7 +1007,7 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
   a.s = reinterpret_cast<unsigned char*>(at);
   at += p.s;
   float* const part_w = reinterpret_cast<float*>(at);
-  at += p.words;
+  at += p.part_w;
   float* const part_h = reinterpret_cast<float*>(at);
   const uint32_t d = a.width;
   a.most_h = most;
@@ -894,7 +1024,7 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
   if (cudaMemsetAsync(most, 0, p.most, st) != cudaSuccess) return DGS_ECUDA;
   const Source h = source_of(hidden), w = source_of(weight);
   const uint32_t most_h = h.spans * ceil_div(h.rows, kMostRows), most_w = w.spans * ceil_div(w.rows, kMostRows), most_g = std::min(ceil_div(n, 256), kSms);
-  const uint32_t blocks_h = ceil_div(uint64_t(h.rows) * h.spans, 8), blocks_w = ceil_div(uint64_t(w.rows) * w.spans, 8);
+  const uint32_t blocks_h = h.spans * ceil_div(h.rows, kPlaneRows), blocks_w = w.spans * ceil_div(w.rows, kPlaneRows);
   rc = with_wide(hidden->type, on_16_bytes(hidden) && on_16_bytes(weight), [&](auto* t, auto vec) {
     using T = std::remove_pointer_t<decltype(t)>;
     k_head_most<T, vec.value><<<most_h + most_w + most_g, 256, 0, st>>>(a, h, w, most_h, most_w, most, most + d, most + 2 * uint64_t(d));
@@ -908,8 +1038,13 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
   if ((rc = inner_operands(hidden, weight, p, inner, &a, &inner_h, &inner_w, &launched, st)) != DGS_OK) return rc;
   const bool bf16 = hidden->type == DGS_TYPE_BF16;
   if ((rc = head_map(outer_h, n, d, p.stride, p.parts, false, 64, &map_h)) != DGS_OK) return rc;
-  if ((rc = head_map(outer_w, v, d, p.stride, p.parts, false, bf16 ? 128 : 64, &map_w)) != DGS_OK) return rc;
+  if ((rc = head_map(outer_w, v, d, p.stride, p.parts, false, 64, &map_w)) != DGS_OK) return rc;
 
+  a.dh.out = part_h;
+  a.dh.splits = p.shares.hidden;
+  a.dw.out = p.shares.words > 1 ? part_w : dw;
+  a.dw.splits = p.shares.words;
+  logit_steps(p.parts, &a);
   for (uint32_t piece = 0; piece < p.pieces; ++piece) {
     const uint32_t tile0 = piece * p.piece_tiles, tiles = std::min(p.piece_tiles, ceil_div(v, 256) - tile0);
     Head s = a;
@@ -917,39 +1052,34 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
     s.first_piece = piece == 0;
     s.n_tiles = tiles;
     s.tiles = s.m_tiles * tiles;
-    s.steps = ceil_div(d, p.parts == 2 ? 64 : 128);
-    rc = p.parts == 2 ? head_launch<kSlope, 2, 2>(s, inner_h, inner_w, true, st) : head_launch<kSlope, 1, 1>(s, inner_h, inner_w, true, st);
+    rc = p.parts == 2 ? head_launch<kSlope, 2, 2, 0>(s, s.tiles, inner_h, inner_w, true, st) : head_launch<kSlope, 1, 1, 0>(s, s.tiles, inner_h, inner_w, true, st);
     if (rc != DGS_OK) return rc;
     s.idesc = kIdescF32;
-    if (dw) {
-      Head b = s;
-      b.m_tiles = ceil_div(d, 256);
-      b.splits = p.word_splits;
-      b.tiles = b.m_tiles * b.n_tiles * b.splits;
-      b.steps = ceil_div(n, 64);
-      b.out = b.splits > 1 ? part_w : dw;
-      rc = p.parts == 2 ? head_launch<kWords, 2, 2>(b, map_h, map_h, true, st) : head_launch<kWords, 1, 2>(b, map_h, map_h, true, st);
-      if (rc != DGS_OK) return rc;
-      if (b.splits > 1) {
-        const EarlyLaunch l(dim3(uint32_t(std::min<uint64_t>((uint64_t(tiles) * 256 * d + 1023) / 1024, kSms * 8))), 256, 0, st);
-        if (cudaLaunchKernelEx(&l.cfg, k_head_words, b, static_cast<const float*>(part_w), dw) != cudaSuccess) return DGS_ECUDA;
-      }
-    }
-    Head b = s;
-    b.m_tiles = ceil_div(d, 256);
-    b.n_tiles = ceil_div(n, 256);
-    b.splits = p.hidden_splits;
-    b.tiles = b.m_tiles * b.n_tiles * b.splits;
-    b.steps = ceil_div(std::min<uint64_t>(tiles * 256, v - s.first_word), bf16 ? 128 : 64);
-    b.out = part_h;
-    rc = bf16 ? head_launch<kHidden, 1, 1>(b, map_w, map_w, true, st)
-              : p.parts == 2 ? head_launch<kHidden, 2, 2>(b, map_w, map_w, true, st) : head_launch<kHidden, 1, 2>(b, map_w, map_w, true, st);
+    s.dw.m_tiles = s.dh.m_tiles = ceil_div(d, 256);
+    s.dw.n_tiles = tiles;
+    s.dw.steps = ceil_div(n, 64);
+    s.dw.tiles = dw ? s.dw.m_tiles * s.dw.n_tiles * s.dw.splits : 0;
+    s.dh.n_tiles = a.m_tiles;
+    s.dh.steps = ceil_div(std::min<uint64_t>(tiles * 256, v - s.first_word), 64);
+    s.dh.tiles = s.dh.m_tiles * s.dh.n_tiles * s.dh.splits;
+    // the last piece may be shorter, and dW not wanted
+    Work words = words_of(n, d, tiles, hidden->type), of_h = hidden_of(n, d, tiles, hidden->type);
+    if (!dw) words.tiles = 0;
+    const Shares shares = dw && tiles == p.piece_tiles ? p.shares : share_out(words, s.dw.splits, of_h, s.dh.splits);
+    s.share_few = shares.few;
+    s.share_more = shares.more;
+    const uint32_t all = s.dw.tiles + s.dh.tiles;
+    rc = bf16 ? head_launch<kGrads, 1, 2, 1>(s, all, map_h, map_w, true, st)
+              : p.parts == 2 ? head_launch<kGrads, 2, 2, 2>(s, all, map_h, map_w, true, st) : head_launch<kGrads, 1, 2, 2>(s, all, map_h, map_w, true, st);
     if (rc != DGS_OK) return rc;
+    if (dw && s.dw.splits > 1) {
+      const EarlyLaunch l(dim3(uint32_t(std::min<uint64_t>((uint64_t(tiles) * 256 * w.spans + 7) / 8, kSms * 16))), 256, 0, st);
+      if (cudaLaunchKernelEx(&l.cfg, k_head_words, s, static_cast<const float*>(part_w), dw, w.spans) != cudaSuccess) return DGS_ECUDA;
+    }
   }
-  a.splits = p.hidden_splits;
   return with_type(hidden->type, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
-    const EarlyLaunch l(dim3(uint32_t(std::min<uint64_t>((n * d + 255) / 256, kSms * 16))), 256, 0, st);
-    return cudaLaunchKernelEx(&l.cfg, k_head_hidden<T>, a, static_cast<const float*>(part_h), static_cast<T*>(dhidden->data), dhidden->stride) == cudaSuccess ? int(DGS_OK) : int(DGS_ECUDA);
+    const EarlyLaunch l(dim3(uint32_t(std::min<uint64_t>((n * h.spans + 7) / 8, kSms * 16))), 256, 0, st);
+    return cudaLaunchKernelEx(&l.cfg, k_head_hidden<T>, a, static_cast<const float*>(part_h), static_cast<T*>(dhidden->data), dhidden->stride, h.spans) == cudaSuccess ? int(DGS_OK) : int(DGS_ECUDA);
   });
 }
