@@ -267,14 +267,14 @@ __device__ __forceinline__ void of_floats(const float2 (&v)[4], Eight<__half>& e
 // A warp takes 256 columns of a row, eight a lane, so that a row in 16 bits is read 512 bytes at a time wherever it lies.  Rows that
 // begin on 16 bytes: eight neighbours a lane; others: every 32nd column, so that a warp's elements are neighbours still.
 constexpr uint32_t kSpan = 256;
-template <class T, bool VEC>
+template <class T, bool VEC, bool KEEP = false>   // KEEP: others will read it too
 __device__ __forceinline__ void load8(const T* row, uint32_t col0, uint32_t lane, uint32_t cols, Eight<T>& e) {
   if constexpr (VEC) {
     const uint32_t c = col0 + lane * 8;
     if (c + 8 <= cols) {
 #pragma unroll
       for (uint32_t i = 0; i < sizeof(T) / 2; ++i) {
-        const uint4 w = __ldcs(reinterpret_cast<const uint4*>(row + c) + i);
+        const uint4 w = KEEP ? __ldg(reinterpret_cast<const uint4*>(row + c) + i) : __ldcs(reinterpret_cast<const uint4*>(row + c) + i);
         e.w[4 * i] = w.x, e.w[4 * i + 1] = w.y, e.w[4 * i + 2] = w.z, e.w[4 * i + 3] = w.w;
       }
       return;

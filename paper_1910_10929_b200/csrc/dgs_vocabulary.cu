@@ -602,6 +602,13 @@ __global__ void __launch_bounds__(256) k_head_rows(const __grid_constant__ Sourc
 }
 
 // ---- behind the products --------------------------------------------------------------------------
+// A row's loss from its maximum and sum.  Not lse less the logit: a loss next to 0 keeps its digits where the target is the largest.
+__device__ __forceinline__ void finish_row(const Head& a, uint32_t row, float2 v, float* loss, float* lse) {
+  const float rest = logf(v.y);
+  const int target = target_of(a, row, true);
+  lse[row] = v.x + rest;
+  loss[row] = target < 0 ? 0.0f : v.x - a.at_target[row] + rest;
+}
 // A row's parts joined in their order: 32 rows a CTA, each eighth part a warp, eight parts on their way together.
 __global__ void __launch_bounds__(256) k_head_loss(const __grid_constant__ Head a, float* loss, float* lse) {
   __shared__ float2 s_part[8][32];
@@ -634,10 +641,7 @@ __global__ void __launch_bounds__(256) k_head_loss(const __grid_constant__ Head 
 #pragma unroll
   for (uint32_t i = 0; i < 8; ++i) x[i] = s_part[i][lane];
   join(x);
-  const float rest = logf(v.y);
-  const int target = target_of(a, row, true);
-  lse[row] = v.x + rest;
-  loss[row] = target < 0 ? 0.0f : v.x - a.at_target[row] + rest;   // not lse less the logit: a loss next to 0 keeps its digits where the target is the largest
+  finish_row(a, row, v, loss, lse);
 }
 
 // Partial results of dW's piece added up in their order, a warp for 256 columns of a word.
@@ -690,6 +694,14 @@ __global__ void __launch_bounds__(256) k_head_hidden(const __grid_constant__ Hea
     }
   }
 }
+
+}  // namespace
+}  // namespace dgs
+
+#include "dgs_vocabulary_few.cuh"
+
+namespace dgs {
+namespace {
 
 // ---- host side --------------------------------------------------------------------------------
 uint32_t ceil_div(uint64_t a, uint64_t b) { return uint32_t((a + b - 1) / b); }
@@ -747,6 +759,7 @@ constexpr uint64_t kPieceBytes = 256ull << 20;   // of s, where one tile of word
 struct HeadPlan {
   uint32_t parts, stride, piece_tiles, pieces, row_blocks;
   bool copy_h, copy_w;
+  uint32_t few, few_ctas, few_words, few_tiles;   // few: rows at a time without tensor cores, 0: with them; words of a tile
   Work words, hidden;   // of a whole piece
   Shares shares;
   uint64_t inner_h, inner_w, scales, most, outer_h, outer_w, s, part_w, part_h, partial, at_target, bytes;
@@ -761,6 +774,15 @@ Work words_of(uint64_t n, uint32_t d, uint32_t tiles, uint32_t type) {
 }
 Work hidden_of(uint64_t n, uint32_t d, uint32_t tiles, uint32_t type) {
   return {ceil_div(n, 256) * ceil_div(d, 256), tiles * 4, kProductUs * (type == DGS_TYPE_F32 ? 3 : type == DGS_TYPE_FP16 ? 2 : 1), n * d};
+}
+
+// Few rows go without tensor cores where there are not many products in all.  Here / with tensor cores, us a call.  Loss, 16 bits: 64 x 512 x 1000 10.5 / 12.5,
+// 3 x 2048 x 8000 15 / 21, 8 of them 25 / 21, 1 x 768 x 50257 20 / 33, 3 of them 32 / 33, 8 47 / 33; f32: 16 x 2048 x 8000 49 / 64, 37 101 / 64, 16 x 768 x 50257
+// 81 / 102, 37 178 / 102.  Gradient, 16 bits: 37 x 512 x 1000 27 / 35, 64 37 / 37, 1 x 768 x 50257 125 / 167, 3 of them 193 / 166, 3 x 2048 x 8000 97 / 86; f32:
+// 64 x 512 x 1000 36 / 52, 8 x 2048 x 8000 91 / 155, 16 161 / 156, 8 x 768 x 50257 181 / 285, 16 300 / 286.
+bool few_rows(uint64_t n, uint64_t v, uint32_t d, uint32_t type, bool grad) {
+  const uint64_t rows = n == 1 ? 1 : n <= 4 ? 4 : up_to(n, 8), most = type == DGS_TYPE_F32 ? (grad ? 260000000 : 640000000) : grad ? 40000000 : 100000000;
+  return n <= kFewRows && v * d <= most / rows;
 }
 
 int plan_head(const dgs_matrix* h, const dgs_matrix* w, bool grad, HeadPlan* out) {
@@ -787,6 +809,27 @@ int plan_head(const dgs_matrix* h, const dgs_matrix* w, bool grad, HeadPlan* out
   if (d > (1u << 24) || n > (1u << 30) || v > (1u << 30) || std::max(n, v) * p->stride > kMostElements / 4 ||
       uint64_t(ceil_div(n, 256)) * ceil_div(v, 256) > 0x3fffffffu)
     return DGS_ELIMIT;
+  if (n && few_rows(n, v, d, h->type, grad)) {
+    p->few = n == 1 ? 1 : n <= 4 ? 4 : 8;
+    if (grad) {
+      // Small tiles where the words are few, and for one row of 16 bits, which is bound by trips to memory (1 x 768 x 50257: 125 us, 182 with large ones; in
+      // f32 123 and 101, eight rows 293 and 259).
+      const bool one = n == 1 && h->type != DGS_TYPE_F32;
+      p->few_words = v <= 8 * 2 * kSms || one ? 8 : 32;
+      p->few_tiles = ceil_div(v, p->few_words);
+      p->few_ctas = std::min(p->few_tiles, kSms * (one ? 6 : 2));
+      p->part_h = up_to(uint64_t(p->few_ctas) * n * d * 4, 256);
+      p->bytes = p->part_h;
+    } else {
+      p->few_ctas = std::min(ceil_div(v, 8 * kFewWords), kSms * 3);
+      p->partial = up_to(uint64_t(p->few_ctas) * n * 8, 256);
+      p->at_target = up_to(n * 4, 256);
+      p->bytes = p->partial + p->at_target;
+    }
+    last = key;
+    *out = plan;
+    return DGS_OK;
+  }
   if (n) {
     p->copy_h = !in_place(h);
     p->copy_w = !in_place(w);
@@ -864,6 +907,14 @@ int head_map(const void* data, uint64_t rows, uint64_t cols, uint64_t stride, ui
              : DGS_ECUDA;
 }
 
+// Calls f with a null pointer of the element type, whether rows begin on 16 bytes, and how many rows go together.
+template <class F>
+int with_few(const dgs_matrix* h, const dgs_matrix* w, uint32_t few, F&& f) {
+  return with_wide(h->type, on_16_bytes(h) && on_16_bytes(w), [&](auto* t, auto vec) {
+    return few == 1 ? f(t, vec, std::integral_constant<uint32_t, 1>{}) : few == 4 ? f(t, vec, std::integral_constant<uint32_t, 4>{}) : f(t, vec, std::integral_constant<uint32_t, 8>{});
+  });
+}
+
 template <int MODE, uint32_t PA, uint32_t PB, uint32_t PH>
 int head_launch(const Head& a, uint32_t tiles, const CUtensorMap& x, const CUtensorMap& y, bool early, cudaStream_t st) {
   EarlyLaunch l(dim3(std::min(tiles, kSms / 2) * 2), kHeadThreads, Step<MODE, PA, PB>::kSmem, st);
@@ -913,6 +964,8 @@ Head head_of(const dgs_matrix* h, const dgs_matrix* w, const void* target, uint3
   return a;
 }
 
+Few few_of(const dgs_matrix* h, const dgs_matrix* w, const HeadPlan& p) { return {h->data, w->data, h->stride, w->stride, (h->cols + kSpan - 1) / kSpan, p.few_tiles}; }
+
 void logit_steps(uint32_t parts, Head* a) {
   using One = Step<kLoss, 1, 1>;
   using Two = Step<kLoss, 2, 2>;
@@ -948,11 +1001,24 @@ extern "C" int dgs_vocabulary_loss(const dgs_matrix* hidden, const dgs_matrix* w
                        {loss, n * 4, true}, {lse, n * 4, true}, {workspace, p.bytes, true}};
   if (!apart(part)) return DGS_EINVAL;
   if (n == 0) return DGS_OK;
-  if ((rc = head_ready()) != DGS_OK) return rc;
   Head a = head_of(hidden, weight, target, flags);
   if (!a.status) return DGS_ECUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   char* const work = static_cast<char*>(workspace);
+  if (p.few) {
+    a.partial = reinterpret_cast<float2*>(work);
+    a.at_target = reinterpret_cast<float*>(work + p.partial);
+    const Few f = few_of(hidden, weight, p);
+    rc = with_few(hidden, weight, p.few, [&](auto* t, auto vec, auto together) {
+      using T = std::remove_pointer_t<decltype(t)>;
+      k_few_loss<T, vec.value, together.value><<<dim3(p.few_ctas, ceil_div(n, p.few)), 256, 0, st>>>(a, f);
+      return cudaGetLastError() == cudaSuccess ? int(DGS_OK) : int(DGS_ECUDA);
+    });
+    if (rc != DGS_OK) return rc;
+    const EarlyLaunch l(dim3(uint32_t(n)), 256, 0, st);
+    return cudaLaunchKernelEx(&l.cfg, k_few_rows, a, p.few_ctas, loss, lse) == cudaSuccess ? DGS_OK : DGS_ECUDA;
+  }
+  if ((rc = head_ready()) != DGS_OK) return rc;
   CUtensorMap map_h = {}, map_w = {};
   bool launched = false;
   if ((rc = inner_operands(hidden, weight, p, work, &a, &map_h, &map_w, &launched, st)) != DGS_OK) return rc;
@@ -992,9 +1058,29 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
   if (!apart(part)) return DGS_EINVAL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (n == 0) return !dw || (flags & DGS_LOSS_ADD) || cudaMemsetAsync(dw, 0, dw_bytes, st) == cudaSuccess ? DGS_OK : DGS_ECUDA;
-  if ((rc = head_ready()) != DGS_OK) return rc;
   Head a = head_of(hidden, weight, target, flags);
   if (!a.status) return DGS_ECUDA;
+  if (p.few) {
+    a.lse = lse;
+    a.dloss = dloss;
+    a.dloss_step = dloss_stride;
+    a.add = flags & DGS_LOSS_ADD ? 1 : 0;
+    const Few f = few_of(hidden, weight, p);
+    float* const parts = static_cast<float*>(workspace);
+    return with_few(hidden, weight, p.few, [&](auto* t, auto vec, auto together) {
+      using T = std::remove_pointer_t<decltype(t)>;
+      if (p.few_words == 8)
+        k_few_grad<T, vec.value, together.value, 8><<<p.few_ctas, 256, 0, st>>>(a, f, dw, parts);
+      else
+        k_few_grad<T, vec.value, together.value, 32><<<p.few_ctas, 256, 0, st>>>(a, f, dw, parts);
+      if (cudaGetLastError() != cudaSuccess) return int(DGS_ECUDA);
+      const EarlyLaunch l(dim3(ceil_div(a.width, 32), a.rows), 256, 0, st);
+      return cudaLaunchKernelEx(&l.cfg, k_few_hidden<T>, a, static_cast<const float*>(parts), p.few_ctas, static_cast<T*>(dhidden->data), dhidden->stride) == cudaSuccess
+                 ? int(DGS_OK)
+                 : int(DGS_ECUDA);
+    });
+  }
+  if ((rc = head_ready()) != DGS_OK) return rc;
   char* at = static_cast<char*>(workspace);
   char* const inner = at;
   at += p.inner_h + p.inner_w + p.scales;
