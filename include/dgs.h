@@ -492,7 +492,7 @@ int dgs_vocabulary_loss(const dgs_matrix* hidden, const dgs_matrix* weight, cons
  * width, of the hidden states' type.  dw: DEVICE f32, words * width elements (4-byte aligned: the layer's slice of the flat gradient), or NULL: not wanted.
  * s is formed a piece of the vocabulary at a time and kept in 22 bits under one power of two for the call (for dhidden in bfloat16 in 11); hidden and weight meet it
  * as 11 bits (f32: 22) under a power of two for each column, which holds bfloat16 values exactly down to 2^-29 of their column's largest.
- * workspace: likewise, dgs_vocabulary_loss_grad_bytes: up to 256 MB (or 1 KB a row, if more) of s, 2 bytes a value of both matrices (f32 4), 4 bytes a value of
+ * workspace: likewise, dgs_vocabulary_loss_grad_bytes: up to 320 MB (or 1 KB a row, if more) of s, 2 bytes a value of both matrices (f32 4), 4 bytes a value of
  * dhidden, partial results where contractions are split, and the copies that the loss needs. */
 int dgs_vocabulary_loss_grad_bytes(const dgs_matrix* hidden, const dgs_matrix* weight, uint64_t* out_bytes);
 int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matrix* weight, const void* target, const float* lse, const float* dloss, uint32_t dloss_stride,

@@ -29,11 +29,6 @@ __device__ __forceinline__ void bulk_load(uint32_t to, const void* from, uint32_
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar)
                : "memory");
 }
-// 32 bytes that are nobody else's: a whole sector.
-__device__ __forceinline__ void store_sector(void* to, const uint32_t (&v)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-               : "memory");
-}
 // *to += v, without waiting for what is there.  The only thread that adds to it in this kernel, so the sum's order is that of the kernels.
 __device__ __forceinline__ void add_behind(float* to, float v) { asm volatile("red.global.add.f32 [%0], %1;" ::"l"(to), "f"(v) : "memory"); }
 
@@ -50,9 +45,12 @@ enum : int { kLoss, kSlope, kGrads };
 // logit's error as it is (a logit of 15 summed over 768 values in one go is off by 7e-6), and two chunks a tile let the products of the next tile run to their
 // end while one is finished.
 constexpr uint32_t kBlockBytes = 128 * 128;                       // 128 rows and 64 columns of s
+// Shared memory is a ring of tiles, one for each part of an operand and step: a step of dW takes three of the twelve, one of dh in bfloat16 two, so that
+// four or six steps are on their way.  (Four of either: the products of dh waited for copies, 0.46 us a step for 0.33.)
 template <int MODE, uint32_t PA, uint32_t PB> struct Step {
-  static constexpr uint32_t kRows = MODE != kGrads && PA == 1 ? 128 : 64, kTile = kRows * 256, kStage = (PA + PB) * kTile;
-  static constexpr uint32_t kStages = 192 * 1024 / kStage, kChunk = 512 / kRows / PA, kSmem = 1024 + kStages * kStage;
+  static constexpr uint32_t kRows = MODE == kLoss && PA == 1 ? 128 : 64, kTile = kRows * 256, kSlots = (MODE == kSlope ? 160 : 192) * 1024 / kTile;
+  static constexpr uint32_t kAhead = kSlots / 2;   // steps under way, at most
+  static constexpr uint32_t kChunk = 512 / kRows / PA, kSmem = 1024 + kSlots * kTile + (MODE == kSlope ? 64 * 1024 : 0);
 };
 // Sixteen warps keep the sums, 64 columns of 32 rows each; four do the rest and leave them their registers.  (With eight warps of 128 columns, two a scheduler, the
 // trips to tensor memory and through the exponentials showed: 5632 words of 8192 x 768 took 105 us.)
@@ -60,14 +58,13 @@ constexpr uint32_t kSumWarps = 16, kHeadThreads = kSumWarps * 32 + 128, kHeadReg
 static_assert(kHeadRegsSum * kSumWarps * 32 + kHeadRegsRest * 128 <= kHeadRegs * kHeadThreads, "setmaxnreg draws on the launch's registers");
 constexpr uint32_t kHeadTmem = 512;                               // two accumulators of 256 columns
 
-// k: which sixteen of the values contracted.
-__device__ __forceinline__ uint64_t desc_inner(uint32_t tile, uint32_t k) {
-  return uint64_t(((tile + (k / 4) * kBlockBytes + (k % 4) * 32) >> 4) & 0x3fff) | uint64_t(1) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+// A tile's descriptor, and what the k-th sixteen of the values contracted add to it.
+template <bool OUTER, uint32_t R>
+__device__ __forceinline__ uint64_t tile_desc(uint32_t tile) {
+  return uint64_t(tile >> 4) | uint64_t(OUTER ? R * 128 >> 4 : 1) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
 }
-template <uint32_t R>
-__device__ __forceinline__ uint64_t desc_outer(uint32_t tile, uint32_t k) {
-  return uint64_t(((tile + k * 2048) >> 4) & 0x3fff) | uint64_t(R * 128 >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
-}
+template <bool OUTER>
+__device__ __forceinline__ uint32_t desc_step(uint32_t k) { return (OUTER ? k * 2048 : (k / 4) * kBlockBytes + (k % 4) * 32) >> 4; }
 __device__ __forceinline__ void tmem_load16(uint32_t at, float (&v)[16]) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
   asm volatile(
@@ -107,6 +104,7 @@ struct Head {
   float2* partial;                  // [n_tiles * 4][rows]: maximum, sum
   float* at_target;                 // [rows]
   unsigned char* s;                 // [2][row_blocks][piece_cols / 64] blocks
+  uint64_t plane;                   // bytes of one part of s
   Product dw, dh;                   // out: dw or partial results [splits][piece_cols][width]; [splits][rows][width]
   uint32_t share_few, share_more;   // tiles of dh for a pair of CTAs with one more tile of dw, and for others
   uint32_t add, first_piece;
@@ -123,6 +121,12 @@ __device__ __forceinline__ int target_of(const Head& a, uint32_t row, bool tell)
   return t < 0 ? -1 : int(t);
 }
 
+// One lane of the warp, the same one each time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+  return p;
+}
 struct HeadTile {
   uint32_t m0, n0, split, from, steps;
   bool hidden;
@@ -170,11 +174,11 @@ template <int MODE, uint32_t PA, uint32_t PB, uint32_t PH>   // PH: parts of s t
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
 k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
   using S = Step<MODE, PA, PB>;
-  constexpr uint32_t R = S::kRows, ST = S::kStages, TILE = S::kTile;
+  constexpr uint32_t R = S::kRows, ST = S::kAhead, SLOTS = S::kSlots, TILE = S::kTile;
   extern __shared__ unsigned char raw[];
   __shared__ __align__(8) uint64_t s_full[ST], s_empty[ST], s_loaded[ST], s_sum_full[2], s_sum_empty[2], s_done;
   __shared__ uint32_t s_tmem;
-  const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = cta_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+  const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32, rank = cta_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   const uint32_t stages = (smem_at(raw) + 1023u) & ~1023u, CH = MODE == kGrads ? S::kChunk : a.chunk;
 
   if (warp == kSumWarps) {
@@ -205,110 +209,130 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
   if (warp >= kSumWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHeadRegsRest));
     HeadTile w;
-    if (warp == kSumWarps && lane == 0 && rank == 0) {
+    if (warp == kSumWarps && rank == 0) {
       bool alive = true;
-      uint32_t it = 0, chunk = 0, in = 0;   // in: steps of the chunk
-      const auto products = [&](auto outer_a, auto outer_b, auto parts_b, uint32_t acc, uint32_t at, uint32_t bt, bool first) {
+      const bool one = elect_one();
+      uint32_t it = 0, chunk = 0, in = 0, slot = 0;   // in: steps of the chunk
+      const auto products = [&](auto outer_a, auto outer_b, auto parts_b, uint32_t acc, bool first) {
         constexpr bool kOuterA = decltype(outer_a)::value, kOuterB = decltype(outer_b)::value;
+        constexpr uint32_t kB = decltype(parts_b)::value;
         const uint32_t idesc = a.idesc | uint32_t(kOuterA) << 15 | uint32_t(kOuterB) << 16 | idesc_cols(256);
+        uint64_t ad[PA], bd[kB];
+#pragma unroll
+        for (uint32_t i = 0; i < PA; ++i) ad[i] = tile_desc<kOuterA, R>(stages + slot * TILE), slot = slot + 1 == SLOTS ? 0 : slot + 1;
+#pragma unroll
+        for (uint32_t j = 0; j < kB; ++j) bd[j] = tile_desc<kOuterB, R>(stages + slot * TILE), slot = slot + 1 == SLOTS ? 0 : slot + 1;
+        if (one)
 #pragma unroll
         for (uint32_t k = 0; k < R / 16; ++k) {
 #pragma unroll
           for (uint32_t i = 0; i < PA; ++i)
 #pragma unroll
-            for (uint32_t j = 0; j < decltype(parts_b)::value; ++j)
-              if (i + j < 2) {
-                const uint64_t ad = kOuterA ? desc_outer<R>(at + i * TILE, k) : desc_inner(at + i * TILE, k);
-                const uint64_t bd = kOuterB ? desc_outer<R>(bt + j * TILE, k) : desc_inner(bt + j * TILE, k);
-                mma(acc, ad, bd, idesc, !first || k || i || j);
-              }
+            for (uint32_t j = 0; j < kB; ++j)
+              if (i + j < 2) mma(acc, ad[i] + desc_step<kOuterA>(k), bd[j] + desc_step<kOuterB>(k), idesc, !first || k || i || j);
         }
       };
       using Yes = std::true_type;
       using No = std::false_type;
       for (uint32_t i = 0; alive && head_tile<MODE>(a, pair, pairs, i, &w); ++i) {
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
-          const uint32_t st = it % ST, at = stages + st * S::kStage, bt = at + PA * TILE, acc = tmem + (chunk & 1) * 256;
+          const uint32_t st = it % ST, acc = tmem + (chunk & 1) * 256;
           const bool begins = in == 0;
-          if (begins && chunk >= 2) alive = bar_wait(smem_at(&s_sum_empty[chunk & 1]), (chunk / 2 - 1) & 1);
-          alive = alive && bar_wait(smem_at(&s_full[st]), it / ST & 1);
+          if (begins && chunk >= 2) alive = warp_wait(smem_at(&s_sum_empty[chunk & 1]), (chunk / 2 - 1) & 1);
+          alive = alive && warp_wait(smem_at(&s_full[st]), it / ST & 1);
           if (!alive) break;
           tmem_after();
           if constexpr (MODE == kGrads) {
-            if (w.hidden) products(Yes{}, No{}, std::integral_constant<uint32_t, PH>{}, acc, at, bt, begins);
-            else products(Yes{}, Yes{}, std::integral_constant<uint32_t, PB>{}, acc, at, bt, begins);
+            if (w.hidden) products(Yes{}, No{}, std::integral_constant<uint32_t, PH>{}, acc, begins);
+            else products(Yes{}, Yes{}, std::integral_constant<uint32_t, PB>{}, acc, begins);
           } else {
-            products(No{}, No{}, std::integral_constant<uint32_t, PB>{}, acc, at, bt, begins);
+            products(No{}, No{}, std::integral_constant<uint32_t, PB>{}, acc, begins);
           }
-          mma_commit(smem_at(&s_empty[st]));
+          if (one) mma_commit(smem_at(&s_empty[st]));
           if (++in == CH || s == w.steps - 1) {
-            mma_commit(smem_at(&s_sum_full[chunk++ & 1]));
+            if (one) mma_commit(smem_at(&s_sum_full[chunk & 1]));
+            ++chunk;
             in = 0;
           }
         }
       }
-      mma_commit(smem_at(&s_done));   // waited for in both CTAs, at the end: nothing is under way when tensor memory is given back
-      if (!alive) report(a.status, DGS_ETIMEOUT);
+      if (one) mma_commit(smem_at(&s_done));   // waited for in both CTAs, at the end: nothing is under way when tensor memory is given back
+      if (!alive && lane == 0) report(a.status, DGS_ETIMEOUT);
     }
-    if ((warp == kSumWarps + 1 || warp == kSumWarps + 3) && lane == 0) {
+    if (warp == kSumWarps + 1 || warp == kSumWarps + 3) {
+      const bool one = elect_one();
       const bool second = warp == kSumWarps + 3;   // of the two operands
       bool alive = true;
-      uint32_t it = 0;
+      uint32_t it = 0, done = 0, slot = 0, used = 0, narrow = 0;   // steps begun, steps whose products are known to be done; narrow: bit i, step i's tiles are PA + PH
       const uint32_t col_blocks = a.piece_cols / 64;
-      const uint64_t plane = uint64_t(a.row_blocks) * col_blocks * kBlockBytes;
       for (uint32_t i = 0; alive && head_tile<MODE>(a, pair, pairs, i, &w); ++i) {
-        const uint32_t m = w.m0 + rank * 128, n = w.n0 + rank * 128;
+        const uint32_t m = w.m0 + rank * 128, n = w.n0 + rank * 128, tiles = PA + (w.hidden ? PH : PB);
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
-          const uint32_t st = it % ST, at = stages + st * S::kStage, bt = at + PA * TILE, bar = smem_at(&s_loaded[st]), k0 = (w.from + s) * R;
-          if (it >= ST && !(alive = bar_wait(smem_at(&s_empty[st]), (it / ST - 1) & 1))) break;
-          if (!second) {
+          const uint32_t st = it % ST, bar = smem_at(&s_loaded[st]), k0 = (w.from + s) * R;
+          while (used + tiles > SLOTS || it - done >= ST) {
+            if (!(alive = warp_wait(smem_at(&s_empty[done % ST]), done / ST & 1))) break;
+            used -= PA + (narrow >> done % ST & 1 ? PH : PB);
+            ++done;
+          }
+          if (!alive) break;
+          used += tiles;
+          narrow = (narrow & ~(1u << st)) | uint32_t(w.hidden) << st;
+          uint32_t at[PA + PB];
+#pragma unroll
+          for (uint32_t p = 0; p < PA + PB; ++p) {
+            at[p] = stages + slot * TILE;
+            if (p < tiles) slot = slot + 1 == SLOTS ? 0 : slot + 1;
+          }
+          if (!one) {
+          } else if (!second) {
             bar_expect(bar, PA * TILE);
 #pragma unroll
             for (uint32_t p = 0; p < PA; ++p) {
               if constexpr (MODE == kGrads) {
                 for (uint32_t b = 0; b < 2; ++b)
-                  tma_load3(at + p * TILE + b * R * 128, w.hidden ? &map_b : &map_a, int(m + b * 64), int(k0 + (w.hidden ? a.first_word : 0)), int(p), bar);
+                  tma_load3(at[p] + b * R * 128, w.hidden ? &map_b : &map_a, int(m + b * 64), int(k0 + (w.hidden ? a.first_word : 0)), int(p), bar);
               } else {
-                for (uint32_t b = 0; b < R / 64; ++b) tma_load3(at + p * TILE + b * kBlockBytes, &map_a, int(k0 + b * 64), int(m), int(p), bar);
+                for (uint32_t b = 0; b < R / 64; ++b) tma_load3(at[p] + b * kBlockBytes, &map_a, int(k0 + b * 64), int(m), int(p), bar);
               }
             }
           } else if constexpr (MODE == kGrads) {
             bar_expect(bar, (w.hidden ? PH : PB) * TILE);
 #pragma unroll
             for (uint32_t p = 0; p < PB; ++p) {
-              const unsigned char* from = a.s + p * plane;
+              const unsigned char* from = a.s + p * a.plane;
               if (!w.hidden) {   // rows k0 on of 128 columns
                 for (uint32_t b = 0; b < 2; ++b)
-                  bulk_load(bt + p * TILE + b * R * 128, from + (uint64_t(k0 / 128) * col_blocks + n / 64 + b) * kBlockBytes + k0 % 128 * 128, R * 128, bar);
+                  bulk_load(at[PA + p] + b * R * 128, from + (uint64_t(k0 / 128) * col_blocks + n / 64 + b) * kBlockBytes + k0 % 128 * 128, R * 128, bar);
               } else if (p < PH) {   // columns k0 on of 128 rows
-                bulk_load(bt + p * TILE, from + (uint64_t(n / 128) * col_blocks + k0 / 64) * kBlockBytes, kBlockBytes, bar);
+                bulk_load(at[PA + p], from + (uint64_t(n / 128) * col_blocks + k0 / 64) * kBlockBytes, kBlockBytes, bar);
               }
             }
           } else {
             bar_expect(bar, PB * TILE);
 #pragma unroll
             for (uint32_t p = 0; p < PB; ++p)
-              for (uint32_t b = 0; b < R / 64; ++b) tma_load3(bt + p * TILE + b * kBlockBytes, &map_b, int(k0 + b * 64), int(a.first_word + n), int(p), bar);
+              for (uint32_t b = 0; b < R / 64; ++b) tma_load3(at[PA + p] + b * kBlockBytes, &map_b, int(k0 + b * 64), int(a.first_word + n), int(p), bar);
           }
         }
       }
       // Nothing is under way to this CTA's memory when it leaves: its copies, and the arrivals that the products' commits send to both CTAs.
-      for (uint32_t i = it > ST ? it - ST : 0; i < it; ++i) {
-        const bool landed = bar_wait(smem_at(&s_loaded[i % ST]), i / ST & 1);
-        alive = alive && landed && bar_wait(smem_at(&s_empty[i % ST]), i / ST & 1);
+      for (; done < it; ++done) {
+        const bool landed = warp_wait(smem_at(&s_loaded[done % ST]), done / ST & 1);
+        alive = alive && landed && warp_wait(smem_at(&s_empty[done % ST]), done / ST & 1);
       }
-      if (!alive) report(a.status, DGS_ETIMEOUT);
+      if (!alive && lane == 0) report(a.status, DGS_ETIMEOUT);
     }
-    if (warp == kSumWarps + 2 && lane == 0) {
+    if (warp == kSumWarps + 2) {
+      const bool one = elect_one();
       bool alive = true;
       uint32_t it = 0;
       for (uint32_t i = 0; alive && head_tile<MODE>(a, pair, pairs, i, &w); ++i) {
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
-          if (!(alive = bar_wait(smem_at(&s_loaded[it % ST]), it / ST & 1))) break;
-          bar_arrive_cluster(in_leader(smem_at(&s_full[it % ST])));
+          if (!(alive = warp_wait(smem_at(&s_loaded[it % ST]), it / ST & 1))) break;
+          if (one) bar_arrive_cluster(in_leader(smem_at(&s_full[it % ST])));
         }
       }
-      if (!alive) report(a.status, DGS_ETIMEOUT);
+      if (!alive && lane == 0) report(a.status, DGS_ETIMEOUT);
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kHeadRegsSum));
@@ -390,17 +414,17 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
             for (int i = 0; i < 64; ++i) acc[i] = kNone;
           }
           const float g = target < 0 ? 0.0f : by * up_g;
-          // Sixteen columns at a time: 32 bytes of a block's row for each of s's parts, its two pieces exchanged by the lowest bit of the row's number.  (By way of
-          // shared memory and copies of 4 KB, the fences and the waits for the buffer took 3000 cycles of a tile's 13,000.)
-          const uint32_t col_blocks = a.piece_cols / 64, turn = lane & 7;
-          unsigned char* const to = a.s + (uint64_t(w.m0 / 128 + rank) * col_blocks + col0 / 64) * kBlockBytes + (quarter * 32 + lane) * 128;
-          const uint64_t plane = uint64_t(a.row_blocks) * col_blocks * kBlockBytes;
+          // By way of 4 KB of shared memory for each warp, so that eight lanes write a row's 128 bytes.
+          const uint32_t stage = stages + SLOTS * TILE + warp * 4096;
+          unsigned char* const to = a.s + (uint64_t(w.m0 / 128 + rank) * (a.piece_cols / 64) + col0 / 64) * kBlockBytes + quarter * 4096 + lane * 16;
+          uint32_t rest[32];
+          __syncwarp();
 #pragma unroll
-          for (uint32_t q = 0; q < 4; ++q) {
-            uint32_t part[2][8];
+          for (uint32_t q = 0; q < 8; ++q) {
+            uint32_t first[4];
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) {
-              const uint32_t c = q * 16 + i * 2;
+            for (uint32_t i = 0; i < 4; ++i) {
+              const uint32_t c = q * 8 + i * 2;
               const float2 d = mul2(add2(make_float2(acc[c], acc[c + 1]), both(-lse)), both(kLog2e));
               float2 v = mul2(make_float2(hardware_exp2(d.x), hardware_exp2(d.y)), both(g));
               if (has) {   // g is 0 in a row without a target
@@ -410,16 +434,29 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
               const __half2 hi = __floats2half2_rn(v.x, v.y);
               const float2 f = __half22float2(hi);
               const __half2 lo = __floats2half2_rn(v.x - f.x, v.y - f.y);
-              memcpy(&part[0][i], &hi, 4);
-              memcpy(&part[1][i], &lo, 4);
+              memcpy(&first[i], &hi, 4);
+              memcpy(&rest[q * 4 + i], &lo, 4);
             }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 128 + ((q ^ (lane & 7)) << 4)), "r"(first[0]), "r"(first[1]), "r"(first[2]), "r"(first[3]) : "memory");
+          }
+          const auto out = [&](unsigned char* at) {
+            __syncwarp();
 #pragma unroll
-            for (uint32_t p = 0; p < 2; ++p) {
-              uint32_t o[8];
-#pragma unroll
-              for (uint32_t i = 0; i < 8; ++i) o[i] = turn & 1 ? part[p][i ^ 4] : part[p][i];
-              if (p < a.parts) store_sector(to + p * plane + ((q * 2 ^ (turn & 6)) << 4), o);
+            for (uint32_t q = 0; q < 8; ++q) {
+              uint4 v;
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(stage + q * 512 + lane * 16));
+              __stcg(reinterpret_cast<uint4*>(at + q * 512), v);
             }
+          };
+          out(to);
+          if (a.parts == 2) {
+            __syncwarp();
+#pragma unroll
+            for (uint32_t q = 0; q < 8; ++q)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 128 + ((q ^ (lane & 7)) << 4)), "r"(rest[q * 4]), "r"(rest[q * 4 + 1]), "r"(rest[q * 4 + 2]),
+                           "r"(rest[q * 4 + 3])
+                           : "memory");
+            out(to + a.plane);
           }
         }
       } else if (row < a.width) {
@@ -754,7 +791,7 @@ Shares share_out(const Work& words, const Work& hidden) {
   return best;
 }
 
-constexpr uint64_t kPieceBytes = 256ull << 20;   // of s, where one tile of words does not take more
+constexpr uint64_t kPieceBytes = 320ull << 20;   // of s, where one tile of words does not take more
 
 struct HeadPlan {
   uint32_t parts, stride, piece_tiles, pieces, row_blocks;
@@ -966,10 +1003,10 @@ Head head_of(const dgs_matrix* h, const dgs_matrix* w, const void* target, uint3
 
 Few few_of(const dgs_matrix* h, const dgs_matrix* w, const HeadPlan& p) { return {h->data, w->data, h->stride, w->stride, (h->cols + kSpan - 1) / kSpan, p.few_tiles}; }
 
+template <int MODE>
 void logit_steps(uint32_t parts, Head* a) {
-  using One = Step<kLoss, 1, 1>;
-  using Two = Step<kLoss, 2, 2>;
-  static_assert(One::kRows == Step<kSlope, 1, 1>::kRows && Two::kRows == Step<kSlope, 2, 2>::kRows, "");
+  using One = Step<MODE, 1, 1>;
+  using Two = Step<MODE, 2, 2>;
   a->steps = ceil_div(a->width, parts == 2 ? Two::kRows : One::kRows);
   a->chunk = std::min(ceil_div(a->steps, 2), parts == 2 ? Two::kChunk : One::kChunk);
 }
@@ -1026,7 +1063,7 @@ extern "C" int dgs_vocabulary_loss(const dgs_matrix* hidden, const dgs_matrix* w
   a.tiles = a.m_tiles * a.n_tiles;
   a.partial = reinterpret_cast<float2*>(work + p.inner_h + p.inner_w + p.scales);
   a.at_target = reinterpret_cast<float*>(work + p.inner_h + p.inner_w + p.scales + p.partial);
-  logit_steps(p.parts, &a);
+  logit_steps<kLoss>(p.parts, &a);
   rc = p.parts == 2 ? head_launch<kLoss, 2, 2, 0>(a, a.tiles, map_h, map_w, launched, st) : head_launch<kLoss, 1, 1, 0>(a, a.tiles, map_h, map_w, launched, st);
   if (rc != DGS_OK) return rc;
   const EarlyLaunch l(dim3(ceil_div(n, 32)), 256, 0, st);
@@ -1106,6 +1143,7 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
   a.row_blocks = p.row_blocks;
   a.parts = dw || hidden->type != DGS_TYPE_BF16 ? 2 : 1;
   a.piece_cols = p.piece_tiles * 256;
+  a.plane = p.s / 2;
 
   if (cudaMemsetAsync(most, 0, p.most, st) != cudaSuccess) return DGS_ECUDA;
   const Source h = source_of(hidden), w = source_of(weight);
@@ -1130,7 +1168,7 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
   a.dh.splits = p.shares.hidden;
   a.dw.out = p.shares.words > 1 ? part_w : dw;
   a.dw.splits = p.shares.words;
-  logit_steps(p.parts, &a);
+  logit_steps<kSlope>(p.parts, &a);
   for (uint32_t piece = 0; piece < p.pieces; ++piece) {
     const uint32_t tile0 = piece * p.piece_tiles, tiles = std::min(p.piece_tiles, ceil_div(v, 256) - tile0);
     Head s = a;

@@ -276,9 +276,10 @@ def route_experts_grad(logits: torch.Tensor, expert: torch.Tensor, dweight: torc
 
 def _slots(place: torch.Tensor) -> int:
     """k of a [tokens, k] place."""
-    if not isinstance(place, torch.Tensor) or place.dim() < 1 or not 1 <= place.shape[-1] <= dgs.DGS_ROUTE_MAX_K:
+    k = place.shape[-1] if isinstance(place, torch.Tensor) and place.dim() else 0
+    if not 1 <= k <= 32:                                # DGS_ROUTE_MAX_K
         raise ValueError(f"place is [tokens, k], k from 1 to {dgs.DGS_ROUTE_MAX_K}")
-    return place.shape[-1]
+    return k
 
 
 def _fit(m: "dgs.dgs_matrix", what: str, rows: int, cols: int, kind: int) -> None:
@@ -286,12 +287,14 @@ def _fit(m: "dgs.dgs_matrix", what: str, rows: int, cols: int, kind: int) -> Non
         raise ValueError(f"{what} must be {rows} x {cols} and of the other matrices' type: got {m.rows} x {m.cols}")
 
 
-def _rows_like(out: Optional[torch.Tensor], what: str, shape, m: "dgs.dgs_matrix", rows: int, like: torch.Tensor):
+def _rows_like(out: Optional[torch.Tensor], m: "dgs.dgs_matrix", rows: int, like: torch.Tensor):
     """(out, its matrix): `rows` rows of m's columns and type, a new tensor if there is none."""
+    cols, kind = m.cols, m.type
     if out is None:
-        out = torch.empty(shape, dtype=like.dtype, device=like.device)
-    mo = _matrix(out, what)
-    _fit(mo, what, rows, m.cols, m.type)
+        out = torch.empty((rows, cols), dtype=like.dtype, device=like.device)
+        return out, dgs.dgs_matrix(out.data_ptr(), rows, cols, cols, kind)
+    mo = _matrix(out, "out")
+    _fit(mo, "out", rows, cols, kind)
     _same_device(like.device, out)
     return out, mo
 
@@ -301,25 +304,24 @@ def gather_experts(x: torch.Tensor, order: torch.Tensor, place: torch.Tensor, *,
     zero where order[i] is -1.  Returns [tokens * k, cols]."""
     m = _matrix(x, "x")
     _cut_off(x, "x", "gather_experts")
-    k = _slots(place)
+    k, device = _slots(place), x.device
     slots = m.rows * k
-    po = _plain(order, "order", torch.int32, slots, x.device)
-    pp = _plain(place, "place", torch.int32, slots, x.device)
-    out, mo = _rows_like(out, "out", (slots, m.cols), m, slots, x)
-    _enqueue(x.device, dgs.dgs_experts_gather, m, po, pp, k, mo)
+    po = _plain(order, "order", torch.int32, slots, device)
+    pp = _plain(place, "place", torch.int32, slots, device)
+    out, mo = _rows_like(out, m, slots, x)
+    _enqueue(device, dgs.dgs_experts_gather, m, po, pp, k, mo)
     return out
 
 
 def _combine(y, weight, place, out, what):
     m = _matrix(y, what)
-    k = _slots(place)
-    if m.rows % k:
-        raise ValueError(f"{what} has a row for each of the tokens' {k} slots: got {m.rows} rows")
-    tokens = m.rows // k
-    pw = _plain(weight, "weight", torch.float32, m.rows, y.device)
-    pp = _plain(place, "place", torch.int32, m.rows, y.device)
-    out, mo = _rows_like(out, "out", (tokens, m.cols), m, tokens, y)
-    _enqueue(y.device, dgs.dgs_experts_combine, m, pw, pp, k, mo)
+    k, rows, device = _slots(place), m.rows, y.device
+    if rows % k:
+        raise ValueError(f"{what} has a row for each of the tokens' {k} slots: got {rows} rows")
+    pw = _plain(weight, "weight", torch.float32, rows, device)
+    pp = _plain(place, "place", torch.int32, rows, device)
+    out, mo = _rows_like(out, m, rows // k, y)
+    _enqueue(device, dgs.dgs_experts_combine, m, pw, pp, k, mo)
     return out
 
 
@@ -351,7 +353,7 @@ def combine_experts_grad(dout: torch.Tensor, y: torch.Tensor, weight: torch.Tens
     pw = _plain(weight, "weight", torch.float32, slots, device)
     po = _plain(order, "order", torch.int32, slots, device)
     pp = _plain(place, "place", torch.int32, slots, device)
-    out, mo = _rows_like(out, "out", (slots, m.cols), m, slots, dout)
+    out, mo = _rows_like(out, m, slots, dout)
     dweight = torch.empty(place.shape, dtype=torch.float32, device=device)
     _enqueue(device, dgs.dgs_experts_combine_grad, m, my, pw, po, pp, k, mo, dweight.data_ptr())
     return out, dweight
