@@ -815,10 +815,10 @@ Work hidden_of(uint64_t n, uint32_t d, uint32_t tiles, uint32_t type) {
 
 // Few rows go without tensor cores where there are not many products in all.  Here / with tensor cores, us a call.  Loss, 16 bits: 64 x 512 x 1000 10.5 / 12.5,
 // 3 x 2048 x 8000 15 / 21, 8 of them 25 / 21, 1 x 768 x 50257 20 / 33, 3 of them 32 / 33, 8 47 / 33; f32: 16 x 2048 x 8000 49 / 64, 37 101 / 64, 16 x 768 x 50257
-// 81 / 102, 37 178 / 102.  Gradient, 16 bits: 37 x 512 x 1000 27 / 35, 64 37 / 37, 1 x 768 x 50257 125 / 167, 3 of them 193 / 166, 3 x 2048 x 8000 97 / 86; f32:
-// 64 x 512 x 1000 36 / 52, 8 x 2048 x 8000 91 / 155, 16 161 / 156, 8 x 768 x 50257 181 / 285, 16 300 / 286.
+// 81 / 102, 37 178 / 102.  Gradient, 16 bits: 37 x 512 x 1000 21 / 35, 64 27 / 37, 1 x 2048 x 8000 85 / 87, 3 of them 97 / 86, 1 x 768 x 50257 182 / 161; f32:
+// 64 x 512 x 1000 25 / 52, 8 x 2048 x 8000 91 / 155, 16 161 / 160, 8 x 768 x 50257 181 / 285, 16 300 / 290.
 bool few_rows(uint64_t n, uint64_t v, uint32_t d, uint32_t type, bool grad) {
-  const uint64_t rows = n == 1 ? 1 : n <= 4 ? 4 : up_to(n, 8), most = type == DGS_TYPE_F32 ? (grad ? 260000000 : 640000000) : grad ? 40000000 : 100000000;
+  const uint64_t rows = n == 1 ? 1 : n <= 4 ? 4 : up_to(n, 8), most = type == DGS_TYPE_F32 ? (grad ? 310000000 : 640000000) : grad ? 36000000 : 100000000;
   return n <= kFewRows && v * d <= most / rows;
 }
 
@@ -849,16 +849,14 @@ int plan_head(const dgs_matrix* h, const dgs_matrix* w, bool grad, HeadPlan* out
   if (n && few_rows(n, v, d, h->type, grad)) {
     p->few = n == 1 ? 1 : n <= 4 ? 4 : 8;
     if (grad) {
-      // Small tiles where the words are few, and for one row of 16 bits, which is bound by trips to memory (1 x 768 x 50257: 125 us, 182 with large ones; in
-      // f32 123 and 101, eight rows 293 and 259).
-      const bool one = n == 1 && h->type != DGS_TYPE_F32;
-      p->few_words = v <= 8 * 2 * kSms || one ? 8 : 32;
+      p->few_words = v <= 8 * 2 * kSms ? 8 : 32;   // small tiles where the words are few
       p->few_tiles = ceil_div(v, p->few_words);
-      p->few_ctas = std::min(p->few_tiles, kSms * (one ? 6 : 2));
+      p->few_ctas = std::min(p->few_tiles, kSms * 2);
       p->part_h = up_to(uint64_t(p->few_ctas) * n * d * 4, 256);
       p->bytes = p->part_h;
     } else {
-      p->few_ctas = std::min(ceil_div(v, 8 * kFewWords), kSms * 3);
+      const uint32_t passes = ceil_div(v, 8 * kFewWords);   // of a CTA; all make as many
+      p->few_ctas = ceil_div(passes, ceil_div(passes, kSms * 4));
       p->partial = up_to(uint64_t(p->few_ctas) * n * 8, 256);
       p->at_target = up_to(n * 4, 256);
       p->bytes = p->partial + p->at_target;
@@ -1107,9 +1105,9 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
     return with_few(hidden, weight, p.few, [&](auto* t, auto vec, auto together) {
       using T = std::remove_pointer_t<decltype(t)>;
       if (p.few_words == 8)
-        k_few_grad<T, vec.value, together.value, 8><<<p.few_ctas, 256, 0, st>>>(a, f, dw, parts);
+        k_few_grad<T, vec.value, together.value, 8><<<p.few_ctas, kFewThreads<8>, 0, st>>>(a, f, dw, parts);
       else
-        k_few_grad<T, vec.value, together.value, 32><<<p.few_ctas, 256, 0, st>>>(a, f, dw, parts);
+        k_few_grad<T, vec.value, together.value, 32><<<p.few_ctas, kFewThreads<32>, 0, st>>>(a, f, dw, parts);
       if (cudaGetLastError() != cudaSuccess) return int(DGS_ECUDA);
       const EarlyLaunch l(dim3(ceil_div(a.width, 32), a.rows), 256, 0, st);
       return cudaLaunchKernelEx(&l.cfg, k_few_hidden<T>, a, static_cast<const float*>(parts), p.few_ctas, static_cast<T*>(dhidden->data), dhidden->stride) == cudaSuccess

@@ -38,10 +38,11 @@ struct Few {
 // The products of rows row0 .. row0 + RB with words word0 .. word0 + 4: lane l gets row l / (32 / (4 RB)) % RB with word l / (32 / 4).
 template <class T, bool VEC, uint32_t RB>
 __device__ __forceinline__ float few_products(const Head& a, const Few& f, uint32_t row0, uint32_t word0, uint32_t lane) {
+  constexpr int kUnroll = RB == 1 ? 3 : 1;   // of 256 columns: one row's loads are all there is to wait for
   float2 sum[kFewWords * RB];
 #pragma unroll
   for (uint32_t i = 0; i < kFewWords * RB; ++i) sum[i] = make_float2(0.0f, 0.0f);
-#pragma unroll 1
+#pragma unroll kUnroll
   for (uint32_t s = 0; s < f.spans; ++s) {
     Eight<T> we[kFewWords];
 #pragma unroll
@@ -118,8 +119,9 @@ __global__ void __launch_bounds__(256) k_few_rows(const __grid_constant__ Head a
 }
 
 // dW of the words and, in `parts` [CTAs][rows][width], each CTA's part of dh.
+template <uint32_t TW> constexpr uint32_t kFewThreads = TW == 8 ? 512 : 256;
 template <class T, bool VEC, uint32_t RB, uint32_t TW>
-__global__ void __launch_bounds__(256, 2) k_few_grad(const __grid_constant__ Head a, const __grid_constant__ Few f, float* dw, float* parts) {
+__global__ void __launch_bounds__(kFewThreads<TW>, TW == 8 ? 1 : 2) k_few_grad(const __grid_constant__ Head a, const __grid_constant__ Few f, float* dw, float* parts) {
   constexpr uint32_t V = kFewWords * RB, kSame = 32 / V;
   __shared__ __align__(16) float s_s[kFewRows][TW];
   __shared__ int s_target[kFewRows];
@@ -130,7 +132,7 @@ __global__ void __launch_bounds__(256, 2) k_few_grad(const __grid_constant__ Hea
   parts += uint64_t(blockIdx.x) * a.rows * a.width;
   for (uint32_t tile = blockIdx.x; tile < f.tiles; tile += gridDim.x) {
     const uint32_t first = tile * TW, row_blocks = (a.rows + RB - 1) / RB;
-    for (uint32_t u = warp; u < row_blocks * (TW / kFewWords); u += 8) {
+    for (uint32_t u = warp; u < row_blocks * (TW / kFewWords); u += kFewThreads<TW> / 32) {
       const uint32_t row0 = u / (TW / kFewWords) * RB, word0 = first + u % (TW / kFewWords) * kFewWords;
       if (word0 >= a.words) continue;
       const float z = few_products<T, VEC, RB>(a, f, row0, word0, lane);
@@ -144,28 +146,36 @@ __global__ void __launch_bounds__(256, 2) k_few_grad(const __grid_constant__ Hea
     }
     __syncthreads();
     const uint32_t words = min(TW, a.words - first);
-    for (uint32_t c = threadIdx.x; c < a.width; c += 256) {
+    for (uint32_t c = threadIdx.x; c < a.width; c += kFewThreads<TW>) {
       float w[TW], d[TW];
 #pragma unroll
       for (uint32_t i = 0; i < TW; ++i) w[i] = i < words ? Elem<T>::get(static_cast<const T*>(f.w)[(first + i) * f.w_stride + c]) : 0.0f, d[i] = 0.0f;
-#pragma unroll 2
-      for (uint32_t r = 0; r < a.rows; ++r) {
-        float sum = 0.0f;
-        if (s_target[r] >= 0) {
-          const float x = Elem<T>::get(static_cast<const T*>(f.h)[r * f.h_stride + c]);
+      constexpr uint32_t kAtOnce = TW == 8 ? 8 : 4;   // rows whose values are on their way together
+      for (uint32_t r0 = 0; r0 < a.rows; r0 += kAtOnce) {
+        float x[kAtOnce];
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) {
+          const uint32_t r = r0 + i;
+          x[i] = r < a.rows && s_target[r] >= 0 ? Elem<T>::get(static_cast<const T*>(f.h)[r * f.h_stride + c]) : 0.0f;
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kAtOnce; ++j) {
+          const uint32_t r = r0 + j;
+          if (r >= a.rows) break;
+          float sum = 0.0f;   // s of an ignored row is 0
 #pragma unroll
           for (uint32_t i = 0; i < TW; i += 4) {
             if (i < words) {   // s behind the last word was not written
               const float4 s = *reinterpret_cast<const float4*>(&s_s[r][i]);
-              sum = fmaf(s.x, w[i], sum), d[i] = fmaf(s.x, x, d[i]);
-              sum = fmaf(s.y, w[i + 1], sum), d[i + 1] = fmaf(s.y, x, d[i + 1]);
-              sum = fmaf(s.z, w[i + 2], sum), d[i + 2] = fmaf(s.z, x, d[i + 2]);
-              sum = fmaf(s.w, w[i + 3], sum), d[i + 3] = fmaf(s.w, x, d[i + 3]);
+              sum = fmaf(s.x, w[i], sum), d[i] = fmaf(s.x, x[j], d[i]);
+              sum = fmaf(s.y, w[i + 1], sum), d[i + 1] = fmaf(s.y, x[j], d[i + 1]);
+              sum = fmaf(s.z, w[i + 2], sum), d[i + 2] = fmaf(s.z, x[j], d[i + 2]);
+              sum = fmaf(s.w, w[i + 3], sum), d[i + 3] = fmaf(s.w, x[j], d[i + 3]);
             }
           }
+          float* p = parts + uint64_t(r) * a.width + c;
+          *p = tile == blockIdx.x ? sum : *p + sum;
         }
-        float* p = parts + uint64_t(r) * a.width + c;
-        *p = tile == blockIdx.x ? sum : *p + sum;
       }
       if (dw)
 #pragma unroll
