@@ -8,8 +8,8 @@
 //
 // Numbers: s is kept as the sum of two fp16 numbers (22 bits) under one power of two for the call, since dW goes to a flat gradient in f32; products of fp16 need
 // fp16 partners, so W and h are held beside as fp16 numbers under a power of two for each column: exact for bfloat16 and fp16 values down to 2^-29 of their column's
-// largest, and below that to 2^-40 of it.  f32 matrices are sums of two fp16 numbers each; of their four products the smallest, under 2^-22 of the whole, is left out.
-// dh of bfloat16 is formed from the first part of s alone: 12 bits where the result keeps 8.
+// largest, and below that to 2^-40 of it (s likewise: an exponential below 2^-29 keeps fewer bits).  f32 matrices are sums of two fp16 numbers each; of their four products the smallest, under 2^-22 of the whole, is left out.
+// dh of bfloat16 is formed from the first part of s alone: 11 bits where the result keeps 8.
 #include "dgs_tensor.cuh"
 
 #include <algorithm>
@@ -87,23 +87,22 @@ constexpr float kNone = -__builtin_huge_valf();
 
 // One of the two products of a piece's s.
 struct Product {
-  uint32_t m_tiles, n_tiles, splits, tiles, steps, parts;   // steps over the whole contraction; parts of s that it takes
+  uint32_t m_tiles, n_tiles, splits, tiles, steps;   // steps over the whole contraction
   float* out;
 };
 struct Head {
   uint32_t rows, width, words;      // N, D, V
   uint32_t m_tiles, n_tiles, tiles, steps, chunk;   // logits
   uint32_t first_word, piece_cols;  // of the piece (a multiple of 256 in the workspace)
-  uint32_t row_blocks;              // of s
   uint32_t idesc;
-  uint32_t wide_targets, dloss_step, parts;
+  uint32_t wide_targets, dloss_step, parts;   // parts: of s that are wanted
   const void* target;
   const float *lse, *dloss;
   const uint32_t *most_h, *most_w, *most_g;     // bits of the largest magnitudes: of each column of h and of W, of dloss
   const float *row_h, *row_w;       // f32: what the rows of the logits' operands are multiplied with
   float2* partial;                  // [n_tiles * 4][rows]: maximum, sum
   float* at_target;                 // [rows]
-  unsigned char* s;                 // [2][row_blocks][piece_cols / 64] blocks
+  unsigned char* s;                 // [2][m_tiles * 2][piece_cols / 64] blocks
   uint64_t plane;                   // bytes of one part of s
   Product dw, dh;                   // out: dw or partial results [splits][piece_cols][width]; [splits][rows][width]
   uint32_t share_few, share_more;   // tiles of dh for a pair of CTAs with one more tile of dw, and for others
@@ -170,6 +169,8 @@ __device__ __forceinline__ bool head_tile(const Head& a, uint32_t pair, uint32_t
 // Warps: 0 to 15 keep the sums, 16 issues products, 17 and 19 copies (one operand each), 18 passes on that copies have landed.  Accumulators go to registers every
 // kChunk steps, since the tensor cores add with bits cut off, and are added up there with rounding.  One pair of CTAs per pair of SMs takes tile after tile,
 // so that the products of the next run while one is finished.
+// Warps 16 to 19 go through their loops with all lanes, one of which does what has to be done once: descriptors and addresses then stay in uniform registers (with
+// one lane in the loops the products of a step waited for their operands to be moved there: loss of 8192 x 768 x 50257 436 us, 383 so).
 template <int MODE, uint32_t PA, uint32_t PB, uint32_t PH>   // PH: parts of s that dh takes
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
 k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
@@ -222,14 +223,14 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
         for (uint32_t i = 0; i < PA; ++i) ad[i] = tile_desc<kOuterA, R>(stages + slot * TILE), slot = slot + 1 == SLOTS ? 0 : slot + 1;
 #pragma unroll
         for (uint32_t j = 0; j < kB; ++j) bd[j] = tile_desc<kOuterB, R>(stages + slot * TILE), slot = slot + 1 == SLOTS ? 0 : slot + 1;
-        if (one)
+        if (one) {
 #pragma unroll
-        for (uint32_t k = 0; k < R / 16; ++k) {
+          for (uint32_t k = 0; k < R / 16; ++k)
 #pragma unroll
-          for (uint32_t i = 0; i < PA; ++i)
+            for (uint32_t i = 0; i < PA; ++i)
 #pragma unroll
-            for (uint32_t j = 0; j < kB; ++j)
-              if (i + j < 2) mma(acc, ad[i] + desc_step<kOuterA>(k), bd[j] + desc_step<kOuterB>(k), idesc, !first || k || i || j);
+              for (uint32_t j = 0; j < kB; ++j)
+                if (i + j < 2) mma(acc, ad[i] + desc_step<kOuterA>(k), bd[j] + desc_step<kOuterB>(k), idesc, !first || k || i || j);
         }
       };
       using Yes = std::true_type;
@@ -377,11 +378,11 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
         const uint32_t word0 = a.first_word + col0;
         if constexpr (PA == 2) {
           const float row_by = row < a.rows ? a.row_h[row] : 0.0f;
+          float word_by[2];   // of two of the warp's words a lane
 #pragma unroll
-          for (uint32_t i = 0; i < 64; ++i) {
-            acc[i] = acc[i] * row_by * (word0 + i < a.words ? a.row_w[word0 + i] : 0.0f);
-            if (i % 8 == 7) asm volatile("" ::: "memory");   // not all of them on their way at once
-          }
+          for (uint32_t i = 0; i < 2; ++i) word_by[i] = word0 + i * 32 + lane < a.words ? a.row_w[word0 + i * 32 + lane] : 0.0f;
+#pragma unroll
+          for (uint32_t i = 0; i < 64; ++i) acc[i] = acc[i] * row_by * __shfl_sync(0xffffffffu, word_by[i / 32], i % 32);
         }
         if (word0 + 64 > a.words) {
 #pragma unroll
@@ -414,7 +415,9 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
             for (int i = 0; i < 64; ++i) acc[i] = kNone;
           }
           const float g = target < 0 ? 0.0f : by * up_g;
-          // By way of 4 KB of shared memory for each warp, so that eight lanes write a row's 128 bytes.
+          // By way of 4 KB of shared memory for each warp, so that eight lanes write a row's 128 bytes.  Bound by these stores: 5632 words of 8192 x 768 are 184 MB
+          // and 74 us, 60 with the first part alone, 51 without.  (Straight from the registers, 32 bytes a lane: 78.  By copies from shared memory, with
+          // their fences and waits for the buffer: 88.)
           const uint32_t stage = stages + SLOTS * TILE + warp * 4096;
           unsigned char* const to = a.s + (uint64_t(w.m0 / 128 + rank) * (a.piece_cols / 64) + col0 / 64) * kBlockBytes + quarter * 4096 + lane * 16;
           uint32_t rest[32];
@@ -724,10 +727,11 @@ __global__ void __launch_bounds__(256) k_head_hidden(const __grid_constant__ Hea
         const uint32_t c = col0 + i * 32 + lane;
         if (c < a.width) v[i] += parts[s * each + uint64_t(row) * a.width + c];
       }
+    const bool live = target_of(a, row, false) >= 0;   // others: 0, also where W holds infinities
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
       const uint32_t c = col0 + i * 32 + lane;
-      if (c < a.width) dh[row * stride + c] = Elem<T>::put(v[i] * down_of(a.most_w[c]) * by2);
+      if (c < a.width) dh[row * stride + c] = Elem<T>::put(live ? v[i] * down_of(a.most_w[c]) * by2 : 0.0f);
     }
   }
 }
@@ -1138,7 +1142,6 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
   a.dloss = dloss;
   a.dloss_step = dloss_stride;
   a.add = flags & DGS_LOSS_ADD ? 1 : 0;
-  a.row_blocks = p.row_blocks;
   a.parts = dw || hidden->type != DGS_TYPE_BF16 ? 2 : 1;
   a.piece_cols = p.piece_tiles * 256;
   a.plane = p.s / 2;

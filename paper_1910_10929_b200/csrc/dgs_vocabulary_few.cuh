@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(256) k_few_hidden(const __grid_constant__ Head
   __syncthreads();
   if (warp || c >= a.width) return;
   for (uint32_t q = 1; q < 8; ++q) v += s_sum[q][lane];
-  dh[row * stride + c] = Elem<T>::put(v);
+  dh[row * stride + c] = Elem<T>::put(target_of(a, row, false) >= 0 ? v : 0.0f);   // also where W holds infinities
 }
 
 }  // namespace

@@ -394,17 +394,17 @@ def vocabulary_loss(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Te
 def vocabulary_loss_grad(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
                          dw: Optional[torch.Tensor] = None, *, add: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The gradient of vocabulary_loss: returns that of the hidden states, of their type, and writes (with `add`, adds) the vocabulary's to dw, a
-    contiguous float32 tensor of words * width elements such as the layer's slice of the flat gradient.  dloss: float32, one for each row or one for all."""
+    contiguous float32 tensor of words * width elements such as the layer's slice of the flat gradient.  dloss: float32, one for each row or one for all (an expanded one too)."""
     mh, mw, pt, flags = _head(hidden, weight, target)
     device = hidden.device
     if add:
         flags |= dgs.DGS_LOSS_ADD
-    one = isinstance(dloss, torch.Tensor) and dloss.numel() == 1
-    pl = _plain(lse, "lse", torch.float32, mh.rows, device)
-    pg = _plain(dloss, "dloss", torch.float32, 1 if one else mh.rows, device)
-    pw = _plain(dw, "dw", torch.float32, mw.rows * mw.cols, device)
-    if (mh.rows and not pl) or not isinstance(dloss, torch.Tensor):
+    if not isinstance(lse, torch.Tensor) or not isinstance(dloss, torch.Tensor):
         raise ValueError("lse and dloss are tensors")
+    one = dloss.numel() == 1 or (dloss.numel() == mh.rows and not any(dloss.stride()))   # one value, or one value seen from every row
+    pl = _plain(lse, "lse", torch.float32, mh.rows, device)
+    pg = _plain(dloss[(0,) * dloss.dim()] if one else dloss, "dloss", torch.float32, 1 if one else mh.rows, device)
+    pw = _plain(dw, "dw", torch.float32, mw.rows * mw.cols, device)
     if out is None:
         out = torch.empty(hidden.shape, dtype=hidden.dtype, device=device)
     mo = _matrix(out, "out")
