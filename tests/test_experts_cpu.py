@@ -62,7 +62,7 @@ def test_torch_calls_refuse_what_does_not_fit(monkeypatch):
         with pytest.raises(ValueError, match="CUDA"):
             call()
     monkeypatch.setattr(operators, "_on_gpu", lambda t, what: None)
-    monkeypatch.setattr(operators, "_enqueue", lambda *a: pytest.fail("enqueued"))
+    monkeypatch.setattr(operators, "_run", lambda *a: pytest.fail("enqueued"))
     for bad in (dict(p=place.long()), dict(p=place[:, :1]), dict(p=place[:3]), dict(p=torch.zeros(4, 33, dtype=torch.int32)), dict(p=torch.zeros(4, 0, dtype=torch.int32)),
                 dict(p=torch.zeros(2, 4, dtype=torch.int32).T), dict(p=torch.zeros((), dtype=torch.int32)), dict(p=None)):
         for call in calls:

@@ -90,7 +90,7 @@ def test_torch_calls_refuse_what_does_not_fit(monkeypatch):
         with pytest.raises(ValueError, match="CUDA"):
             call()
     monkeypatch.setattr(operators, "_on_gpu", lambda t, what: None)
-    monkeypatch.setattr(operators, "_enqueue", lambda *a: pytest.fail("enqueued"))
+    monkeypatch.setattr(operators, "_run", lambda *a: pytest.fail("enqueued"))
     for call in (first, second):
         for bad in (dict(w=w[:, :7]), dict(w=w.half()), dict(t=t[:3]), dict(t=t.float()), dict(t=t.to(torch.int16)), dict(t=None), dict(t=torch.zeros(8, dtype=torch.int64)[::2]), dict(h=h.double())):
             with pytest.raises(ValueError):
