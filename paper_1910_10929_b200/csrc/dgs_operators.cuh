@@ -267,11 +267,11 @@ __device__ __forceinline__ void of_floats(const float2 (&v)[4], Eight<__half>& e
 // A warp takes 256 columns of a row, eight a lane, so that a row in 16 bits is read 512 bytes at a time wherever it lies.  Rows that
 // begin on 16 bytes: eight neighbours a lane; others: every 32nd column, so that a warp's elements are neighbours still.
 constexpr uint32_t kSpan = 256;
-template <class T, bool VEC, bool KEEP = false>   // KEEP: others will read it too
+template <class T, bool VEC, bool KEEP = false, bool WHOLE = false>   // KEEP: others will read it too; WHOLE: all 256 columns are there
 __device__ __forceinline__ void load8(const T* row, uint32_t col0, uint32_t lane, uint32_t cols, Eight<T>& e) {
   if constexpr (VEC) {
     const uint32_t c = col0 + lane * 8;
-    if (c + 8 <= cols) {
+    if (WHOLE || c + 8 <= cols) {
 #pragma unroll
       for (uint32_t i = 0; i < sizeof(T) / 2; ++i) {
         const uint4 w = KEEP ? __ldg(reinterpret_cast<const uint4*>(row + c) + i) : __ldcs(reinterpret_cast<const uint4*>(row + c) + i);
@@ -279,40 +279,43 @@ __device__ __forceinline__ void load8(const T* row, uint32_t col0, uint32_t lane
       }
       return;
     }
-    T t[8];
+    if constexpr (!WHOLE) {
+      T t[8];
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) t[i] = c + i < cols ? row[c + i] : Elem<T>::put(0.0f);
-    memcpy(e.w, t, sizeof(t));
+      for (uint32_t i = 0; i < 8; ++i) t[i] = c + i < cols ? row[c + i] : Elem<T>::put(0.0f);
+      memcpy(e.w, t, sizeof(t));
+    }
   } else {
     T t[8];
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
       const uint32_t c = col0 + i * 32 + lane;
-      t[i] = c < cols ? row[c] : Elem<T>::put(0.0f);
+      t[i] = WHOLE || c < cols ? row[c] : Elem<T>::put(0.0f);
     }
     memcpy(e.w, t, sizeof(t));
   }
 }
-template <class T, bool VEC>
+template <class T, bool VEC, bool WHOLE = false>
 __device__ __forceinline__ void store8(T* row, uint32_t col0, uint32_t lane, uint32_t cols, const Eight<T>& e) {
   T t[8];
   memcpy(t, e.w, sizeof(t));
   if constexpr (VEC) {
     const uint32_t c = col0 + lane * 8;
-    if (c + 8 <= cols) {
+    if (WHOLE || c + 8 <= cols) {
 #pragma unroll
       for (uint32_t i = 0; i < sizeof(T) / 2; ++i)
         __stcs(reinterpret_cast<uint4*>(row + c) + i, make_uint4(e.w[4 * i], e.w[4 * i + 1], e.w[4 * i + 2], e.w[4 * i + 3]));
       return;
     }
+    if constexpr (!WHOLE)
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i)
-      if (c + i < cols) row[c + i] = t[i];
+      for (uint32_t i = 0; i < 8; ++i)
+        if (c + i < cols) row[c + i] = t[i];
   } else {
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
       const uint32_t c = col0 + i * 32 + lane;
-      if (c < cols) row[c] = t[i];
+      if (WHOLE || c < cols) row[c] = t[i];
     }
   }
 }

@@ -510,19 +510,23 @@ __device__ __forceinline__ void columns_most(const Head& a, const Source& m, boo
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, col0 = block % m.spans * kSpan, row0 = block / m.spans * kMostRows;
   __shared__ uint32_t s_most[8][kSpan];
   uint32_t best[8] = {};
-#pragma unroll 2
-  for (uint32_t r = row0 + warp; r < min(row0 + kMostRows, m.rows); r += 8) {
-    if (targets && target_of(a, r, false) < 0) continue;
-    Eight<T> e;
-    load8<T, VEC>(static_cast<const T*>(m.data) + r * m.stride, col0, lane, m.cols, e);
-    float2 v[4];
-    floats_of(e, v);
+  const auto rows = [&](auto whole) {   // loads with a branch of their own for each lane would not be on their way together
+#pragma unroll 4
+    for (uint32_t r = row0 + warp; r < min(row0 + kMostRows, m.rows); r += 8) {
+      Eight<T> e;
+      load8<T, VEC, true, decltype(whole)::value>(static_cast<const T*>(m.data) + r * m.stride, col0, lane, m.cols, e);
+      const uint32_t all = !targets || target_of(a, r, false) >= 0 ? 0x7fffffffu : 0;
+      float2 v[4];
+      floats_of(e, v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      best[2 * i] = max(best[2 * i], __float_as_uint(v[i].x) & 0x7fffffffu);
-      best[2 * i + 1] = max(best[2 * i + 1], __float_as_uint(v[i].y) & 0x7fffffffu);
+      for (int i = 0; i < 4; ++i) {
+        best[2 * i] = max(best[2 * i], __float_as_uint(v[i].x) & all);
+        best[2 * i + 1] = max(best[2 * i + 1], __float_as_uint(v[i].y) & all);
+      }
     }
-  }
+  };
+  if (col0 + kSpan <= m.cols) rows(std::true_type{});
+  else rows(std::false_type{});
 #pragma unroll
   for (int i = 0; i < 8; ++i) s_most[warp][VEC ? lane * 8 + i : i * 32 + lane] = best[i];
   __syncthreads();
@@ -569,21 +573,26 @@ __device__ __forceinline__ void by_columns(const Head& a, const Source& m, bool 
     if (i % 2) up[i / 2].y = v;
     else up[i / 2].x = v;
   }
+  const auto rows = [&](auto whole) {
+    constexpr bool kWhole = decltype(whole)::value;
 #pragma unroll 4
-  for (uint32_t r = row0 + warp; r < min(row0 + kPlaneRows, m.rows); r += 8) {
-    Eight<__half> part[2] = {};
-    Eight<T> e;
-    load8<T, VEC>(static_cast<const T*>(m.data) + r * m.stride, col0, lane, m.cols, e);
-    if (!targets || target_of(a, r, false) >= 0) {
-      float2 v[4];
-      floats_of(e, v);
+    for (uint32_t r = row0 + warp; r < min(row0 + kPlaneRows, m.rows); r += 8) {
+      Eight<__half> part[2] = {};
+      Eight<T> e;
+      load8<T, VEC, false, kWhole>(static_cast<const T*>(m.data) + r * m.stride, col0, lane, m.cols, e);
+      if (!targets || target_of(a, r, false) >= 0) {
+        float2 v[4];
+        floats_of(e, v);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], up[i]);
-      halves(v, part[0], part[1]);
+        for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], up[i]);
+        halves(v, part[0], part[1]);
+      }
+#pragma unroll
+      for (uint32_t p = 0; p < P; ++p) store8<__half, VEC, kWhole>(out + (uint64_t(p) * m.rows + r) * stride, col0, lane, m.cols, part[p]);
     }
-#pragma unroll
-    for (uint32_t p = 0; p < P; ++p) store8<__half, VEC>(out + (uint64_t(p) * m.rows + r) * stride, col0, lane, m.cols, part[p]);
-  }
+  };
+  if (col0 + kSpan <= m.cols) rows(std::true_type{});
+  else rows(std::false_type{});
 }
 template <class T, bool VEC>
 __global__ void __launch_bounds__(256) k_head_columns(const __grid_constant__ Head a, const __grid_constant__ Source h, const __grid_constant__ Source w, uint32_t blocks_h,

@@ -42,16 +42,16 @@ __device__ __forceinline__ float few_products(const Head& a, const Few& f, uint3
   float2 sum[kFewWords * RB];
 #pragma unroll
   for (uint32_t i = 0; i < kFewWords * RB; ++i) sum[i] = make_float2(0.0f, 0.0f);
-#pragma unroll kUnroll
-  for (uint32_t s = 0; s < f.spans; ++s) {
+  const auto span = [&](uint32_t s, auto whole) {   // of 256 columns; loads with a branch in them would wait for one another
+    constexpr bool kWhole = decltype(whole)::value;
     Eight<T> we[kFewWords];
 #pragma unroll
     for (uint32_t i = 0; i < kFewWords; ++i)
-      load8<T, VEC>(static_cast<const T*>(f.w) + min(word0 + i, a.words - 1) * f.w_stride, s * kSpan, lane, a.width, we[i]);
+      load8<T, VEC, false, kWhole>(static_cast<const T*>(f.w) + min(word0 + i, a.words - 1) * f.w_stride, s * kSpan, lane, a.width, we[i]);
 #pragma unroll
     for (uint32_t r = 0; r < RB; ++r) {
       Eight<T> he;
-      load8<T, VEC, true>(static_cast<const T*>(f.h) + min(row0 + r, a.rows - 1) * f.h_stride, s * kSpan, lane, a.width, he);
+      load8<T, VEC, true, kWhole>(static_cast<const T*>(f.h) + min(row0 + r, a.rows - 1) * f.h_stride, s * kSpan, lane, a.width, he);
       float2 hv[4];
       floats_of(he, hv);
 #pragma unroll
@@ -62,7 +62,11 @@ __device__ __forceinline__ float few_products(const Head& a, const Few& f, uint3
         for (int k = 0; k < 4; ++k) sum[i * RB + r] = fma2(hv[k], wv[k], sum[i * RB + r]);
       }
     }
-  }
+  };
+  const uint32_t whole = a.width / kSpan;
+#pragma unroll kUnroll
+  for (uint32_t s = 0; s < whole; ++s) span(s, std::true_type{});
+  if (whole < f.spans) span(whole, std::false_type{});
   float v[kFewWords * RB];
 #pragma unroll
   for (uint32_t i = 0; i < kFewWords * RB; ++i) v[i] = sum[i].x + sum[i].y;
