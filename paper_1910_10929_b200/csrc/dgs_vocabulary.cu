@@ -41,16 +41,16 @@ enum : int { kLoss, kSlope, kGrads };
 //   contracted dimension outermost (h and s for dW, W for dh): blocks of 64 columns, kRows rows of 128 bytes each
 // Either way the 16-byte pieces of a row are exchanged by its number (128-byte swizzle).  s lies in the workspace in blocks of 128 rows and 64 columns that are in
 // that order already, so both uses copy it as it is.
-// kChunk: steps between two sums in registers, at most: 512 values, or 256 where each is three products.  Logits of few steps take half of them: an exponential takes a
-// logit's error as it is (a logit of 15 summed over 768 values in one go is off by 7e-6), and two chunks a tile let the products of the next tile run to their
-// end while one is finished.
+// kChunk: steps between two sums in registers, at most: 512 values; 256 of s and 64 of logits where each is three products, since their results are all in f32.
+// Logits of few steps take half of them: an exponential takes a logit's error as it is (a logit of 15 summed over 768 values in one go is off by 7e-6), and two
+// chunks a tile let the products of the next tile run to their end while one is finished.
 constexpr uint32_t kBlockBytes = 128 * 128;                       // 128 rows and 64 columns of s
 // Shared memory is a ring of tiles, one for each part of an operand and step: a step of dW takes three of the twelve, one of dh in bfloat16 two, so that
 // four or six steps are on their way.  (Four of either: the products of dh waited for copies, 0.46 us a step for 0.33.)
 template <int MODE, uint32_t PA, uint32_t PB> struct Step {
   static constexpr uint32_t kRows = MODE == kLoss && PA == 1 ? 128 : 64, kTile = kRows * 256, kSlots = (MODE == kSlope ? 160 : 192) * 1024 / kTile;
   static constexpr uint32_t kAhead = kSlots / 2;   // steps under way, at most
-  static constexpr uint32_t kChunk = 512 / kRows / PA, kSmem = 1024 + kSlots * kTile + (MODE == kSlope ? 64 * 1024 : 0);
+  static constexpr uint32_t kChunk = (PA == 1 ? 512 : MODE == kGrads ? 256 : 64) / kRows, kSmem = 1024 + kSlots * kTile + (MODE == kSlope ? 64 * 1024 : 0);
 };
 // Sixteen warps keep the sums, 64 columns of 32 rows each; four do the rest and leave them their registers.  (With eight warps of 128 columns, two a scheduler, the
 // trips to tensor memory and through the exponentials showed: 5632 words of 8192 x 768 took 105 us.)
@@ -223,14 +223,18 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
         for (uint32_t i = 0; i < PA; ++i) ad[i] = tile_desc<kOuterA, R>(stages + slot * TILE), slot = slot + 1 == SLOTS ? 0 : slot + 1;
 #pragma unroll
         for (uint32_t j = 0; j < kB; ++j) bd[j] = tile_desc<kOuterB, R>(stages + slot * TILE), slot = slot + 1 == SLOTS ? 0 : slot + 1;
-        if (one) {
+        if (one) {   // products with second parts first: what is cut off as they are added is small
+          bool more = !first;
 #pragma unroll
-          for (uint32_t k = 0; k < R / 16; ++k)
+          for (int i = PA - 1; i >= 0; --i)
 #pragma unroll
-            for (uint32_t i = 0; i < PA; ++i)
+            for (int j = kB - 1; j >= 0; --j)
 #pragma unroll
-              for (uint32_t j = 0; j < kB; ++j)
-                if (i + j < 2) mma(acc, ad[i] + desc_step<kOuterA>(k), bd[j] + desc_step<kOuterB>(k), idesc, !first || k || i || j);
+              for (uint32_t k = 0; k < R / 16; ++k)
+                if (i + j < 2) {
+                  mma(acc, ad[i] + desc_step<kOuterA>(k), bd[j] + desc_step<kOuterB>(k), idesc, more);
+                  more = true;
+                }
         }
       };
       using Yes = std::true_type;
