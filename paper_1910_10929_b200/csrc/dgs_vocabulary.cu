@@ -707,6 +707,7 @@ __global__ void __launch_bounds__(256) k_head_words(const __grid_constant__ Head
   for (uint64_t u = uint64_t(blockIdx.x) * 8 + threadIdx.x / 32; u < units; u += uint64_t(gridDim.x) * 8) {
     const uint32_t word = units >> 32 ? uint32_t(u / spans) : uint32_t(u) / spans, col0 = uint32_t(u - uint64_t(word) * spans) * kSpan;
     float v[8] = {};
+#pragma unroll 4
     for (uint32_t s = 0; s < a.dw.splits; ++s)
 #pragma unroll
       for (uint32_t i = 0; i < 8; ++i) {
@@ -724,7 +725,26 @@ __global__ void __launch_bounds__(256) k_head_words(const __grid_constant__ Head
     }
   }
 }
-// dh from its partial results, likewise.
+// dh from many partial results: 32 columns of a row a CTA, each eighth part a warp.  (128 x 768 of 32 parts: 38 us if a warp adds up all of them for 256 columns.)
+constexpr uint32_t kManyParts = 6;
+template <class T>
+__global__ void __launch_bounds__(256) k_head_join(const __grid_constant__ Head a, const float* parts, uint32_t count, T* dh, uint64_t stride, uint32_t spans) {
+  __shared__ float s_sum[8][32];
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, row = blockIdx.x / spans, c = (blockIdx.x - row * spans) * 32 + lane;
+  const uint64_t each = uint64_t(a.rows) * a.width;
+  wait_for_last_kernel();
+  float v = 0.0f;
+  if (c < a.width)
+#pragma unroll 8
+    for (uint32_t p = warp; p < count; p += 8) v += parts[p * each + uint64_t(row) * a.width + c];
+  s_sum[warp][lane] = v;
+  __syncthreads();
+  if (warp || c >= a.width) return;
+  for (uint32_t q = 1; q < 8; ++q) v += s_sum[q][lane];
+  if (a.most_w) v = v * down_of(a.most_w[c]) * down_of(*a.most_g);   // NULL: the parts are what they stand for
+  dh[row * stride + c] = Elem<T>::put(target_of(a, row, false) >= 0 ? v : 0.0f);   // also where W holds infinities
+}
+// And from few, likewise a warp for 256 columns.
 template <class T>
 __global__ void __launch_bounds__(256) k_head_hidden(const __grid_constant__ Head a, const float* parts, T* dh, uint64_t stride, uint32_t spans) {
   wait_for_last_kernel();
@@ -1126,8 +1146,9 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
       else
         k_few_grad<T, vec.value, together.value, 32><<<p.few_ctas, kFewThreads<32>, 0, st>>>(a, f, dw, parts);
       if (cudaGetLastError() != cudaSuccess) return int(DGS_ECUDA);
-      const EarlyLaunch l(dim3(ceil_div(a.width, 32), a.rows), 256, 0, st);
-      return cudaLaunchKernelEx(&l.cfg, k_few_hidden<T>, a, static_cast<const float*>(parts), p.few_ctas, static_cast<T*>(dhidden->data), dhidden->stride) == cudaSuccess
+      const uint32_t spans = ceil_div(a.width, 32);
+      const EarlyLaunch l(dim3(spans * a.rows), 256, 0, st);
+      return cudaLaunchKernelEx(&l.cfg, k_head_join<T>, a, static_cast<const float*>(parts), p.few_ctas, static_cast<T*>(dhidden->data), dhidden->stride, spans) == cudaSuccess
                  ? int(DGS_OK)
                  : int(DGS_ECUDA);
     });
@@ -1217,7 +1238,13 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
   }
   return with_type(hidden->type, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
+    T* const to = static_cast<T*>(dhidden->data);
+    if (a.dh.splits >= kManyParts) {
+      const uint32_t spans = ceil_div(d, 32);
+      const EarlyLaunch l(dim3(spans * a.rows), 256, 0, st);
+      return cudaLaunchKernelEx(&l.cfg, k_head_join<T>, a, static_cast<const float*>(part_h), a.dh.splits, to, dhidden->stride, spans) == cudaSuccess ? int(DGS_OK) : int(DGS_ECUDA);
+    }
     const EarlyLaunch l(dim3(uint32_t(std::min<uint64_t>((n * h.spans + 7) / 8, kSms * 16))), 256, 0, st);
-    return cudaLaunchKernelEx(&l.cfg, k_head_hidden<T>, a, static_cast<const float*>(part_h), static_cast<T*>(dhidden->data), dhidden->stride, h.spans) == cudaSuccess ? int(DGS_OK) : int(DGS_ECUDA);
+    return cudaLaunchKernelEx(&l.cfg, k_head_hidden<T>, a, static_cast<const float*>(part_h), to, dhidden->stride, h.spans) == cudaSuccess ? int(DGS_OK) : int(DGS_ECUDA);
   });
 }

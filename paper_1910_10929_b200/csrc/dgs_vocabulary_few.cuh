@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(256) k_few_rows(const __grid_constant__ Head a
   finish_row(a, row, v, loss, lse);
 }
 
-// dW of the words and, in `parts` [CTAs][rows][width], each CTA's part of dh.
+// dW of the words and, in `parts` [CTAs][rows][width], each CTA's part of dh, which k_head_join adds up.
 template <uint32_t TW> constexpr uint32_t kFewThreads = TW == 8 ? 512 : 256;
 template <class T, bool VEC, uint32_t RB, uint32_t TW>
 __global__ void __launch_bounds__(kFewThreads<TW>, TW == 8 ? 1 : 2) k_few_grad(const __grid_constant__ Head a, const __grid_constant__ Few f, float* dw, float* parts) {
@@ -192,23 +192,5 @@ __global__ void __launch_bounds__(kFewThreads<TW>, TW == 8 ? 1 : 2) k_few_grad(c
     __syncthreads();
   }
 }
-// dh: 32 columns of a row a CTA, each eighth part a warp.
-template <class T>
-__global__ void __launch_bounds__(256) k_few_hidden(const __grid_constant__ Head a, const float* parts, uint32_t count, T* dh, uint64_t stride) {
-  __shared__ float s_sum[8][32];
-  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, c = blockIdx.x * 32 + lane, row = blockIdx.y;
-  const uint64_t each = uint64_t(a.rows) * a.width;
-  wait_for_last_kernel();
-  float v = 0.0f;
-  if (c < a.width)
-#pragma unroll 8
-    for (uint32_t p = warp; p < count; p += 8) v += parts[p * each + uint64_t(row) * a.width + c];
-  s_sum[warp][lane] = v;
-  __syncthreads();
-  if (warp || c >= a.width) return;
-  for (uint32_t q = 1; q < 8; ++q) v += s_sum[q][lane];
-  dh[row * stride + c] = Elem<T>::put(target_of(a, row, false) >= 0 ? v : 0.0f);   // also where W holds infinities
-}
-
 }  // namespace
 }  // namespace dgs
