@@ -303,7 +303,7 @@ def _rows_like(out: Optional[torch.Tensor], m: "dgs.dgs_matrix", rows: int, like
     """(out, its matrix): `rows` rows of m's columns and type, a new tensor if there is none."""
     cols, kind = m.cols, m.type
     if out is None:
-        out = torch.empty((rows, cols), dtype=like.dtype, device=like.device)
+        out = like.new_empty(rows, cols)                # 1 us less than torch.empty
         return out, dgs.dgs_matrix(out.data_ptr(), rows, cols, cols, kind)
     mo = _matrix(out, "out")
     _fit(mo, "out", rows, cols, kind)
@@ -362,11 +362,12 @@ def combine_experts_grad(dout: torch.Tensor, y: torch.Tensor, weight: torch.Tens
     slots = m.rows * k
     _fit(my, "y", slots, m.cols, m.type)
     _same_device(device, y)
+    _on_gpu(weight, "weight")
     pw = _plain(weight, "weight", torch.float32, slots, device)
     po = _plain(order, "order", torch.int32, slots, device)
     pp = _plain(place, "place", torch.int32, slots, device)
     out, mo = _rows_like(out, m, slots, dout)
-    dweight = torch.empty(place.shape, dtype=torch.float32, device=device)
+    dweight = weight.new_empty(place.shape)
     _run(device, "dgs_experts_combine_grad", m, my, pw, po, pp, k, mo, dweight.data_ptr())
     return out, dweight
 
@@ -408,7 +409,7 @@ def vocabulary_loss(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Te
     _cut_off(weight, "weight", "vocabulary_loss")
     device = hidden.device
     need = _workspace(False, mh, mw)
-    loss, lse = torch.empty((2, *target.shape), dtype=torch.float32, device=device).unbind()
+    loss, lse = torch.empty(2, *target.shape, dtype=torch.float32, device=device).unbind()
     work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     _run(device, "dgs_vocabulary_loss", mh, mw, pt, flags, loss.data_ptr(), lse.data_ptr(), work.data_ptr() if need else 0, need)
     return VocabularyLoss(loss, lse)
@@ -431,7 +432,7 @@ def vocabulary_loss_grad(hidden: torch.Tensor, weight: torch.Tensor, target: tor
     pg = _plain(dloss, "dloss", torch.float32, 1 if one else rows, device)
     pw = _plain(dw, "dw", torch.float32, mw.rows * mw.cols, device)
     if out is None:
-        out = torch.empty(hidden.shape, dtype=hidden.dtype, device=device)
+        out = hidden.new_empty(hidden.shape)
         mo = dgs.dgs_matrix(out.data_ptr(), rows, mh.cols, mh.cols, mh.type)
     else:
         mo = _matrix(out, "out")
