@@ -136,6 +136,10 @@ def test_long_sums_pieces_and_splits(rows, width, words, dtype):
     check_loss(hidden, table, target, got)
     dh, dw = grad(hidden, table, target, got.lse, dloss)
     check_grad(hidden, table, target, got.lse, dloss, dh, dw)
+    before = torch.randn(words, width, device=DEV) / rows         # what an earlier part of the batch has left
+    again, added = grad(hidden, table, target, got.lse, dloss, before)
+    assert torch.equal(again, dh)
+    check_grad(hidden, table, target, got.lse, dloss, again, added, before)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
