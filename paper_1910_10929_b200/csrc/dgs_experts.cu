@@ -50,11 +50,11 @@ __global__ void __launch_bounds__(256) k_experts_gather(const __grid_constant__ 
 }
 
 // out[t] = sum over j of weight[t][j] y[place[t][j]], slots ascending, in f32.  weight NULL: 1, which is the gather's gradient.  Bound by HBM: the
-// rows of four slots (two in f32) are on their way together, in 48 warps an SM (eight slots in 24 warps: 32768 x 2048, top 8 237 us, 187 so; 48 warps that go on to the next
+// rows of four slots (two in f32 and of rows that begin anywhere) are on their way together, in 48 warps an SM (eight slots in 24 warps: 32768 x 2048, top 8 237 us, 187 so; 48 warps that go on to the next
 // token 212).
 template <class T, bool VEC>
-__global__ void __launch_bounds__(256, VEC ? 6 : 3) k_experts_combine(const __grid_constant__ Rows a, const float* weight, const T* y, T* out) {
-  constexpr uint32_t J = sizeof(T) == 2 ? 4 : 2;
+__global__ void __launch_bounds__(256, 6) k_experts_combine(const __grid_constant__ Rows a, const float* weight, const T* y, T* out) {
+  constexpr uint32_t J = VEC && sizeof(T) == 2 ? 4 : 2;
   const uint32_t lane = threadIdx.x % 32;
   const uint64_t units = uint64_t(a.tokens) * a.chunks, step = uint64_t(gridDim.x) * 8;
   for (uint64_t u = uint64_t(blockIdx.x) * 8 + threadIdx.x / 32; u < units; u += step) {
@@ -88,10 +88,11 @@ __global__ void __launch_bounds__(256, VEC ? 6 : 3) k_experts_combine(const __gr
 }
 
 // dy[place[t][j]] = weight[t][j] dout[t] and dweight[t][j] = <dout[t], y[place[t][j]]>.  `warps` warps share a token's columns; their parts of the
-// products are added in their order.  Bound by HBM: a token's dout is read once for eight slots.
+// products are added in their order.  Bound by HBM: a token's dout is read once for eight slots (four in f32; two of rows that begin anywhere, in 40 warps an SM for 16 bits:
+// 16384 x 767 with top 8 114 us, 172 with eight slots in 16 warps; words put together from two, which need fewer loads: 272).
 template <class T, bool VEC>
-__global__ void __launch_bounds__(256, VEC ? 3 : 2) k_experts_combine_grad(const __grid_constant__ Rows a, const float* weight, const T* dout, const T* y, T* dy, float* dweight) {
-  constexpr uint32_t J = sizeof(T) == 2 ? 8 : 4;
+__global__ void __launch_bounds__(256, VEC || sizeof(T) == 4 ? 3 : 5) k_experts_combine_grad(const __grid_constant__ Rows a, const float* weight, const T* dout, const T* y, T* dy, float* dweight) {
+  constexpr uint32_t J = !VEC ? 2 : sizeof(T) == 2 ? 8 : 4;
   __shared__ float s_part[8][J];
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, part = warp % a.warps, each = 8 / a.warps;
   const uint32_t rounds = (a.tokens + gridDim.x * each - 1) / (gridDim.x * each);
