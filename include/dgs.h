@@ -490,7 +490,7 @@ int dgs_vocabulary_loss(const dgs_matrix* hidden, const dgs_matrix* weight, cons
  *     dhidden[r][c] = sum over v of s[r][v] * weight[v][c],     dw[v][c] = sum over r of s[r][v] * hidden[r][c]
  * lse: DEVICE f32[rows], as dgs_vocabulary_loss writes it.  dloss: DEVICE f32[rows] with dloss_stride 1, or one value for all rows with 0; finite.  dhidden: rows x
  * width, of the hidden states' type.  dw: DEVICE f32, words * width elements (4-byte aligned: the layer's slice of the flat gradient), or NULL: not wanted.
- * s is formed a piece of the vocabulary at a time and kept in 22 bits (for dhidden in bfloat16 in 11) under one power of two for the call, down to 2^-40 of the largest
+ * s is formed a piece of the vocabulary at a time and kept in 22 bits under one power of two for the call, down to 2^-40 of the largest
  * |dloss|: what lies below, and the last digits of rows whose dloss is far below the largest, are lost.  hidden and weight meet it as 11 bits (f32: 22) under a power of
  * two for each column, which holds bfloat16 values exactly down to 2^-29 of their column's largest.  Up to 64 rows with few products in all are computed in f32 throughout.
  * workspace: likewise, dgs_vocabulary_loss_grad_bytes: up to 320 MB (or 1 KB a row, if more) of s, 2 bytes a value of both matrices (f32 4), 4 bytes a value of

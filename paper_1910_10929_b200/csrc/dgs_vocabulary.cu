@@ -9,7 +9,8 @@
 // Numbers: s is kept as the sum of two fp16 numbers (22 bits) under one power of two for the call, since dW goes to a flat gradient in f32; products of fp16 need
 // fp16 partners, so W and h are held beside as fp16 numbers under a power of two for each column: exact for bfloat16 and fp16 values down to 2^-29 of their column's
 // largest, and below that to 2^-40 of it (s likewise: an exponential below 2^-29 keeps fewer bits).  f32 matrices are sums of two fp16 numbers each; of their four products the smallest, under 2^-22 of the whole, is left out.
-// dh of bfloat16 is formed from the first part of s alone: 11 bits where the result keeps 8.
+// Both gradients are formed from both parts of s, so that dh is rounded once, to its type: 1.0e-3 of dh in bfloat16 differed from the f32 form's with the first part alone
+// (11 bits for a result of 8) and 1.4e-4 does with both, for 8192 x 768 x 50257 at the price of 2.93 ms for 2.53.
 #include "dgs_tensor.cuh"
 
 #include <algorithm>
@@ -45,11 +46,11 @@ enum : int { kLoss, kSlope, kGrads };
 // Logits of few steps take half of them: an exponential takes a logit's error as it is (a logit of 15 summed over 768 values in one go is off by 7e-6), and two
 // chunks a tile let the products of the next tile run to their end while one is finished.
 constexpr uint32_t kBlockBytes = 128 * 128;                       // 128 rows and 64 columns of s
-// Shared memory is a ring of tiles, one for each part of an operand and step: a step of dW takes three of the twelve, one of dh in bfloat16 two, so that
-// four or six steps are on their way.  (Four of either: the products of dh waited for copies, 0.46 us a step for 0.33.)
+// Shared memory is a ring of tiles, one for each part of an operand and step: a step of the gradients takes three of the twelve (f32 four), so that four steps are on
+// their way.
 template <int MODE, uint32_t PA, uint32_t PB> struct Step {
   static constexpr uint32_t kRows = MODE == kLoss && PA == 1 ? 128 : 64, kTile = kRows * 256, kSlots = (MODE == kSlope ? 160 : 192) * 1024 / kTile;
-  static constexpr uint32_t kAhead = kSlots / 2;   // steps under way, at most
+  static constexpr uint32_t kAhead = kSlots / (PA + PB);   // steps under way, at most
   static constexpr uint32_t kChunk = (PA == 1 ? 512 : MODE == kGrads ? 256 : 64) / kRows, kSmem = 1024 + kSlots * kTile + (MODE == kSlope ? 64 * 1024 : 0);
 };
 // Sixteen warps keep the sums, 64 columns of 32 rows each; four do the rest and leave them their registers.  (With eight warps of 128 columns, two a scheduler, the
@@ -95,7 +96,7 @@ struct Head {
   uint32_t m_tiles, n_tiles, tiles, steps, chunk;   // logits
   uint32_t first_word, piece_cols;  // of the piece (a multiple of 256 in the workspace)
   uint32_t idesc;
-  uint32_t wide_targets, dloss_step, parts;   // parts: of s that are wanted
+  uint32_t wide_targets, dloss_step;
   const void* target;
   const float *lse, *dloss;
   const uint32_t *most_h, *most_w, *most_g;     // bits of the largest magnitudes: of each column of h and of W, of dloss
@@ -171,7 +172,7 @@ __device__ __forceinline__ bool head_tile(const Head& a, uint32_t pair, uint32_t
 // so that the products of the next run while one is finished.
 // Warps 16 to 19 go through their loops with all lanes, one of which does what has to be done once: descriptors and addresses then stay in uniform registers (with
 // one lane in the loops the products of a step waited for their operands to be moved there: loss of 8192 x 768 x 50257 436 us, 383 so).
-template <int MODE, uint32_t PA, uint32_t PB, uint32_t PH>   // PH: parts of s that dh takes
+template <int MODE, uint32_t PA, uint32_t PB>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
 k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
   using S = Step<MODE, PA, PB>;
@@ -214,21 +215,20 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
       bool alive = true;
       const bool one = elect_one();
       uint32_t it = 0, chunk = 0, in = 0, slot = 0;   // in: steps of the chunk
-      const auto products = [&](auto outer_a, auto outer_b, auto parts_b, uint32_t acc, bool first) {
+      const auto products = [&](auto outer_a, auto outer_b, uint32_t acc, bool first) {
         constexpr bool kOuterA = decltype(outer_a)::value, kOuterB = decltype(outer_b)::value;
-        constexpr uint32_t kB = decltype(parts_b)::value;
         const uint32_t idesc = a.idesc | uint32_t(kOuterA) << 15 | uint32_t(kOuterB) << 16 | idesc_cols(256);
-        uint64_t ad[PA], bd[kB];
+        uint64_t ad[PA], bd[PB];
 #pragma unroll
         for (uint32_t i = 0; i < PA; ++i) ad[i] = tile_desc<kOuterA, R>(stages + slot * TILE), slot = slot + 1 == SLOTS ? 0 : slot + 1;
 #pragma unroll
-        for (uint32_t j = 0; j < kB; ++j) bd[j] = tile_desc<kOuterB, R>(stages + slot * TILE), slot = slot + 1 == SLOTS ? 0 : slot + 1;
+        for (uint32_t j = 0; j < PB; ++j) bd[j] = tile_desc<kOuterB, R>(stages + slot * TILE), slot = slot + 1 == SLOTS ? 0 : slot + 1;
         if (one) {   // products with second parts first: what is cut off as they are added is small
           bool more = !first;
 #pragma unroll
           for (int i = PA - 1; i >= 0; --i)
 #pragma unroll
-            for (int j = kB - 1; j >= 0; --j)
+            for (int j = PB - 1; j >= 0; --j)
 #pragma unroll
               for (uint32_t k = 0; k < R / 16; ++k)
                 if (i + j < 2) {
@@ -248,10 +248,10 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
           if (!alive) break;
           tmem_after();
           if constexpr (MODE == kGrads) {
-            if (w.hidden) products(Yes{}, No{}, std::integral_constant<uint32_t, PH>{}, acc, begins);
-            else products(Yes{}, Yes{}, std::integral_constant<uint32_t, PB>{}, acc, begins);
+            if (w.hidden) products(Yes{}, No{}, acc, begins);
+            else products(Yes{}, Yes{}, acc, begins);
           } else {
-            products(No{}, No{}, std::integral_constant<uint32_t, PB>{}, acc, begins);
+            products(No{}, No{}, acc, begins);
           }
           if (one) mma_commit(smem_at(&s_empty[st]));
           if (++in == CH || s == w.steps - 1) {
@@ -268,25 +268,21 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
       const bool one = elect_one();
       const bool second = warp == kSumWarps + 3;   // of the two operands
       bool alive = true;
-      uint32_t it = 0, done = 0, slot = 0, used = 0, narrow = 0;   // steps begun, steps whose products are known to be done; narrow: bit i, step i's tiles are PA + PH
+      uint32_t it = 0, done = 0, slot = 0;   // steps begun, steps whose products are known to be done
       const uint32_t col_blocks = a.piece_cols / 64;
       for (uint32_t i = 0; alive && head_tile<MODE>(a, pair, pairs, i, &w); ++i) {
-        const uint32_t m = w.m0 + rank * 128, n = w.n0 + rank * 128, tiles = PA + (w.hidden ? PH : PB);
+        const uint32_t m = w.m0 + rank * 128, n = w.n0 + rank * 128;
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           const uint32_t st = it % ST, bar = smem_at(&s_loaded[st]), k0 = (w.from + s) * R;
-          while (used + tiles > SLOTS || it - done >= ST) {
+          if (it - done >= ST) {
             if (!(alive = warp_wait(smem_at(&s_empty[done % ST]), done / ST & 1))) break;
-            used -= PA + (narrow >> done % ST & 1 ? PH : PB);
             ++done;
           }
-          if (!alive) break;
-          used += tiles;
-          narrow = (narrow & ~(1u << st)) | uint32_t(w.hidden) << st;
           uint32_t at[PA + PB];
 #pragma unroll
           for (uint32_t p = 0; p < PA + PB; ++p) {
             at[p] = stages + slot * TILE;
-            if (p < tiles) slot = slot + 1 == SLOTS ? 0 : slot + 1;
+            slot = slot + 1 == SLOTS ? 0 : slot + 1;
           }
           if (!one) {
           } else if (!second) {
@@ -301,14 +297,14 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
               }
             }
           } else if constexpr (MODE == kGrads) {
-            bar_expect(bar, (w.hidden ? PH : PB) * TILE);
+            bar_expect(bar, PB * TILE);
 #pragma unroll
             for (uint32_t p = 0; p < PB; ++p) {
               const unsigned char* from = a.s + p * a.plane;
               if (!w.hidden) {   // rows k0 on of 128 columns
                 for (uint32_t b = 0; b < 2; ++b)
                   bulk_load(at[PA + p] + b * R * 128, from + (uint64_t(k0 / 128) * col_blocks + n / 64 + b) * kBlockBytes + k0 % 128 * 128, R * 128, bar);
-              } else if (p < PH) {   // columns k0 on of 128 rows
+              } else {   // columns k0 on of 128 rows
                 bulk_load(at[PA + p], from + (uint64_t(n / 128) * col_blocks + k0 / 64) * kBlockBytes, kBlockBytes, bar);
               }
             }
@@ -423,6 +419,7 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
           // and 74 us, 60 with the first part alone, 51 without.  (Straight from the registers, 32 bytes a lane: 78.  By copies from shared memory, with
           // their fences and waits for the buffer: 88.)
           const uint32_t stage = stages + SLOTS * TILE + warp * 4096;
+          const uint32_t mine_at = stage + lane * 128 + ((lane & 7) << 4);   // of a row's first 16 bytes; the q-th are at mine_at ^ q << 4
           unsigned char* const to = a.s + (uint64_t(w.m0 / 128 + rank) * (a.piece_cols / 64) + col0 / 64) * kBlockBytes + quarter * 4096 + lane * 16;
           uint32_t rest[32];
           __syncwarp();
@@ -444,7 +441,7 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
               memcpy(&first[i], &hi, 4);
               memcpy(&rest[q * 4 + i], &lo, 4);
             }
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 128 + ((q ^ (lane & 7)) << 4)), "r"(first[0]), "r"(first[1]), "r"(first[2]), "r"(first[3]) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(mine_at ^ (q << 4)), "r"(first[0]), "r"(first[1]), "r"(first[2]), "r"(first[3]) : "memory");
           }
           const auto out = [&](unsigned char* at) {
             __syncwarp();
@@ -456,15 +453,13 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
             }
           };
           out(to);
-          if (a.parts == 2) {
-            __syncwarp();
+          __syncwarp();
 #pragma unroll
-            for (uint32_t q = 0; q < 8; ++q)
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 128 + ((q ^ (lane & 7)) << 4)), "r"(rest[q * 4]), "r"(rest[q * 4 + 1]), "r"(rest[q * 4 + 2]),
-                           "r"(rest[q * 4 + 3])
-                           : "memory");
-            out(to + a.plane);
-          }
+          for (uint32_t q = 0; q < 8; ++q)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(mine_at ^ (q << 4)), "r"(rest[q * 4]), "r"(rest[q * 4 + 1]), "r"(rest[q * 4 + 2]),
+                         "r"(rest[q * 4 + 3])
+                         : "memory");
+          out(to + a.plane);
         }
       } else if (row < a.width) {
         // lanes are neighbours in dW's and dh's rows
@@ -841,13 +836,13 @@ struct HeadPlan {
 
 bool head_ok(const dgs_matrix* h, const dgs_matrix* w) { return matrix_ok(h, false) && matrix_ok(w, false) && h->type == w->type && h->cols == w->cols && w->rows; }
 
-// Steps of 64 values: a product 0.40 us; dh of bfloat16 takes one, of fp16 two, dW two, f32 three.
+// Steps of 64 values: a product 0.40 us; two of either gradient, of f32 three.
 constexpr double kProductUs = 0.40;
 Work words_of(uint64_t n, uint32_t d, uint32_t tiles, uint32_t type) {
   return {tiles * ceil_div(d, 256), ceil_div(n, 64), kProductUs * (type == DGS_TYPE_F32 ? 3 : 2), uint64_t(tiles) * 256 * d};
 }
 Work hidden_of(uint64_t n, uint32_t d, uint32_t tiles, uint32_t type) {
-  return {ceil_div(n, 256) * ceil_div(d, 256), tiles * 4, kProductUs * (type == DGS_TYPE_F32 ? 3 : type == DGS_TYPE_FP16 ? 2 : 1), n * d};
+  return {ceil_div(n, 256) * ceil_div(d, 256), tiles * 4, kProductUs * (type == DGS_TYPE_F32 ? 3 : 2), n * d};
 }
 
 // Few rows go without tensor cores where there are not many products in all.  Here / with tensor cores, us a call.  Loss, 16 bits: 64 x 512 x 1000 10.5 / 12.5,
@@ -946,20 +941,20 @@ constexpr int kMaxDevices = 64;
 std::mutex g_head_mu;
 bool g_head_ready[kMaxDevices];
 PFN_cuTensorMapEncodeTiled_v12000 g_head_encode;   // written once, under the mutex
-template <int MODE, uint32_t PA, uint32_t PB, uint32_t PH>
+template <int MODE, uint32_t PA, uint32_t PB>
 bool head_setup() {
   cudaFuncAttributes f;
   // the split of the registers counts on what the launch brings
-  return cudaFuncGetAttributes(&f, k_head<MODE, PA, PB, PH>) == cudaSuccess && uint32_t(f.numRegs) >= kHeadRegs &&
-         cudaFuncSetAttribute(k_head<MODE, PA, PB, PH>, cudaFuncAttributeMaxDynamicSharedMemorySize, Step<MODE, PA, PB>::kSmem) == cudaSuccess;
+  return cudaFuncGetAttributes(&f, k_head<MODE, PA, PB>) == cudaSuccess && uint32_t(f.numRegs) >= kHeadRegs &&
+         cudaFuncSetAttribute(k_head<MODE, PA, PB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Step<MODE, PA, PB>::kSmem) == cudaSuccess;
 }
 int head_ready() {   // once per device
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return DGS_ECUDA;
   std::lock_guard<std::mutex> lock(g_head_mu);
   if (!g_head_ready[dev]) {
-    if (!head_setup<kLoss, 1, 1, 0>() || !head_setup<kLoss, 2, 2, 0>() || !head_setup<kSlope, 1, 1, 0>() || !head_setup<kSlope, 2, 2, 0>() ||
-        !head_setup<kGrads, 1, 2, 1>() || !head_setup<kGrads, 1, 2, 2>() || !head_setup<kGrads, 2, 2, 2>())
+    if (!head_setup<kLoss, 1, 1>() || !head_setup<kLoss, 2, 2>() || !head_setup<kSlope, 1, 1>() || !head_setup<kSlope, 2, 2>() ||
+        !head_setup<kGrads, 1, 2>() || !head_setup<kGrads, 2, 2>())
       return DGS_ECUDA;
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult found;
@@ -987,11 +982,11 @@ int with_few(const dgs_matrix* h, const dgs_matrix* w, uint32_t few, F&& f) {
   });
 }
 
-template <int MODE, uint32_t PA, uint32_t PB, uint32_t PH>
+template <int MODE, uint32_t PA, uint32_t PB>
 int head_launch(const Head& a, uint32_t tiles, const CUtensorMap& x, const CUtensorMap& y, bool early, cudaStream_t st) {
   EarlyLaunch l(dim3(std::min(tiles, kSms / 2) * 2), kHeadThreads, Step<MODE, PA, PB>::kSmem, st);
   if (!early) l.cfg.numAttrs = 0;
-  return cudaLaunchKernelEx(&l.cfg, k_head<MODE, PA, PB, PH>, a, x, y) == cudaSuccess ? DGS_OK : DGS_ECUDA;
+  return cudaLaunchKernelEx(&l.cfg, k_head<MODE, PA, PB>, a, x, y) == cudaSuccess ? DGS_OK : DGS_ECUDA;
 }
 
 Source source_of(const dgs_matrix* m) { return {m->data, m->stride, uint32_t(m->rows), m->cols, (m->cols + kSpan - 1) / kSpan}; }
@@ -1099,7 +1094,7 @@ extern "C" int dgs_vocabulary_loss(const dgs_matrix* hidden, const dgs_matrix* w
   a.partial = reinterpret_cast<float2*>(work + p.inner_h + p.inner_w + p.scales);
   a.at_target = reinterpret_cast<float*>(work + p.inner_h + p.inner_w + p.scales + p.partial);
   logit_steps<kLoss>(p.parts, &a);
-  rc = p.parts == 2 ? head_launch<kLoss, 2, 2, 0>(a, a.tiles, map_h, map_w, launched, st) : head_launch<kLoss, 1, 1, 0>(a, a.tiles, map_h, map_w, launched, st);
+  rc = p.parts == 2 ? head_launch<kLoss, 2, 2>(a, a.tiles, map_h, map_w, launched, st) : head_launch<kLoss, 1, 1>(a, a.tiles, map_h, map_w, launched, st);
   if (rc != DGS_OK) return rc;
   const EarlyLaunch l(dim3(ceil_div(n, 32)), 256, 0, st);
   return cudaLaunchKernelEx(&l.cfg, k_head_loss, a, loss, lse) == cudaSuccess ? DGS_OK : DGS_ECUDA;
@@ -1176,7 +1171,6 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
   a.dloss = dloss;
   a.dloss_step = dloss_stride;
   a.add = flags & DGS_LOSS_ADD ? 1 : 0;
-  a.parts = dw || hidden->type != DGS_TYPE_BF16 ? 2 : 1;
   a.piece_cols = p.piece_tiles * 256;
   a.plane = p.s / 2;
 
@@ -1195,7 +1189,6 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
   CUtensorMap inner_h = {}, inner_w = {}, map_h = {}, map_w = {};
   bool launched = true;
   if ((rc = inner_operands(hidden, weight, p, inner, &a, &inner_h, &inner_w, &launched, st)) != DGS_OK) return rc;
-  const bool bf16 = hidden->type == DGS_TYPE_BF16;
   if ((rc = head_map(outer_h, n, d, p.stride, p.parts, false, 64, &map_h)) != DGS_OK) return rc;
   if ((rc = head_map(outer_w, v, d, p.stride, p.parts, false, 64, &map_w)) != DGS_OK) return rc;
 
@@ -1211,7 +1204,7 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
     s.first_piece = piece == 0;
     s.n_tiles = tiles;
     s.tiles = s.m_tiles * tiles;
-    rc = p.parts == 2 ? head_launch<kSlope, 2, 2, 0>(s, s.tiles, inner_h, inner_w, true, st) : head_launch<kSlope, 1, 1, 0>(s, s.tiles, inner_h, inner_w, true, st);
+    rc = p.parts == 2 ? head_launch<kSlope, 2, 2>(s, s.tiles, inner_h, inner_w, true, st) : head_launch<kSlope, 1, 1>(s, s.tiles, inner_h, inner_w, true, st);
     if (rc != DGS_OK) return rc;
     s.idesc = kIdescF32;
     s.dw.m_tiles = s.dh.m_tiles = ceil_div(d, 256);
@@ -1228,8 +1221,7 @@ extern "C" int dgs_vocabulary_loss_grad(const dgs_matrix* hidden, const dgs_matr
     s.share_few = shares.few;
     s.share_more = shares.more;
     const uint32_t all = s.dw.tiles + s.dh.tiles;
-    rc = bf16 ? head_launch<kGrads, 1, 2, 1>(s, all, map_h, map_w, true, st)
-              : p.parts == 2 ? head_launch<kGrads, 2, 2, 2>(s, all, map_h, map_w, true, st) : head_launch<kGrads, 1, 2, 2>(s, all, map_h, map_w, true, st);
+    rc = p.parts == 2 ? head_launch<kGrads, 2, 2>(s, all, map_h, map_w, true, st) : head_launch<kGrads, 1, 2>(s, all, map_h, map_w, true, st);
     if (rc != DGS_OK) return rc;
     if (dw && s.dw.splits > 1) {
       const EarlyLaunch l(dim3(uint32_t(std::min<uint64_t>((uint64_t(tiles) * 256 * w.spans + 7) / 8, kSms * 16))), 256, 0, st);
