@@ -845,7 +845,8 @@ Work hidden_of(uint64_t n, uint32_t d, uint32_t tiles, uint32_t type) {
   return {ceil_div(n, 256) * ceil_div(d, 256), tiles * 4, kProductUs * (type == DGS_TYPE_F32 ? 3 : 2), n * d};
 }
 
-// Few rows go without tensor cores where there are not many products in all.  Here / with tensor cores, us a call.  Loss, 16 bits: 64 x 512 x 1000 10.5 / 12.5,
+// Few rows go without tensor cores where there are not many products in all.  Loss and gradient have borders of their own, so that between them the two form logits in different ways,
+// each within its own roundings of them.  Here / with tensor cores, us a call.  Loss, 16 bits: 64 x 512 x 1000 10.5 / 12.5,
 // 3 x 2048 x 8000 15 / 21, 8 of them 25 / 21, 1 x 768 x 50257 20 / 33, 3 of them 32 / 33, 8 47 / 33; f32: 16 x 2048 x 8000 49 / 64, 37 101 / 64, 16 x 768 x 50257
 // 81 / 102, 37 178 / 102.  Gradient, 16 bits: 37 x 512 x 1000 21 / 35, 64 27 / 37, 1 x 2048 x 8000 85 / 87, 3 of them 97 / 86, 1 x 768 x 50257 182 / 161; f32:
 // 64 x 512 x 1000 25 / 52, 8 x 2048 x 8000 91 / 155, 16 161 / 160, 8 x 768 x 50257 181 / 285, 16 300 / 290.
@@ -1033,13 +1034,16 @@ Head head_of(const dgs_matrix* h, const dgs_matrix* w, const void* target, uint3
 
 Few few_of(const dgs_matrix* h, const dgs_matrix* w, const HeadPlan& p) { return {h->data, w->data, h->stride, w->stride, (h->cols + kSpan - 1) / kSpan, p.few_tiles}; }
 
-template <int MODE>
-void logit_steps(uint32_t parts, Head* a) {
-  using One = Step<MODE, 1, 1>;
-  using Two = Step<MODE, 2, 2>;
-  a->steps = ceil_div(a->width, parts == 2 ? Two::kRows : One::kRows);
-  a->chunk = std::min(ceil_div(a->steps, 2), parts == 2 ? Two::kChunk : One::kChunk);
+// Loss and gradient sum a logit the same way, bit by bit: the values of a chunk are a whole number of either's steps, and are counted in the loss', the longer ones.
+template <int MODE, uint32_t P>
+void logit_chunks(Head* a) {
+  constexpr uint32_t kMine = Step<MODE, P, P>::kRows, kLong = Step<kLoss, P, P>::kRows;
+  static_assert(kLong % kMine == 0 && Step<MODE, P, P>::kChunk * kMine == Step<kLoss, P, P>::kChunk * kLong, "the same values in loss and gradient");
+  a->steps = ceil_div(a->width, kMine);
+  a->chunk = std::min(ceil_div(ceil_div(a->width, kLong), 2), Step<kLoss, P, P>::kChunk) * (kLong / kMine);
 }
+template <int MODE>
+void logit_steps(uint32_t parts, Head* a) { parts == 2 ? logit_chunks<MODE, 2>(a) : logit_chunks<MODE, 1>(a); }
 
 }  // namespace
 }  // namespace dgs
