@@ -477,8 +477,8 @@ enum { DGS_TARGET_I64 = 1u << 0, /* targets are i64, 8-byte aligned; without it 
  *     lse[r] = log(sum over words v of exp z[r][v]),     loss[r] = lse[r] - z[r][target[r]]
  * hidden: rows x width, weight: words x width (one row a word, one at least), of one type.  target: DEVICE i32 or i64 [rows]; a row whose target is below 0 is
  * ignored: its loss is 0 (its lse is that of whatever the row holds).  A target past the last word is treated so and reported.  loss, lse: DEVICE f32[rows]; lse is
- * what the gradient takes.  Products of 16-bit types are exact, f32 values are taken as 22 bits under a power of two for each row; sums are in f32.  A row whose
- * logits hold a NaN or +inf has NaN for both.
+ * what the gradient takes.  Products of 16-bit types are exact, f32 values are taken as 22 bits under a power of two for each row, down to 2^-39
+ * of its largest (less counts as 0); sums are in f32.  A row whose logits hold a NaN or +inf has NaN for both; a word whose logit is -inf has no part in the row.
  * workspace: DEVICE, 256-byte aligned, at least what dgs_vocabulary_loss_bytes says for these arguments (data pointers included: their alignment counts).  It takes
  * 8 bytes for each row and 64 words, and copies of f32 matrices (4 bytes a value) and of those whose rows do not begin on 16 bytes (2 bytes).
  * width at most 2^24, rows and words 2^30, rows or words times width 2^38, else DGS_ELIMIT. */
@@ -490,6 +490,7 @@ int dgs_vocabulary_loss(const dgs_matrix* hidden, const dgs_matrix* weight, cons
  *     dhidden[r][c] = sum over v of s[r][v] * weight[v][c],     dw[v][c] = sum over r of s[r][v] * hidden[r][c]
  * lse: DEVICE f32[rows], as dgs_vocabulary_loss writes it.  dloss: DEVICE f32[rows] with dloss_stride 1, or one value for all rows with 0; finite.  dhidden: rows x
  * width, of the hidden states' type.  dw: DEVICE f32, words * width elements (4-byte aligned: the layer's slice of the flat gradient), or NULL: not wanted.
+ * An infinity in hidden or weight leaves its column of dhidden or dw infinite or NaN in whatever meets it.
  * s is formed a piece of the vocabulary at a time and kept in 22 bits under one power of two for the call, down to 2^-40 of the largest
  * |dloss|: what lies below, and the last digits of rows whose dloss is far below the largest, are lost.  hidden and weight meet it as 11 bits (f32: 22) under a power of
  * two for each column, which holds bfloat16 values exactly down to 2^-29 of their column's largest.  Up to 64 rows with few products in all are computed in f32 throughout.

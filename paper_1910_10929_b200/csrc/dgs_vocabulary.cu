@@ -502,7 +502,12 @@ struct Source {
   uint32_t rows, cols, spans;
 };
 
-// The bits of the largest magnitude of each column (of rows that are not ignored, where `rows` says which), and of dloss.
+// A magnitude's bits where it is finite: infinities and NaN have no say in the power of two that the numbers beside them are multiplied with.
+__device__ __forceinline__ uint32_t finite_bits(float v) {
+  const uint32_t m = __float_as_uint(v) & 0x7fffffffu;
+  return m < 0x7f800000u ? m : 0;
+}
+// The bits of the largest finite magnitude of each column (of rows that are not ignored, where `rows` says which), and of dloss.
 constexpr uint32_t kMostRows = 64;   // of a CTA
 template <class T, bool VEC>
 __device__ __forceinline__ void columns_most(const Head& a, const Source& m, bool targets, uint32_t block, uint32_t* most) {
@@ -514,13 +519,13 @@ __device__ __forceinline__ void columns_most(const Head& a, const Source& m, boo
     for (uint32_t r = row0 + warp; r < min(row0 + kMostRows, m.rows); r += 8) {
       Eight<T> e;
       load8<T, VEC, true, decltype(whole)::value>(static_cast<const T*>(m.data) + r * m.stride, col0, lane, m.cols, e);
-      const uint32_t all = !targets || target_of(a, r, false) >= 0 ? 0x7fffffffu : 0;
+      const uint32_t all = !targets || target_of(a, r, false) >= 0 ? ~0u : 0;
       float2 v[4];
       floats_of(e, v);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        best[2 * i] = max(best[2 * i], __float_as_uint(v[i].x) & all);
-        best[2 * i + 1] = max(best[2 * i + 1], __float_as_uint(v[i].y) & all);
+        best[2 * i] = max(best[2 * i], finite_bits(v[i].x) & all);
+        best[2 * i + 1] = max(best[2 * i + 1], finite_bits(v[i].y) & all);
       }
     }
   };
@@ -551,9 +556,14 @@ __global__ void __launch_bounds__(256) k_head_most(const __grid_constant__ Head 
   }
 }
 
+// The sum of two fp16 numbers.  An infinity is the second alone: it meets first parts only (the product of second parts is left out), so that its sign and whether it
+// meets a zero are the formula's.  As a first part it would meet second parts, which may be 0 or of the other sign.
+__device__ __forceinline__ float unless_infinite(float v) { return fabsf(v) == __builtin_huge_valf() ? 0.0f : v; }
 __device__ __forceinline__ void halves(const float2 (&v)[4], Eight<__half>& hi, Eight<__half>& lo) {
   float2 rest[4];
-  of_floats(v, hi);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) rest[i] = make_float2(unless_infinite(v[i].x), unless_infinite(v[i].y));
+  of_floats(rest, hi);
   floats_of(hi, rest);
 #pragma unroll
   for (int i = 0; i < 4; ++i) rest[i] = make_float2(v[i].x - rest[i].x, v[i].y - rest[i].y);
@@ -584,7 +594,8 @@ __device__ __forceinline__ void by_columns(const Head& a, const Source& m, bool 
         floats_of(e, v);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], up[i]);
-        halves(v, part[0], part[1]);
+        if constexpr (P == 2) halves(v, part[0], part[1]);
+        else of_floats(v, part[0]);
       }
 #pragma unroll
       for (uint32_t p = 0; p < P; ++p) store8<__half, VEC, kWhole>(out + (uint64_t(p) * m.rows + r) * stride, col0, lane, m.cols, part[p]);
@@ -620,7 +631,7 @@ __device__ __forceinline__ void by_rows(const Source& m, uint64_t r, void* out, 
     }
   } else {
     uint32_t most = 0;
-    for (uint32_t c = lane; c < m.cols; c += 32) most = max(most, __float_as_uint(row[c]) & 0x7fffffffu);
+    for (uint32_t c = lane; c < m.cols; c += 32) most = max(most, finite_bits(row[c]));
     most = __reduce_max_sync(0xffffffffu, most);
     const float up = up_of(most);
     for (uint32_t s = 0; s < m.spans; ++s) {
