@@ -30,7 +30,8 @@ __device__ __forceinline__ void bulk_load(uint32_t to, const void* from, uint32_
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar)
                : "memory");
 }
-// *to += v, without waiting for what is there.  The only thread that adds to it in this kernel, so the sum's order is that of the kernels.
+// *to += v, without waiting for what is there.  The only thread that adds to it in this kernel, so the sum's order is that of the kernels.  This addition takes subnormal numbers
+// for 0, so it is for sums of products that still stand under their powers of two, multiples of 2^-48, and not for the caller's numbers.
 __device__ __forceinline__ void add_behind(float* to, float v) { asm volatile("red.global.add.f32 [%0], %1;" ::"l"(to), "f"(v) : "memory"); }
 
 // What the kernel forms: maxima and sums of logits; s of a piece; the products of a piece's s with h (dW) and with W (dh's part).
@@ -463,7 +464,7 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
         }
       } else if (row < a.width) {
         // lanes are neighbours in dW's and dh's rows
-        const bool direct = !w.hidden && a.dw.splits == 1, add = w.hidden ? !a.first_piece : direct && a.add;
+        const bool direct = !w.hidden && a.dw.splits == 1, behind = w.hidden && !a.first_piece;
         const uint32_t end = w.hidden ? a.rows : min(a.piece_cols, a.words - a.first_word), last = col0 < end ? min(64u, end - col0) : 0;   // columns of the thread's
         float* p = (w.hidden ? a.dh.out : a.dw.out) + (uint64_t(w.split) * (w.hidden ? a.rows : a.piece_cols) + (direct ? a.first_word : 0) + col0) * a.width + row;
         if (direct) {
@@ -471,10 +472,20 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
 #pragma unroll
           for (int i = 0; i < 64; ++i) acc[i] = acc[i] * by1 * by2;
         }
+        if (direct && a.add) {   // sixteen of the caller's numbers on their way together
+#pragma unroll
+          for (uint32_t q = 0; q < 64; q += 16) {
+            float before[16];
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) before[i] = q + i < last ? __ldcg(p + uint64_t(q + i) * a.width) : 0.0f;
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) acc[q + i] += before[i];
+          }
+        }
 #pragma unroll
         for (uint32_t i = 0; i < 64; ++i)
           if (i < last) {
-            if (add) add_behind(p + uint64_t(i) * a.width, acc[i]);
+            if (behind) add_behind(p + uint64_t(i) * a.width, acc[i]);
             else p[uint64_t(i) * a.width] = acc[i];
           }
       }
