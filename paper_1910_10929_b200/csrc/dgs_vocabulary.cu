@@ -77,15 +77,23 @@ __device__ __forceinline__ void tmem_load16(uint32_t at, float (&v)[16]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
-// The power of two that takes a largest magnitude (its bits) to [2^14, 2^15), kept where it is a normal number, and its reciprocal.  Infinities and NaN: 1.
-__device__ __forceinline__ float up_of(uint32_t largest) {
-  const int e = int(largest >> 23);   // biased exponent
-  if (e == 0xff || largest == 0) return 1.0f;
-  return __uint_as_float(uint32_t(min(127 + 14 + 127 - max(e, 1), 253)) << 23);
+// The power of two that takes a largest finite magnitude (its bits) to [2^14, 2^15), kept where it is a normal number, and its reciprocal.
+__device__ __forceinline__ uint32_t down_exponent(uint32_t largest) { return uint32_t(max(int(largest >> 23) - 14, 1)); }   // with its bias: 1 .. 240
+__device__ __forceinline__ float up_of(uint32_t largest) { return __uint_as_float((254 - down_exponent(largest)) << 23); }
+__device__ __forceinline__ float down_of(uint32_t largest) { return __uint_as_float(down_exponent(largest) << 23); }
+// The reciprocal as two factors of about its square root: of two reciprocals the product, and a sum under one of them, may lie outside f32's range where the result does not.
+struct Down {
+  float a, b;
+};
+__device__ __forceinline__ Down downs_of(uint32_t largest) {
+  const uint32_t e = down_exponent(largest), half = e / 2;
+  return {__uint_as_float((63 + half) << 23), __uint_as_float((64 + e - half) << 23)};
 }
-__device__ __forceinline__ float down_of(uint32_t largest) { return __uint_as_float((254u << 23) - __float_as_uint(up_of(largest))); }
+__device__ __forceinline__ Down operator*(Down x, Down y) { return {x.a * y.a, x.b * y.b}; }   // from 2^-128 on: exact
+__device__ __forceinline__ float operator*(float v, Down x) { return v * x.a * x.b; }
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -__builtin_huge_valf();
+constexpr float kLeastPower = 0x1p-126f, kMostPower = 0x1p127f;
 
 // One of the two products of a piece's s.
 struct Product {
@@ -383,7 +391,8 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
 #pragma unroll
           for (uint32_t i = 0; i < 2; ++i) word_by[i] = word0 + i * 32 + lane < a.words ? a.row_w[word0 + i * 32 + lane] : 0.0f;
 #pragma unroll
-          for (uint32_t i = 0; i < 64; ++i) acc[i] = acc[i] * row_by * __shfl_sync(0xffffffffu, word_by[i / 32], i % 32);
+          for (uint32_t i = 0; i < 64; ++i)   // a logit between f32's ends stays there: their product first, which neither passes them nor makes 0 of an infinity's power of two
+            acc[i] *= fminf(fmaxf(row_by * __shfl_sync(0xffffffffu, word_by[i / 32], i % 32), kLeastPower), kMostPower);
         }
         if (word0 + 64 > a.words) {
 #pragma unroll
@@ -468,9 +477,9 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
         const uint32_t end = w.hidden ? a.rows : min(a.piece_cols, a.words - a.first_word), last = col0 < end ? min(64u, end - col0) : 0;   // columns of the thread's
         float* p = (w.hidden ? a.dh.out : a.dw.out) + (uint64_t(w.split) * (w.hidden ? a.rows : a.piece_cols) + (direct ? a.first_word : 0) + col0) * a.width + row;
         if (direct) {
-          const float by1 = down_of(a.most_h[row]), by2 = down_of(*a.most_g);
+          const Down by_both = downs_of(a.most_h[row]) * downs_of(*a.most_g);
 #pragma unroll
-          for (int i = 0; i < 64; ++i) acc[i] = acc[i] * by1 * by2;
+          for (int i = 0; i < 64; ++i) acc[i] = acc[i] * by_both;
         }
         if (direct && a.add) {   // sixteen of the caller's numbers on their way together
 #pragma unroll
@@ -561,7 +570,7 @@ __global__ void __launch_bounds__(256) k_head_most(const __grid_constant__ Head 
   } else {
     uint32_t v = 0;
     for (uint32_t r = (blockIdx.x - blocks_w - blocks_h) * 256 + threadIdx.x; r < a.rows; r += (gridDim.x - blocks_w - blocks_h) * 256)
-      if (target_of(a, r, true) >= 0) v = max(v, __float_as_uint(a.dloss[uint64_t(r) * a.dloss_step]) & 0x7fffffffu);
+      if (target_of(a, r, true) >= 0) v = max(v, finite_bits(a.dloss[uint64_t(r) * a.dloss_step]));
     v = __reduce_max_sync(0xffffffffu, v);
     if (v && threadIdx.x % 32 == 0) atomicMax(most_g, v);
   }
@@ -720,7 +729,7 @@ __global__ void __launch_bounds__(256) k_head_words(const __grid_constant__ Head
   wait_for_last_kernel();
   const uint32_t lane = threadIdx.x % 32, words = min(a.piece_cols, a.words - a.first_word);
   const uint64_t each = uint64_t(a.piece_cols) * a.width, units = uint64_t(words) * spans;
-  const float by2 = down_of(*a.most_g);
+  const Down by_g = downs_of(*a.most_g);
   for (uint64_t u = uint64_t(blockIdx.x) * 8 + threadIdx.x / 32; u < units; u += uint64_t(gridDim.x) * 8) {
     const uint32_t word = units >> 32 ? uint32_t(u / spans) : uint32_t(u) / spans, col0 = uint32_t(u - uint64_t(word) * spans) * kSpan;
     float v[8] = {};
@@ -736,7 +745,7 @@ __global__ void __launch_bounds__(256) k_head_words(const __grid_constant__ Head
       const uint32_t c = col0 + i * 32 + lane;
       if (c < a.width) {
         float* p = dw + (uint64_t(a.first_word) + word) * a.width + c;
-        const float x = v[i] * down_of(a.most_h[c]) * by2;
+        const float x = v[i] * (downs_of(a.most_h[c]) * by_g);
         *p = a.add ? *p + x : x;
       }
     }
@@ -758,7 +767,7 @@ __global__ void __launch_bounds__(256) k_head_join(const __grid_constant__ Head 
   __syncthreads();
   if (warp || c >= a.width) return;
   for (uint32_t q = 1; q < 8; ++q) v += s_sum[q][lane];
-  if (a.most_w) v = v * down_of(a.most_w[c]) * down_of(*a.most_g);   // NULL: the parts are what they stand for
+  if (a.most_w) v = v * (downs_of(a.most_w[c]) * downs_of(*a.most_g));   // NULL: the parts are what they stand for
   dh[row * stride + c] = Elem<T>::put(target_of(a, row, false) >= 0 ? v : 0.0f);   // also where W holds infinities
 }
 // And from few, likewise a warp for 256 columns.
@@ -767,7 +776,7 @@ __global__ void __launch_bounds__(256) k_head_hidden(const __grid_constant__ Hea
   wait_for_last_kernel();
   const uint32_t lane = threadIdx.x % 32;
   const uint64_t each = uint64_t(a.rows) * a.width, units = uint64_t(a.rows) * spans;
-  const float by2 = down_of(*a.most_g);
+  const Down by_g = downs_of(*a.most_g);
   for (uint64_t u = uint64_t(blockIdx.x) * 8 + threadIdx.x / 32; u < units; u += uint64_t(gridDim.x) * 8) {
     const uint32_t row = units >> 32 ? uint32_t(u / spans) : uint32_t(u) / spans, col0 = uint32_t(u - uint64_t(row) * spans) * kSpan;
     float v[8] = {};
@@ -778,10 +787,13 @@ __global__ void __launch_bounds__(256) k_head_hidden(const __grid_constant__ Hea
         if (c < a.width) v[i] += parts[s * each + uint64_t(row) * a.width + c];
       }
     const bool live = target_of(a, row, false) >= 0;   // others: 0, also where W holds infinities
+    uint32_t most[8];   // on their way together: 2000 x 512 x 8000 10 us, 22 where each is asked for as it is needed
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) most[i] = col0 + i * 32 + lane < a.width ? a.most_w[col0 + i * 32 + lane] : 0;
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
       const uint32_t c = col0 + i * 32 + lane;
-      if (c < a.width) dh[row * stride + c] = Elem<T>::put(live ? v[i] * down_of(a.most_w[c]) * by2 : 0.0f);
+      if (c < a.width) dh[row * stride + c] = Elem<T>::put(live ? v[i] * (downs_of(most[i]) * by_g) : 0.0f);
     }
   }
 }
