@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(256, VEC || sizeof(T) == 4 ? 3 : 5) k_experts_
 }
 
 bool slots_ok(const uint32_t* order, const uint32_t* place, uint32_t k, uint64_t tokens) {
-  return k && k <= DGS_ROUTE_MAX_K && tokens < (1ull << 31) / k && aligned(order, 4) && aligned(place, 4) && (tokens == 0 || place);
+  return k && k <= DGS_ROUTE_MAX_K && tokens <= ((1ull << 31) - 1) / k && aligned(order, 4) && aligned(place, 4) && (tokens == 0 || place);
 }
 bool rows_fit(const dgs_matrix* one, const dgs_matrix* all, uint32_t k) {
   return one->cols == all->cols && one->type == all->type && one->cols <= (1u << 30) && all->rows == one->rows * k;
