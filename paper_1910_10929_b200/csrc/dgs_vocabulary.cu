@@ -880,13 +880,20 @@ Work hidden_of(uint64_t n, uint32_t d, uint32_t tiles, uint32_t type) {
 }
 
 // Few rows go without tensor cores where there are not many products in all.  Loss and gradient have borders of their own, so that between them the two form logits in different ways,
-// each within its own roundings of them.  Here / with tensor cores, us a call.  Loss, 16 bits: 64 x 512 x 1000 10.5 / 12.5,
-// 3 x 2048 x 8000 15 / 21, 8 of them 25 / 21, 1 x 768 x 50257 20 / 33, 3 of them 32 / 33, 8 47 / 33; f32: 16 x 2048 x 8000 49 / 64, 37 101 / 64, 16 x 768 x 50257
-// 81 / 102, 37 178 / 102.  Gradient, 16 bits: 37 x 512 x 1000 21 / 35, 64 27 / 37, 1 x 2048 x 8000 85 / 87, 3 of them 97 / 86, 1 x 768 x 50257 182 / 161; f32:
-// 64 x 512 x 1000 25 / 52, 8 x 2048 x 8000 91 / 155, 16 161 / 160, 8 x 768 x 50257 181 / 285, 16 300 / 290.
+// each within its own roundings of them.  A warp without tensor cores goes through whole spans of 256 columns and has as much to do beside them again, and rows cost more the more there are,
+// while 64 rows cost the tensor cores what one does.  Here / with tensor cores, us a call, rows x width x words.
+//   loss, 16 bits: 8 x 16 x 5000 10.4 / 10.4, 20000 18.6 / 16.4; 37 x 16 x 1000 10.3 / 10.3, 2500 14.5 / 10.3; 64 x 512 x 1000 10.4 / 12.4, 2500 16.5 / 12.3; 1 x 768 x 50257 18.5 / 33.6;
+//     8 x 768 x 8000 12.4 / 14.4, 20000 24.7 / 20.5; 8 x 2048 x 2500 15.6 / 18.5, 8000 20.6 / 20.1
+//   loss, f32: 37 x 16 x 5000 18.5 / 14.5; 64 x 768 x 1000 12.4 / 22.7, 2500 25.2 / 22.8; 37 x 768 x 2500 19.7 / 23.0, 8000 40.2 / 26.7; 16 x 768 x 20000 50.2 / 55.1
+//   gradient, 16 bits: 64 x 16 x 1000 20.6 / 26.8, 2500 55.5 / 26.9; 37 x 512 x 1000 18.5 / 25.8, 2500 50.1 / 26.7; 8 x 768 x 8000 36.9 / 37.0; 1 x 768 x 50257 158 / 138;
+//     3 x 2048 x 2500 47.2 / 39.0; 16 x 2048 x 1000 30.8 / 36.7
+//   gradient, f32: 64 x 16 x 1000 20.6 / 34.4, 8000 57.5 / 40.6; 64 x 512 x 1000 24.7 / 39.0, 2500 82.1 / 41.1; 8 x 768 x 50257 191 / 276; 16 x 2048 x 2500 88.3 / 80.7, 8000 141 / 142
+// (Over 384 such sizes from 16 columns to 2048 the choice costs 0.5 to 1.6 % against the better of the two each time; by products alone, rows x width x words, it cost 5 to 15 %, at 64 x 16 seven times.)
 bool few_rows(uint64_t n, uint64_t v, uint32_t d, uint32_t type, bool grad) {
-  const uint64_t rows = n == 1 ? 1 : n <= 4 ? 4 : up_to(n, 8), most = type == DGS_TYPE_F32 ? (grad ? 310000000 : 640000000) : grad ? 36000000 : 100000000;
-  return n <= kFewRows && v * d <= most / rows;
+  const uint64_t rows = n == 1 ? 1 : n <= 4 ? 4 : up_to(n, 8), spans = up_to(d, 256);
+  if (n > kFewRows) return false;
+  if (type == DGS_TYPE_F32) return rows * rows * v * (spans + (grad ? 256 : 512)) <= (grad ? 4000000000ull : 5300000000ull);
+  return rows * (rows + (grad ? 16 : 32)) * v * (spans + (grad ? 0 : 512)) <= (grad ? 1360000000ull : 4300000000ull);
 }
 
 int plan_head(const dgs_matrix* h, const dgs_matrix* w, bool grad, HeadPlan* out) {
