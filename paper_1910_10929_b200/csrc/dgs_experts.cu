@@ -51,9 +51,9 @@ __global__ void __launch_bounds__(256) k_experts_gather(const __grid_constant__ 
 
 // out[t] = sum over j of weight[t][j] y[place[t][j]], slots ascending, in f32.  weight NULL: 1, which is the gather's gradient.  Bound by HBM: the
 // rows of four slots (two in f32 and of rows that begin anywhere) are on their way together, in 48 warps an SM (eight slots in 24 warps: 32768 x 2048, top 8 237 us, 187 so; 48 warps that go on to the next
-// token 212).
+// token 212).  Rows of f32 that begin anywhere go in 32, which need not spill registers: 40000 x 33, top 8 27 us (31 in 48 warps), 16384 x 767, top 8 77 (80).
 template <class T, bool VEC>
-__global__ void __launch_bounds__(256, 6) k_experts_combine(const __grid_constant__ Rows a, const float* weight, const T* y, T* out) {
+__global__ void __launch_bounds__(256, VEC || sizeof(T) == 2 ? 6 : 4) k_experts_combine(const __grid_constant__ Rows a, const float* weight, const T* y, T* out) {
   constexpr uint32_t J = VEC && sizeof(T) == 2 ? 4 : 2;
   const uint32_t lane = threadIdx.x % 32;
   const uint64_t units = uint64_t(a.tokens) * a.chunks, step = uint64_t(gridDim.x) * 8;
