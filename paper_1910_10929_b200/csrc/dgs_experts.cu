@@ -226,7 +226,8 @@ extern "C" int dgs_experts_combine_grad(const dgs_matrix* dout, const dgs_matrix
   a.in_stride = y->stride;
   a.mid_stride = dout->stride;
   a.out_stride = dy->stride;
-  // few tokens: their columns are shared out, so that no warp makes more trips to memory than it has to
+  // Few tokens: their columns are shared out, so that no warp makes more trips to memory than it has to.  Where 32 warps an SM are the aim / 8 / 128, us: 1000 x 8192 with top 8 in bfloat16
+  // 54 / 58 / 55, 4000 x 2048 with top 8 55 / 66 / 53, 2500 x 2048 with top 2 16.5 / 16.5 / 19.6, 8000 x 1024 with top 2 24.7 / 24.7 / 30.9.
   a.warps = 1;
   while (a.warps < 8 && a.warps < a.chunks && uint64_t(a.tokens) * a.warps < kSms * 32) a.warps *= 2;
   const uint32_t grid = uint32_t(std::min<uint64_t>((uint64_t(a.tokens) * a.warps + 7) / 8, 1u << 22));

@@ -751,7 +751,8 @@ __global__ void __launch_bounds__(256) k_head_words(const __grid_constant__ Head
     }
   }
 }
-// dh from many partial results: 32 columns of a row a CTA, each eighth part a warp.  (128 x 768 of 32 parts: 38 us if a warp adds up all of them for 256 columns.)
+// dh from many partial results: 32 columns of a row a CTA, each eighth part a warp.  A gradient by this / by k_head_hidden, us, rows x width x words: from up to four parts 700 x 512 x 3000
+// 44 / 38, 1000 x 256 x 4000 43 / 40; from six or eight 70 x 2048 x 8000 76 / 78, 1500 x 128 x 1000 49 / 47; from more 100 x 128 x 5000 31 / 45, 128 x 768 x 50257 138 / 149.
 constexpr uint32_t kManyParts = 6;
 template <class T>
 __global__ void __launch_bounds__(256) k_head_join(const __grid_constant__ Head a, const float* parts, uint32_t count, T* dh, uint64_t stride, uint32_t spans) {
@@ -857,7 +858,9 @@ Shares share_out(const Work& words, const Work& hidden) {
   return best;
 }
 
-constexpr uint64_t kPieceBytes = 320ull << 20;   // of s, where one tile of words does not take more
+// Of s, where one tile of words does not take more.  At 160 / 320 / 640 MB, us a gradient: 8192 x 768 x 50257 in bfloat16 2510 / 2370 / 2390 (by itself, cool), 16384 x 256 x 20000 1018 / 912 / 850,
+// 1000 x 768 x 50257 363 / 352 / 352: what twice the memory would give is not worth it to a caller who keeps a model there.
+constexpr uint64_t kPieceBytes = 320ull << 20;
 
 struct HeadPlan {
   uint32_t parts, stride, piece_tiles, pieces, row_blocks;
@@ -923,7 +926,9 @@ int plan_head(const dgs_matrix* h, const dgs_matrix* w, bool grad, HeadPlan* out
   if (n && few_rows(n, v, d, h->type, grad)) {
     p->few = n == 1 ? 1 : n <= 4 ? 4 : 8;
     if (grad) {
-      p->few_words = v <= 8 * 2 * kSms ? 8 : 32;   // small tiles where the words are few
+      // Small tiles where the words are few; their CTAs fill an SM, two of the others share one.  Here / with 32 words, us a call, rows x width x words in bfloat16 (f32 alike): 3 x 512 x 1184
+      // 12.3 / 14.5, 2368 18.5 / 14.4; 37 x 512 x 1184 18.8 / 51, 2368 33 / 51, 3000 43 / 51, 6000 80 / 64; 64 x 16 x 3000 49 / 57, 6000 94 / 62; 64 x 1024 x 3000 146 / 162, 6000 314 / 215.
+      p->few_words = v <= 8 * kSms * (n <= 4 ? 1 : 3) ? 8 : 32;
       p->few_tiles = ceil_div(v, p->few_words);
       p->few_ctas = std::min(p->few_tiles, kSms * 2);
       p->part_h = up_to(uint64_t(p->few_ctas) * n * d * 4, 256);
