@@ -903,14 +903,16 @@ int plan_head(const dgs_matrix* h, const dgs_matrix* w, bool grad, HeadPlan* out
   if (!head_ok(h, w)) return DGS_EINVAL;
   const uint64_t n = h->rows, v = w->rows;
   const uint32_t d = h->cols;
-  // The last plan of this thread: a call asks twice, and a training loop again and again.
+  // The last plans of this thread, of a loss and of a gradient: a call and its question for bytes ask for one, and a training loop for both in turn.
   struct Key {
-    uint64_t n, v, d, type, copies, grad;
+    uint64_t n, v, d, type, copies;
   };
-  thread_local Key last = {};
-  thread_local HeadPlan plan;
+  thread_local Key keys[2] = {};
+  thread_local HeadPlan plans[2];
+  Key& last = keys[grad];
+  HeadPlan& plan = plans[grad];
   HeadPlan* const p = &plan;
-  const Key key = {n, v, d, h->type, uint64_t(!in_place(h)) | uint64_t(!in_place(w)) << 1, grad};
+  const Key key = {n, v, d, h->type, uint64_t(!in_place(h)) | uint64_t(!in_place(w)) << 1};
   if (last.d && memcmp(&key, &last, sizeof(key)) == 0) {
     *out = plan;
     return DGS_OK;
