@@ -102,7 +102,7 @@ struct Product {
 };
 struct Head {
   uint32_t rows, width, words;      // N, D, V
-  uint32_t m_tiles, n_tiles, tiles, steps, chunk;   // logits
+  uint32_t m_tiles, n_tiles, tiles, steps, chunk, skip;   // logits; skip: steps that a tile's first chunk is short of
   uint32_t first_word, piece_cols;  // of the piece (a multiple of 256 in the workspace)
   uint32_t idesc;
   uint32_t wide_targets, dloss_step;
@@ -190,7 +190,7 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
   __shared__ __align__(8) uint64_t s_full[ST], s_empty[ST], s_loaded[ST], s_sum_full[2], s_sum_empty[2], s_done;
   __shared__ uint32_t s_tmem;
   const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32, rank = cta_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
-  const uint32_t stages = (smem_at(raw) + 1023u) & ~1023u, CH = MODE == kGrads ? S::kChunk : a.chunk;
+  const uint32_t stages = (smem_at(raw) + 1023u) & ~1023u, CH = MODE == kGrads ? S::kChunk : a.chunk, SKIP = MODE == kGrads ? 0 : a.skip;
 
   if (warp == kSumWarps) {
     tmem_alloc(&s_tmem, kHeadTmem);
@@ -251,7 +251,8 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
       for (uint32_t i = 0; alive && head_tile<MODE>(a, pair, pairs, i, &w); ++i) {
         for (uint32_t s = 0; s < w.steps; ++s, ++it) {
           const uint32_t st = it % ST, acc = tmem + (chunk & 1) * 256;
-          const bool begins = in == 0;
+          const bool begins = s == 0 || in == 0;
+          if (s == 0) in = SKIP;
           if (begins && chunk >= 2) alive = warp_wait(smem_at(&s_sum_empty[chunk & 1]), (chunk / 2 - 1) & 1);
           alive = alive && warp_wait(smem_at(&s_full[st]), it / ST & 1);
           if (!alive) break;
@@ -352,7 +353,7 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
     HeadTile w;
     const float up_g = MODE == kSlope ? up_of(*a.most_g) : 0.0f;
     for (uint32_t ordinal = 0; alive && head_tile<MODE>(a, pair, pairs, ordinal, &w); ++ordinal) {
-      const uint32_t chunks = (w.steps + CH - 1) / CH, row = w.m0 + mine, col0 = w.n0 + group * 64;
+      const uint32_t chunks = (w.steps + SKIP + CH - 1) / CH, row = w.m0 + mine, col0 = w.n0 + group * 64;
       // what the end of the tile needs comes while its products are formed
       int target = -1;
       float lse = 0.0f, by = 1.0f;   // by: dloss; f32 logits: what the row is multiplied with
@@ -425,9 +426,9 @@ k_head(const __grid_constant__ Head a, const __grid_constant__ CUtensorMap map_a
             for (int i = 0; i < 64; ++i) acc[i] = kNone;
           }
           const float g = target < 0 ? 0.0f : by * up_g;
-          // By way of 4 KB of shared memory for each warp, so that eight lanes write a row's 128 bytes.  Bound by these stores: 5632 words of 8192 x 768 are 184 MB
-          // and 74 us, 60 with the first part alone, 51 without.  (Straight from the registers, 32 bytes a lane: 78.  By copies from shared memory, with
-          // their fences and waits for the buffer: 88.)
+          // By way of 4 KB of shared memory for each warp, so that eight lanes write a row's 128 bytes.  Bound by these stores: 10240 words of 8192 x 768 are 336 MB and
+          // 122 us, for products of 79.  (When 5632 words, 184 MB, were measured alone: 74, 60 with the first part alone, 51 without; straight from the registers, 32 bytes a lane, 78; by
+          // copies from shared memory, with their fences and waits for the buffer, 88.)
           const uint32_t stage = stages + SLOTS * TILE + warp * 4096;
           const uint32_t mine_at = stage + lane * 128 + ((lane & 7) << 4);   // of a row's first 16 bytes; the q-th are at mine_at ^ q << 4
           unsigned char* const to = a.s + (uint64_t(w.m0 / 128 + rank) * (a.piece_cols / 64) + col0 / 64) * kBlockBytes + quarter * 4096 + lane * 16;
@@ -1088,7 +1089,9 @@ void logit_chunks(Head* a) {
   constexpr uint32_t kMine = Step<MODE, P, P>::kRows, kLong = Step<kLoss, P, P>::kRows;
   static_assert(kLong % kMine == 0 && Step<MODE, P, P>::kChunk * kMine == Step<kLoss, P, P>::kChunk * kLong, "the same values in loss and gradient");
   a->steps = ceil_div(a->width, kMine);
-  a->chunk = std::min(ceil_div(ceil_div(a->width, kLong), 2), Step<kLoss, P, P>::kChunk) * (kLong / kMine);
+  const uint32_t steps = ceil_div(a->width, kLong), chunk = std::min(ceil_div(steps, 2), Step<kLoss, P, P>::kChunk);
+  a->chunk = chunk * (kLong / kMine);
+  a->skip = (ceil_div(steps, chunk) * chunk - steps) * (kLong / kMine);   // the last step's values may be few: what a chunk is short of is at the other end
 }
 template <int MODE>
 void logit_steps(uint32_t parts, Head* a) { parts == 2 ? logit_chunks<MODE, 2>(a) : logit_chunks<MODE, 1>(a); }
