@@ -884,20 +884,23 @@ Work hidden_of(uint64_t n, uint32_t d, uint32_t tiles, uint32_t type) {
 }
 
 // Few rows go without tensor cores where there are not many products in all.  Loss and gradient have borders of their own, so that between them the two form logits in different ways,
-// each within its own roundings of them.  A warp without tensor cores goes through whole spans of 256 columns and has as much to do beside them again, and rows cost more the more there are,
-// while 64 rows cost the tensor cores what one does.  Here / with tensor cores, us a call, rows x width x words.
-//   loss, 16 bits: 8 x 16 x 5000 10.4 / 10.4, 20000 18.6 / 16.4; 37 x 16 x 1000 10.3 / 10.3, 2500 14.5 / 10.3; 64 x 512 x 1000 10.4 / 12.4, 2500 16.5 / 12.3; 1 x 768 x 50257 18.5 / 33.6;
-//     8 x 768 x 8000 12.4 / 14.4, 20000 24.7 / 20.5; 8 x 2048 x 2500 15.6 / 18.5, 8000 20.6 / 20.1
-//   loss, f32: 37 x 16 x 5000 18.5 / 14.5; 64 x 768 x 1000 12.4 / 22.7, 2500 25.2 / 22.8; 37 x 768 x 2500 19.7 / 23.0, 8000 40.2 / 26.7; 16 x 768 x 20000 50.2 / 55.1
-//   gradient, 16 bits: 64 x 16 x 1000 20.6 / 26.8, 2500 55.5 / 26.9; 37 x 512 x 1000 18.5 / 25.8, 2500 50.1 / 26.7; 8 x 768 x 8000 36.9 / 37.0; 1 x 768 x 50257 158 / 138;
-//     3 x 2048 x 2500 47.2 / 39.0; 16 x 2048 x 1000 30.8 / 36.7
-//   gradient, f32: 64 x 16 x 1000 20.6 / 34.4, 8000 57.5 / 40.6; 64 x 512 x 1000 24.7 / 39.0, 2500 82.1 / 41.1; 8 x 768 x 50257 191 / 276; 16 x 2048 x 2500 88.3 / 80.7, 8000 141 / 142
-// (Over 384 such sizes from 16 columns to 2048 the choice costs 0.5 to 1.6 % against the better of the two each time; by products alone, rows x width x words, it cost 5 to 15 %, at 64 x 16 seven times.)
+// each within its own roundings of them.  Beside the products (a wide vocabulary is read as fast either way) it counts what a warp does without tensor cores: whole spans of 256 columns, for the
+// loss as much again as 1024 columns beside them, and more for each row the more rows there are, while the tensor cores take 64 rows as they take one.  A loss of up to 1000 words ends before
+// that shows.  Here / with tensor cores, us a call, rows x width x words:
+//   loss, 16 bits: 8 x 16 x 8000 10.4 / 10.5, 20000 18.5 / 14.6; 37 x 16 x 1000 10.4 / 10.4, 2500 14.5 / 10.3; 64 x 512 x 1000 10.4 / 12.3, 2500 16.5 / 12.4; 1 x 768 x 50257 18.6 / 30.9;
+//     8 x 768 x 8000 12.2 / 14.4, 20000 24.7 / 20.6; 8 x 2048 x 5000 18.7 / 19.0, 8000 20.6 / 20.4
+//   loss, f32: 16 x 16 x 50257 47.2 / 41.4; 37 x 768 x 2500 20.4 / 22.7, 5000 28.0 / 25.2; 64 x 768 x 1000 13.0 / 22.6, 2500 25.7 / 22.6; 16 x 768 x 20000 50.1 / 55.0; 8 x 2048 x 50257 112 / 271
+//   gradient, 16 bits: 8 x 16 x 20000 32.9 / 40.2, 50257 60.2 / 62.8; 64 x 16 x 1000 20.6 / 26.8, 2500 48.5 / 26.9; 37 x 512 x 1000 18.6 / 24.8, 2500 42.5 / 26.8; 1 x 768 x 20000
+//     57.7 / 69.9, 50257 158 / 136; 8 x 768 x 5000 32.9 / 32.9; 16 x 2048 x 1000 30.8 / 35.6; 8 x 2048 x 2500 59.5 / 39.1
+//   gradient, f32: 64 x 16 x 2500 43.3 / 34.9, 5000 55.2 / 38.3; 64 x 512 x 1000 25.1 / 39.0, 2500 61.6 / 41.1; 8 x 768 x 50257 188 / 275; 16 x 2048 x 5000 119 / 116; 24 x 2048 x 5000 169 / 118
+// (Over 784 such sizes, 16 to 2048 columns, the choice costs 0.3 to 0.8 % against the better of the two each time, at the worst a half; by products alone it cost 4 to 13 % and up to six times,
+// by spans and rows alone 1 % and up to 2.4 times.)
 bool few_rows(uint64_t n, uint64_t v, uint32_t d, uint32_t type, bool grad) {
-  const uint64_t rows = n == 1 ? 1 : n <= 4 ? 4 : up_to(n, 8), spans = up_to(d, 256);
   if (n > kFewRows) return false;
-  if (type == DGS_TYPE_F32) return rows * rows * v * (spans + (grad ? 256 : 512)) <= (grad ? 4000000000ull : 5300000000ull);
-  return rows * (rows + (grad ? 16 : 32)) * v * (spans + (grad ? 0 : 512)) <= (grad ? 1360000000ull : 4300000000ull);
+  const bool f32 = type == DGS_TYPE_F32;
+  const uint64_t rows = n == 1 ? 1 : n <= 4 ? 4 : up_to(n, 8), products = rows * v * d, spans = up_to(d, 256);
+  if (grad) return products <= (f32 ? 465000000 : 36000000) && rows * (f32 ? rows : rows + 16) * v * spans <= (f32 ? 3760000000 : 1330000000);
+  return products <= (f32 ? 960000000 : 200000000) && (v <= 1000 || rows * rows * v * (spans + 1024) <= (f32 ? 10600000000 : 1450000000));
 }
 
 int plan_head(const dgs_matrix* h, const dgs_matrix* w, bool grad, HeadPlan* out) {
