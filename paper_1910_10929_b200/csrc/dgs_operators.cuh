@@ -18,7 +18,7 @@ namespace dgs {
 // Defined in dgs_checkpoint.cu; the other files get its address as a kernel argument.
 int* operator_status_word();
 
-constexpr uint32_t kSms = 148;    // of a B200: sizes of grids, nothing that results depend on
+constexpr uint32_t kSms = 148;    // of a B200: sizes of grids; results depend on it where sums are split among CTAs (dgs_weight.cu, dgs_vocabulary.cu, dweight in dgs_experts.cu), by the order of f32 additions
 constexpr uint32_t kBlock = 32;   // values under one scale byte
 
 // ---- the caller's matrices ------------------------------------------------------------------
